@@ -77,7 +77,7 @@
 extern "C" {
 #endif
 
-enum corm_dtype { CORM_F32 = 0, CORM_BF16 = 1, CORM_BIT = 2 /* score_dtype only */ };
+enum corm_dtype { CORM_F32 = 0, CORM_BF16 = 1, CORM_BIT = 2 /* score_dtype only */, CORM_I8 = 3, CORM_E4M3 = 4 /* codes only */ };
 
 enum corm_status {
   CORM_OK = 0,
@@ -91,7 +91,8 @@ enum corm_status {
 enum corm_dev_status {
   CORM_DEV_UNIT_FULL = 1, /* append skipped: lens == Lcap                                        */
   CORM_DEV_BAD_STEP = 2,  /* t < 1 or t > Tcap or a position outside [0,Tcap): record skipped   */
-  CORM_DEV_BAD_LENS = 4   /* lens outside [0,Lcap]: clamped                                      */
+  CORM_DEV_BAD_LENS = 4,  /* lens outside [0,Lcap]: clamped                                      */
+  CORM_DEV_BAD_BLOCK = 8  /* a listed block beyond the unit's slots (or below -1): skipped       */
 };
 
 typedef struct corm_desc {
@@ -272,6 +273,85 @@ int corm_prefill_seed(const corm_desc* desc, const void* q_tail, int32_t m, void
                       int32_t* pos, int32_t* last_hit, const int32_t* t, int32_t* t_first, void* score_ring,
                       uint8_t* keep, int32_t* kept_idx, void* workspace, size_t workspace_bytes, int32_t* status,
                       void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------
+ * What else bounds the reads of a decode step: fewer bits a key, fewer blocks of keys, fewer keys by another rule.
+ * The calls below have the conventions above: device pointers, caller-owned memory, errors on the host before anything
+ * is launched.  A BLOCK is 64 consecutive slots of a unit, slots 64*j .. 64*j+63; nblk = ceil(Lcap / 64).
+ * Preconditions as everywhere: finite q, K, V.  Of the descriptor they read B, Hq, Hkv, d, Lcap, kv_dtype, sm_scale and,
+ * where it says so, r; the other fields have to be valid and do nothing.
+ *
+ * corm_blocks_workspace_bytes: the workspace of corm_q8_attend, corm_block_select, corm_block_attend and
+ * corm_evict_mask_weight (256-byte aligned).  Nothing in it has to be prepared or survives a call, so calls on one stream, and
+ * captured graphs that are replayed one after the other, may share it. */
+int corm_blocks_workspace_bytes(const corm_desc* desc, size_t* bytes);
+
+/* 8-bit cache.  Full blocks are held in codes with a scale each; the lens % 64 newest rows, which fill no block yet, stay in
+ * kv_dtype (the tail).  A block is quantised once, when it gets full, from the rows themselves:
+ *   amax = largest magnitude of the block's 64 x d elements (K and V apart);  Q = 127 (CORM_I8) or 448 (CORM_E4M3)
+ *   scale = fp32(amax / Q);  code = x * fp32(Q / amax) in fp32, rounded to the nearest (even) integer / e4m3 (OCP) value
+ * (a block with amax < 2^-100 is held as zeros with scale 0).  The key of a slot is then scale * code.
+ *   K_codes  [B, Hkv, nblk, d/64, 64, 64]  1 byte    [.., block, channel / 64, slot % 64, channel % 64]
+ *   V_codes  [B, Hkv, nblk, d, 64]         1 byte    [.., block, channel, slot % 64]
+ *   k_scale, v_scale  [B, Hkv, nblk]       float32
+ *   K_tail, V_tail    [B, Hkv, 64, d]      kv_dtype  row slot % 64 of the unfinished block
+ *   lens     [B, Hkv]                      int32
+ * Codes and scales of blocks that are not full, and tail rows at or above lens % 64, are never read.
+ *
+ * corm_q8_append: rows k_new, v_new [B, Hkv, n, d] (kv_dtype) to slots lens ..; the first n_new[b] rows of a
+ * sequence (device int32 [B], held to [0, n]; NULL = n), so a batch of prompts may be padded: rows beyond are not read.
+ * lens_out [B, Hkv] receives the new lengths and may be lens.  A unit that has no room for all its rows gets none
+ * (CORM_DEV_UNIT_FULL).  bounds (may be NULL): the block bounds of corm_block_bounds, kept up for the appended rows.
+ * 1 <= n <= Lcap. */
+int corm_q8_append(const corm_desc* desc, int32_t code_dtype, const void* k_new, const void* v_new, int32_t n, const int32_t* n_new,
+                   void* K_codes, void* V_codes, float* k_scale, float* v_scale, void* K_tail, void* V_tail, const int32_t* lens,
+                   int32_t* lens_out, void* bounds, int32_t* status, void* stream);
+
+/* Decode attention (Eq. 1) over the 8-bit cache: out [B, Hq, d] float32; a unit without keys yields 0.
+ * blocks (may be NULL: every block; then nsel = 0): only the slots of the listed blocks, as in corm_block_attend. */
+int corm_q8_attend(const corm_desc* desc, int32_t code_dtype, const void* q, const void* K_codes, const void* V_codes,
+                   const float* k_scale, const float* v_scale, const void* K_tail, const void* V_tail, const int32_t* lens,
+                   const int32_t* blocks, int32_t nsel, float* out, void* workspace, size_t workspace_bytes, int32_t* status,
+                   void* stream);
+
+/* Bounds of the keys of a block: bounds [B, Hkv, nblk, 2, d] (kv_dtype, 16-byte aligned), [.., 0, c] the smallest and [.., 1, c] the
+ * largest element of channel c over the block's slots < lens.  newest = 0: of every block that holds a key; newest > 0: of the
+ * blocks that hold one of the newest `newest` slots (a decode step: 1).  Others are left as they were.  K as in
+ * corm_decode_attend; an eviction moves keys, so their bounds are to be found anew behind it. */
+int corm_block_bounds(const corm_desc* desc, const void* K, const int32_t* lens, int32_t newest, void* bounds, void* stream);
+
+/* The blocks a decode step attends to: the nlast newest blocks of the unit and, of the others, those with the highest upper
+ * bound of a logit of the group, max over its heads of sum_c max(q_c lo_c, q_c hi_c), formed in 64 bits and rounded once to
+ * fp32 (equal ones: the lower block first; not a number: last).  blocks [B, Hkv, nsel] int32: ascending, -1 behind the last where the unit has
+ * fewer than nsel.  1 <= nlast <= nsel <= max(nblk, 512). */
+int corm_block_select(const corm_desc* desc, const void* q, const void* bounds, const int32_t* lens, int32_t nsel, int32_t nlast,
+                      int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Decode attention over the slots < lens of the listed blocks alone, softmax over them: out [B, Hq, d] float32, 0 where nothing is
+ * listed.  blocks [B, Hkv, nsel]: any order, -1 = no block; a block that is listed twice counts twice; one beyond the unit's slots is skipped
+ * (CORM_DEV_BAD_BLOCK).  1 <= nsel <= max(nblk, 512). */
+int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const void* V, const int32_t* lens, const int32_t* blocks,
+                      int32_t nsel, float* out, void* workspace, size_t workspace_bytes, int32_t* status, void* stream);
+
+/* Eviction by accumulated attention weight, a rule beside CORM's: every key has an account, weight [B, Hkv, Lcap] float32, of the
+ * attention that the queries of its group have paid to it.
+ *
+ * corm_decode_attend_weigh: corm_decode_attend's out, and weight[i] = weight_in[i] + sum over the heads of the group of the
+ * normalized scores (Eq. 2), for slots < lens; others are left as they were.  weight may be weight_in.  Workspace, status and
+ * opts as corm_decode_attend (path 2 is taken as 1); neither pos nor t is needed.
+ *
+ * corm_evict_mask_weight: keep [B, Hkv, Lcap] of a unit with lens > budget: the r newest slots (desc->r) and of the others the
+ * budget - r with the greatest weight (equal ones: the lower slot first; not a number: least); all of them where lens <= budget.
+ * budget >= r.  Entries >= lens are left as they were.
+ *
+ * corm_append and corm_compact carry the accounts where they are given in the place of last_hit, whose 4-byte entries they set
+ * to 0 (0.0f) for a new key and move with a survivor.  A whole step is corm_append, corm_decode_attend_weigh and, where
+ * the cache is to be cut, corm_evict_mask_weight and corm_compact. */
+int corm_decode_attend_weigh(const corm_desc* desc, const void* q, const void* K, const void* V, const int32_t* lens,
+                             const float* weight_in, float* weight, float* out, void* workspace, size_t workspace_bytes,
+                             int32_t* status, const corm_launch_opts* opts, void* stream);
+int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int32_t* lens, int32_t budget, uint8_t* keep, void* workspace,
+                           size_t workspace_bytes, void* stream);
 
 /* HIP graph capture.  The step, seeding and standalone calls enqueue kernels only (no allocation, no memset,
  * no host synchronization), so a caller may capture them in a HIP graph on `stream` and replay it with the

@@ -16,15 +16,17 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libcorm.so")
 
-CORM_F32, CORM_BF16, CORM_BIT = 0, 1, 2
+CORM_F32, CORM_BF16, CORM_BIT, CORM_I8, CORM_E4M3 = 0, 1, 2, 3, 4
 CORM_OK, CORM_EINVAL, CORM_EUNSUPPORTED, CORM_ECAPACITY, CORM_EHIP = 0, -1, -2, -3, -4
-CORM_DEV_UNIT_FULL, CORM_DEV_BAD_STEP, CORM_DEV_BAD_LENS = 1, 2, 4
+CORM_DEV_UNIT_FULL, CORM_DEV_BAD_STEP, CORM_DEV_BAD_LENS, CORM_DEV_BAD_BLOCK = 1, 2, 4, 8
+BLOCK = 64   # slots per block of the 8-bit cache and of the calls that choose blocks
 CORM_STATIC_SCRATCH_BYTES = 40 << 20
 
 EXPORTS = ("corm_version", "corm_strerror", "corm_workspace_bytes", "corm_workspace_init", "corm_append",
            "corm_decode_attend", "corm_decode_attend_static", "corm_evict_mask", "corm_evict_mask_summary", "corm_row_density", "corm_compact",
            "corm_decode_step", "corm_step_attend", "corm_step_evict", "corm_decode_step_lazy", "corm_prefill_seed",
-           "corm_selected_path", "corm_threshold")
+           "corm_selected_path", "corm_threshold", "corm_blocks_workspace_bytes", "corm_q8_append", "corm_q8_attend",
+           "corm_block_bounds", "corm_block_select", "corm_block_attend", "corm_decode_attend_weigh", "corm_evict_mask_weight")
 
 
 class corm_desc(ctypes.Structure):
@@ -82,6 +84,15 @@ def lib() -> ctypes.CDLL:
                                             i32p, ctypes.c_int32, ctypes.c_int32, vp, sz, i32p, op, vp]
         L.corm_prefill_seed.argtypes = [dp, vp, ctypes.c_int32, vp, vp, i32p, i32p, i32p, i32p, i32p, vp, vp, i32p,
                                         vp, sz, i32p, vp]
+        i32 = ctypes.c_int32
+        L.corm_blocks_workspace_bytes.argtypes = [dp, ctypes.POINTER(ctypes.c_size_t)]
+        L.corm_q8_append.argtypes = [dp, i32, vp, vp, i32, i32p, vp, vp, vp, vp, vp, vp, i32p, i32p, vp, i32p, vp]
+        L.corm_q8_attend.argtypes = [dp, i32, vp, vp, vp, vp, vp, vp, vp, i32p, i32p, i32, vp, vp, sz, i32p, vp]
+        L.corm_block_bounds.argtypes = [dp, vp, i32p, i32, vp, vp]
+        L.corm_block_select.argtypes = [dp, vp, vp, i32p, i32, i32, i32p, vp, sz, vp]
+        L.corm_block_attend.argtypes = [dp, vp, vp, vp, i32p, i32p, i32, vp, vp, sz, i32p, vp]
+        L.corm_decode_attend_weigh.argtypes = [dp, vp, vp, vp, i32p, vp, vp, vp, vp, sz, i32p, op, vp]
+        L.corm_evict_mask_weight.argtypes = [dp, vp, i32p, i32, vp, vp, sz, vp]
         L.corm_threshold.argtypes = [ctypes.c_float, i32p, ctypes.c_int32, vp, vp]
         for name in EXPORTS:
             if name not in ("corm_version", "corm_strerror"):
@@ -304,6 +315,125 @@ def corm_threshold(c: float, t, n: int, thr, stream=None, check=True) -> int:
     return _check(rc, "corm_threshold") if check else rc
 
 
+# ---- fewer bits, fewer blocks, another eviction rule
+
+_FLOATS = {CORM_F32: torch.float32, CORM_BF16: torch.bfloat16}
+_CODES = {CORM_I8: (torch.int8,), CORM_E4M3: (torch.float8_e4m3fn, torch.uint8, torch.int8)}
+_code_ids = {"i8": CORM_I8, "e4m3": CORM_E4M3, torch.int8: CORM_I8, torch.float8_e4m3fn: CORM_E4M3}
+
+
+def _code(x) -> int:
+    return x if isinstance(x, int) else _code_ids[x]
+
+
+def _dev(x, n: int, dtypes, name: str) -> Optional[int]:
+    """Pointer of an argument whose layout the call takes for granted.  A tensor has to be whole, of the right type, large enough and on the
+    current device (the call goes to one of its streams); a raw pointer is taken as it is."""
+    if not isinstance(x, torch.Tensor):
+        return None if x is None else int(x)
+    if x.dtype not in dtypes:
+        raise ValueError(f"{name}: expected {dtypes}, got {x.dtype}")
+    if not x.is_contiguous() or x.numel() < n:
+        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(x.shape)} with strides {x.stride()}")
+    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: is on {x.device}, not on the current device")
+    return x.data_ptr()
+
+
+_I32, _F4, _U8 = (torch.int32,), (torch.float32,), (torch.uint8, torch.bool)
+
+
+def _sizes(desc):
+    """units, heads, blocks per unit, dtypes of q, K and V"""
+    return desc.B * desc.Hkv, desc.B * desc.Hq, (desc.Lcap + BLOCK - 1) // BLOCK, (_FLOATS.get(desc.kv_dtype),)
+
+
+def corm_blocks_workspace_bytes(desc: corm_desc, check=True) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().corm_blocks_workspace_bytes(ctypes.byref(desc), ctypes.byref(n))
+    if check:
+        _check(rc, "corm_blocks_workspace_bytes")
+        return n.value
+    return rc
+
+
+def corm_q8_append(desc, code, k_new, v_new, n, n_new, K_codes, V_codes, k_scale, v_scale, K_tail, V_tail, lens, lens_out,
+                   bounds=None, status=None, stream=None, check=True) -> int:
+    """code: "i8" or "e4m3"; n_new: rows per sequence, None = n for all."""
+    code = _code(code)
+    units, _, nblk, kv = _sizes(desc)
+    ct, d = _CODES.get(code, ()), desc.d
+    rc = lib().corm_q8_append(ctypes.byref(desc), code, _dev(k_new, units * n * d, kv, "k_new"), _dev(v_new, units * n * d, kv, "v_new"),
+                              n, _dev(n_new, desc.B, _I32, "n_new"), _dev(K_codes, units * nblk * BLOCK * d, ct, "K_codes"),
+                              _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes"), _dev(k_scale, units * nblk, _F4, "k_scale"),
+                              _dev(v_scale, units * nblk, _F4, "v_scale"), _dev(K_tail, units * BLOCK * d, kv, "K_tail"),
+                              _dev(V_tail, units * BLOCK * d, kv, "V_tail"), _dev(lens, units, _I32, "lens"),
+                              _dev(lens_out, units, _I32, "lens_out"), _dev(bounds, units * nblk * 2 * d, kv, "bounds"),
+                              _dev(status, 1, _I32, "status"), _stream(stream))
+    return _check(rc, "corm_q8_append") if check else rc
+
+
+def corm_q8_attend(desc, code, q, K_codes, V_codes, k_scale, v_scale, K_tail, V_tail, lens, out, workspace, workspace_bytes=None,
+                   blocks=None, nsel=0, status=None, stream=None, check=True) -> int:
+    code = _code(code)
+    units, heads, nblk, kv = _sizes(desc)
+    ct, d = _CODES.get(code, ()), desc.d
+    rc = lib().corm_q8_attend(ctypes.byref(desc), code, _dev(q, heads * d, kv, "q"), _dev(K_codes, units * nblk * BLOCK * d, ct, "K_codes"),
+                              _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes"), _dev(k_scale, units * nblk, _F4, "k_scale"),
+                              _dev(v_scale, units * nblk, _F4, "v_scale"), _dev(K_tail, units * BLOCK * d, kv, "K_tail"),
+                              _dev(V_tail, units * BLOCK * d, kv, "V_tail"), _dev(lens, units, _I32, "lens"),
+                              _dev(blocks, units * nsel, _I32, "blocks"), nsel, _dev(out, heads * d, _F4, "out"), _ptr(workspace),
+                              _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status"), _stream(stream))
+    return _check(rc, "corm_q8_attend") if check else rc
+
+
+def corm_block_bounds(desc, K, lens, bounds, newest=0, stream=None, check=True) -> int:
+    """newest: renew the blocks that hold one of the newest `newest` slots; 0 = every block."""
+    units, _, nblk, kv = _sizes(desc)
+    rc = lib().corm_block_bounds(ctypes.byref(desc), _dev(K, units * desc.Lcap * desc.d, kv, "K"), _dev(lens, units, _I32, "lens"), newest,
+                                 _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds"), _stream(stream))
+    return _check(rc, "corm_block_bounds") if check else rc
+
+
+def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace=None, workspace_bytes=None, stream=None, check=True) -> int:
+    units, heads, nblk, kv = _sizes(desc)
+    rc = lib().corm_block_select(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q"), _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds"),
+                                 _dev(lens, units, _I32, "lens"), nsel, nlast, _dev(blocks, units * nsel, _I32, "blocks"), _ptr(workspace),
+                                 _nbytes(workspace, workspace_bytes), _stream(stream))
+    return _check(rc, "corm_block_select") if check else rc
+
+
+def corm_block_attend(desc, q, K, V, lens, blocks, nsel, out, workspace, workspace_bytes=None, status=None, stream=None,
+                      check=True) -> int:
+    units, heads, _, kv = _sizes(desc)
+    rows = units * desc.Lcap * desc.d
+    rc = lib().corm_block_attend(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q"), _dev(K, rows, kv, "K"), _dev(V, rows, kv, "V"),
+                                 _dev(lens, units, _I32, "lens"), _dev(blocks, units * nsel, _I32, "blocks"), nsel,
+                                 _dev(out, heads * desc.d, _F4, "out"), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                 _dev(status, 1, _I32, "status"), _stream(stream))
+    return _check(rc, "corm_block_attend") if check else rc
+
+
+def corm_decode_attend_weigh(desc, q, K, V, lens, weight_in, weight, out, workspace, workspace_bytes=None, status=None, stream=None,
+                             check=True, opts=None) -> int:
+    units, heads, _, kv = _sizes(desc)
+    rows = units * desc.Lcap * desc.d
+    rc = lib().corm_decode_attend_weigh(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q"), _dev(K, rows, kv, "K"), _dev(V, rows, kv, "V"),
+                                        _dev(lens, units, _I32, "lens"), _dev(weight_in, units * desc.Lcap, _F4, "weight_in"),
+                                        _dev(weight, units * desc.Lcap, _F4, "weight"), _dev(out, heads * desc.d, _F4, "out"),
+                                        _ptr(workspace), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status"),
+                                        _opts(opts), _stream(stream))
+    return _check(rc, "corm_decode_attend_weigh") if check else rc
+
+
+def corm_evict_mask_weight(desc, weight, lens, budget, keep, workspace, workspace_bytes=None, stream=None, check=True) -> int:
+    units = desc.B * desc.Hkv
+    rc = lib().corm_evict_mask_weight(ctypes.byref(desc), _dev(weight, units * desc.Lcap, _F4, "weight"), _dev(lens, units, _I32, "lens"),
+                                      budget, _dev(keep, units * desc.Lcap, _U8, "keep"), _ptr(workspace),
+                                      _nbytes(workspace, workspace_bytes), _stream(stream))
+    return _check(rc, "corm_evict_mask_weight") if check else rc
+
+
 # ---- device-memory plumbing for one layer (allocation only; no arithmetic of the method)
 
 class LayerState:
@@ -376,3 +506,95 @@ class LayerState:
         corm_prefill_seed(self.desc, q_tail, q_tail.shape[2], self.K, self.V, self.lens, self.pos, self.last_hit, t,
                           t_first, self.ring, self.keep, self.kept_idx,
                           self.workspace if workspace is None else workspace, status=self.status, stream=stream)
+
+    # The two steps below keep what they need in arrays of their own, allocated at first use; neither touches the ring.
+
+    def _blocks_workspace(self):
+        need = corm_blocks_workspace_bytes(self.desc)
+        if getattr(self, "blocks_workspace", None) is None:
+            self.blocks_workspace = torch.empty(need, dtype=torch.uint8, device=self.K.device)
+        return self.blocks_workspace
+
+    def renew_bounds(self, newest=0, stream=None) -> None:
+        """Bounds of the blocks' keys (all of them, or those of the newest slots): after a prompt, and after rows have moved."""
+        if getattr(self, "bounds", None) is None:
+            self.bounds = torch.zeros(self.B, self.Hkv, (self.Lcap + BLOCK - 1) // BLOCK, 2, self.d, dtype=self.dtype, device=self.K.device)
+        corm_block_bounds(self.desc, self.K, self.lens, self.bounds, newest, stream=stream)
+
+    def step_blocks(self, q, k_new, v_new, t, nsel, nlast=1, stream=None) -> None:
+        """One decode step that attends to nsel blocks of 64 slots (the nlast newest and those with the highest score bounds): append,
+        the newest block's bounds, choice, attention.  Nothing is recorded or evicted.  renew_bounds() first, after the prompt."""
+        if getattr(self, "bounds", None) is None:
+            raise RuntimeError("renew_bounds() first")
+        if getattr(self, "blocks", None) is None or self.blocks.shape[2] != nsel:
+            self.blocks = torch.empty(self.B, self.Hkv, nsel, dtype=torch.int32, device=self.K.device)
+        ws = self._blocks_workspace()
+        corm_append(self.desc, self.K, self.V, self.lens, self.pos, self.last_hit, k_new, v_new, t, self.status, stream=stream)
+        self.renew_bounds(1, stream=stream)
+        corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, ws, stream=stream)
+        corm_block_attend(self.desc, q, self.K, self.V, self.lens, self.blocks, nsel, self.out, ws, status=self.status, stream=stream)
+
+    def step_weigh(self, q, k_new, v_new, t, budget=None, stream=None) -> None:
+        """One decode step of eviction by accumulated attention weight: append, attend and account, and with a budget cut every
+        longer unit to it (the r newest slots and the heaviest others).  weight [B,Hkv,Lcap] holds the accounts."""
+        if getattr(self, "weight", None) is None:
+            self.weight = torch.zeros(self.B, self.Hkv, self.Lcap, dtype=torch.float32, device=self.K.device)
+        account = self.weight   # 4-byte entries: append and the gather carry them in the place of last_hit
+        corm_append(self.desc, self.K, self.V, self.lens, self.pos, account, k_new, v_new, t, self.status, stream=stream)
+        corm_decode_attend_weigh(self.desc, q, self.K, self.V, self.lens, account, account, self.out, self.workspace,
+                                 status=self.status, stream=stream)
+        if budget is None:
+            return
+        if getattr(self, "keep", None) is None:
+            self.keep = torch.zeros(self.B, self.Hkv, self.Lcap, dtype=torch.uint8, device=self.K.device)
+        corm_evict_mask_weight(self.desc, account, self.lens, budget, self.keep, self._blocks_workspace(), stream=stream)
+        corm_compact(self.desc, self.K, self.V, self.pos, account, self.lens, self.keep, self.kept_idx, self.workspace, stream=stream)
+
+
+class Q8State:
+    """The device arrays of one layer's 8-bit cache, in the layouts corm.h documents.  want_bounds: keep up the blocks' bounds, for
+    steps that attend to chosen blocks."""
+
+    def __init__(self, B, Hq, Hkv, d, Lcap, dtype, code="i8", device="cuda", want_bounds=False, workspace: Optional[torch.Tensor] = None):
+        tdt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        self.desc = make_desc(B, Hq, Hkv, d, Lcap, Lcap, 1, 1, dtype)
+        self.B, self.Hq, self.Hkv, self.d, self.Lcap, self.dtype, self.code = B, Hq, Hkv, d, Lcap, tdt, code
+        n = (Lcap + BLOCK - 1) // BLOCK
+        cdt = {"i8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
+        self.K_codes = torch.zeros(B, Hkv, n, d // BLOCK, BLOCK, BLOCK, dtype=torch.int8, device=device).view(cdt)
+        self.V_codes = torch.zeros(B, Hkv, n, d, BLOCK, dtype=torch.int8, device=device).view(cdt)
+        self.k_scale = torch.zeros(B, Hkv, n, dtype=torch.float32, device=device)
+        self.v_scale = torch.zeros(B, Hkv, n, dtype=torch.float32, device=device)
+        self.K_tail = torch.zeros(B, Hkv, BLOCK, d, dtype=tdt, device=device)
+        self.V_tail = torch.zeros(B, Hkv, BLOCK, d, dtype=tdt, device=device)
+        self.lens = torch.zeros(B, Hkv, dtype=torch.int32, device=device)
+        self.out = torch.zeros(B, Hq, d, dtype=torch.float32, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        self.bounds = torch.zeros(B, Hkv, n, 2, d, dtype=tdt, device=device) if want_bounds else None
+        self.blocks = None
+        if workspace is None:
+            workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
+        self.workspace = workspace
+
+    def append(self, k, v, n_new=None, stream=None) -> None:
+        """k, v [B,Hkv,n,d] (or [B,Hkv,d]: one row); n_new [B]: the rows of a sequence that count."""
+        n = 1 if k.dim() == 3 else k.shape[2]
+        corm_q8_append(self.desc, self.code, k, v, n, n_new, self.K_codes, self.V_codes, self.k_scale, self.v_scale, self.K_tail,
+                       self.V_tail, self.lens, self.lens, self.bounds, self.status, stream=stream)
+
+    def attend(self, q, nsel=0, nlast=1, stream=None) -> None:
+        """q [B,Hq,d] -> out.  nsel > 0: over the nlast newest blocks and those with the highest score bounds, nsel in all."""
+        if nsel:
+            if self.bounds is None:
+                raise RuntimeError("made without want_bounds")
+            if self.blocks is None or self.blocks.shape[2] != nsel:
+                self.blocks = torch.empty(self.B, self.Hkv, nsel, dtype=torch.int32, device=self.lens.device)
+            corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, self.workspace, stream=stream)
+        corm_q8_attend(self.desc, self.code, q, self.K_codes, self.V_codes, self.k_scale, self.v_scale, self.K_tail, self.V_tail,
+                       self.lens, self.out, self.workspace, blocks=self.blocks if nsel else None, nsel=nsel, status=self.status,
+                       stream=stream)
+
+    def step(self, q, k_new, v_new, nsel=0, nlast=1, stream=None) -> None:
+        """One decode step: the new row goes in, the query attends to all keys (or the chosen blocks), itself among them."""
+        self.append(k_new, v_new, stream=stream)
+        self.attend(q, nsel, nlast, stream=stream)

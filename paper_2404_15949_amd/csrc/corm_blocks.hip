@@ -1,0 +1,253 @@
+// HIP kernels (gfx950 / CDNA4, wave64) and C ABI of what bounds a decode step's reads beside CORM's own rule: a cache held in 8
+// bits, attention over chosen blocks of it or of the plain cache, and the eviction decision by accumulated attention weight.
+// One translation unit:
+//   q8.hpp             rows quantised into blocks of 64, and attention over them (q.K^T and p.V on the matrix cores)
+//   blocks.hpp         bounds of the blocks' keys, the choice, attention over the chosen ones
+//   evict_weight.hpp   the decision by weight (the weights themselves are summed behind corm_kernels.hip's attend launch)
+// Kernel boundaries are the only synchronization between workgroups, and nothing is kept from one call for the next.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <math.h>
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "corm.h"
+
+#include "common.hpp"
+#include "attend.hpp"
+#include "q8.hpp"
+#include "blocks.hpp"
+#include "evict_weight.hpp"
+#include "checks.hpp"
+
+namespace {
+
+int blocks_of(const corm_desc* d) { return (d->Lcap + QBLK - 1) / QBLK; }
+
+// Partials a head can have: parts of at least four blocks, or of a list of up to 512 (the tail's is the last).
+int max_parts(const corm_desc* d) { return std::max((blocks_of(d) + 3) / 4, 128) + 1; }
+int max_listed(const corm_desc* d) { return std::max(blocks_of(d), 512); }
+
+// Each of the calls below has the whole workspace to itself: partials, or scores.
+size_t blocks_workspace(const corm_desc* d) {
+  const size_t partials = (size_t)d->B * d->Hq * max_parts(d) * (d->d + 2) * sizeof(float);
+  const size_t scores = (size_t)d->B * d->Hkv * blocks_of(d) * sizeof(float);
+  return align_up(std::max(partials, scores), 256);
+}
+
+int check_blocks_workspace(const corm_desc* d, const void* workspace, size_t bytes) {
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CORM_EINVAL;
+  return bytes < blocks_workspace(d) ? CORM_ECAPACITY : CORM_OK;
+}
+
+float scale_log2(const corm_desc* d) { return (d->sm_scale > 0.f ? d->sm_scale : 1.0f / sqrtf((float)d->d)) * LOG2E; }
+
+int merge_parts(const corm_desc* d, const float* partials, const int32_t* lens, float* out, int npart, int part_slots, int all_parts,
+                bool last_apart, hipStream_t s) {
+  const int G = d->Hq / d->Hkv;
+  const dim3 grid(d->B * d->Hq);
+  if (d->d == 64)
+    hipLaunchKernelGGL(corm_parts_merge_kernel<64>, grid, dim3(64), 0, s, partials, lens, out, G, npart, part_slots, d->Lcap, all_parts,
+                       (int)last_apart);
+  else
+    hipLaunchKernelGGL(corm_parts_merge_kernel<128>, grid, dim3(128), 0, s, partials, lens, out, G, npart, part_slots, d->Lcap,
+                       all_parts, (int)last_apart);
+  return launch_status();
+}
+
+// kernel<code, element type, d> by the call's types
+template <typename F>
+int by_types(const corm_desc* d, int32_t code, const F& f) {
+  auto inner = [&](auto c) {
+    if (d->kv_dtype == CORM_F32) return d->d == 64 ? f(c, F32(), std::integral_constant<int, 64>()) : f(c, F32(), std::integral_constant<int, 128>());
+    return d->d == 64 ? f(c, BF16(), std::integral_constant<int, 64>()) : f(c, BF16(), std::integral_constant<int, 128>());
+  };
+  return code == CORM_I8 ? inner(CodeI8()) : inner(CodeE4M3());
+}
+template <typename F>
+int by_group(const corm_desc* d, const F& f) {
+  switch (d->Hq / d->Hkv) {
+    case 1: return f(std::integral_constant<int, 1>());
+    case 2: return f(std::integral_constant<int, 2>());
+    case 4: return f(std::integral_constant<int, 4>());
+    case 8: return f(std::integral_constant<int, 8>());
+    default: return CORM_EUNSUPPORTED;
+  }
+}
+template <typename F>
+int by_row(const corm_desc* d, const F& f) {
+  if (d->kv_dtype == CORM_F32) return d->d == 64 ? f(F32(), std::integral_constant<int, 64>()) : f(F32(), std::integral_constant<int, 128>());
+  return d->d == 64 ? f(BF16(), std::integral_constant<int, 64>()) : f(BF16(), std::integral_constant<int, 128>());
+}
+
+int check_code(int32_t code) { return code == CORM_I8 || code == CORM_E4M3 ? CORM_OK : CORM_EUNSUPPORTED; }
+
+}  // namespace
+
+extern "C" {
+
+int corm_blocks_workspace_bytes(const corm_desc* desc, size_t* bytes) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!bytes) return CORM_EINVAL;
+  *bytes = blocks_workspace(desc);
+  return CORM_OK;
+}
+
+int corm_q8_append(const corm_desc* desc, int32_t code_dtype, const void* k_new, const void* v_new, int32_t n, const int32_t* n_new,
+                   void* K_codes, void* V_codes, float* k_scale, float* v_scale, void* K_tail, void* V_tail, const int32_t* lens,
+                   int32_t* lens_out, void* bounds, int32_t* status, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  rc = check_code(code_dtype);
+  if (rc) return rc;
+  if (!k_new || !v_new || !K_codes || !V_codes || !k_scale || !v_scale || !K_tail || !V_tail || !lens || !lens_out) return CORM_EINVAL;
+  if (misaligned16(k_new) || misaligned16(v_new) || misaligned16(K_codes) || misaligned16(V_codes) || misaligned16(K_tail) ||
+      misaligned16(V_tail) || misaligned16(bounds))
+    return CORM_EINVAL;
+  if (misaligned4(n_new) || misaligned4(k_scale) || misaligned4(v_scale) || misaligned4(lens) || misaligned4(lens_out) || misaligned4(status))
+    return CORM_EINVAL;
+  if (n < 1 || n > desc->Lcap) return CORM_EINVAL;
+  Q8AppendArgs a;
+  a.k_new = reinterpret_cast<const char*>(k_new); a.v_new = reinterpret_cast<const char*>(v_new); a.n_new = n_new;
+  a.Kc = reinterpret_cast<unsigned char*>(K_codes); a.Vc = reinterpret_cast<unsigned char*>(V_codes);
+  a.ks = k_scale; a.vs = v_scale;
+  a.Kt = reinterpret_cast<char*>(K_tail); a.Vt = reinterpret_cast<char*>(V_tail);
+  a.lens = lens; a.lens_out = lens_out; a.bounds = reinterpret_cast<char*>(bounds); a.status = status;
+  a.Hkv = desc->Hkv; a.Lcap = desc->Lcap; a.nblk = blocks_of(desc); a.n = n;
+  const int units = desc->B * desc->Hkv;
+  const dim3 grid((n + 2 * QBLK - 2) / QBLK, units);   // blocks that n rows behind up to 63 others can touch
+  hipStream_t s = (hipStream_t)stream;
+  rc = by_types(desc, code_dtype, [&](auto c, auto dt, auto dd) {
+    hipLaunchKernelGGL((corm_q8_append_kernel<decltype(c), decltype(dt), decltype(dd)::value>), grid, dim3(WG), 0, s, a);
+    return launch_status();
+  });
+  if (rc || grid.x == 1) return rc;
+  hipLaunchKernelGGL(corm_q8_lens_kernel, dim3((units + WG - 1) / WG), dim3(WG), 0, s, a, units);
+  return launch_status();
+}
+
+int corm_q8_attend(const corm_desc* desc, int32_t code_dtype, const void* q, const void* K_codes, const void* V_codes,
+                   const float* k_scale, const float* v_scale, const void* K_tail, const void* V_tail, const int32_t* lens,
+                   const int32_t* blocks, int32_t nsel, float* out, void* workspace, size_t workspace_bytes, int32_t* status,
+                   void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  rc = check_code(code_dtype);
+  if (rc) return rc;
+  if (!q || !K_codes || !V_codes || !k_scale || !v_scale || !K_tail || !V_tail || !lens || !out) return CORM_EINVAL;
+  if (misaligned16(q) || misaligned16(K_codes) || misaligned16(V_codes) || misaligned16(K_tail) || misaligned16(V_tail)) return CORM_EINVAL;
+  if (misaligned4(k_scale) || misaligned4(v_scale) || misaligned4(lens) || misaligned4(blocks) || misaligned4(out) || misaligned4(status))
+    return CORM_EINVAL;
+  if (blocks ? nsel < 1 || nsel > max_listed(desc) : nsel != 0) return CORM_EINVAL;
+  rc = check_blocks_workspace(desc, workspace, workspace_bytes);
+  if (rc) return rc;
+  Q8Args a;
+  a.q = q; a.Kc = reinterpret_cast<const unsigned char*>(K_codes); a.Vc = reinterpret_cast<const unsigned char*>(V_codes);
+  a.ks = k_scale; a.vs = v_scale; a.Kt = K_tail; a.Vt = V_tail; a.lens = lens; a.blocks = blocks;
+  a.out = out; a.partials = reinterpret_cast<float*>(workspace); a.status = status;
+  a.Hq = desc->Hq; a.Hkv = desc->Hkv; a.Lcap = desc->Lcap; a.nblk = blocks_of(desc); a.nsel = blocks ? nsel : 0;
+  a.scale_log2 = scale_log2(desc);
+  const long units = (long)desc->B * desc->Hkv;
+  const int listed = blocks ? nsel : a.nblk;
+  // parts: about four workgroups per compute unit, of whole rounds of blocks over the waves
+  const int want = (int)std::min<long>((4L * device_cus() + units - 1) / units, (listed + WAVES - 1) / WAVES);
+  a.part_blocks = std::min(256, ((listed + want - 1) / want + WAVES - 1) / WAVES * WAVES);
+  const int parts = (listed + a.part_blocks - 1) / a.part_blocks;
+  a.npart = parts + 1;
+  hipStream_t s = (hipStream_t)stream;
+  rc = by_types(desc, code_dtype, [&](auto c, auto dt, auto dd) {
+    hipLaunchKernelGGL((corm_q8_attend_kernel<decltype(c), decltype(dt), decltype(dd)::value>), dim3(parts + 1, (unsigned)units), dim3(WG), 0,
+                       s, a);
+    return launch_status();
+  });
+  if (rc) return rc;
+  return merge_parts(desc, a.partials, lens, out, a.npart, blocks ? 0 : a.part_blocks * QBLK, parts, true, s);
+}
+
+int corm_block_bounds(const corm_desc* desc, const void* K, const int32_t* lens, int32_t newest, void* bounds, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!K || !lens || !bounds || misaligned16(K) || misaligned16(bounds) || misaligned4(lens) || newest < 0) return CORM_EINVAL;
+  const int nblk = blocks_of(desc);
+  const int n = newest > 0 ? (int)std::min<long long>(nblk, ((long long)newest + 2 * QBLK - 2) / QBLK) : nblk;
+  return by_row(desc, [&](auto dt, auto dd) {
+    hipLaunchKernelGGL((corm_block_bounds_kernel<decltype(dt), decltype(dd)::value>), dim3(n, desc->B * desc->Hkv), dim3(WG), 0,
+                       (hipStream_t)stream, reinterpret_cast<const char*>(K), lens, reinterpret_cast<char*>(bounds), desc->Lcap, nblk,
+                       newest);
+    return launch_status();
+  });
+}
+
+int corm_block_select(const corm_desc* desc, const void* q, const void* bounds, const int32_t* lens, int32_t nsel, int32_t nlast,
+                      int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!q || !bounds || !lens || !blocks || misaligned16(q) || misaligned16(bounds) || misaligned4(lens) || misaligned4(blocks))
+    return CORM_EINVAL;
+  if (nsel < 1 || nsel > max_listed(desc) || nlast < 1 || nlast > nsel) return CORM_EINVAL;
+  rc = check_blocks_workspace(desc, workspace, workspace_bytes);
+  if (rc) return rc;
+  const int nblk = blocks_of(desc), units = desc->B * desc->Hkv;
+  float* scores = reinterpret_cast<float*>(workspace);
+  hipStream_t s = (hipStream_t)stream;
+  rc = by_row(desc, [&](auto dt, auto dd) {
+    return by_group(desc, [&](auto g) {
+      hipLaunchKernelGGL((corm_block_score_kernel<decltype(dt), decltype(dd)::value, decltype(g)::value>), dim3((nblk + 63) / 64, units),
+                         dim3(WG), 0, s, reinterpret_cast<const char*>(q), reinterpret_cast<const char*>(bounds), lens, scores,
+                         desc->Lcap, nblk);
+      return launch_status();
+    });
+  });
+  if (rc) return rc;
+  hipLaunchKernelGGL(corm_block_pick_kernel, dim3(units), dim3(PICK_WG), 0, s, scores, lens, blocks, desc->Lcap, nblk, nsel, nlast);
+  return launch_status();
+}
+
+int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const void* V, const int32_t* lens, const int32_t* blocks,
+                      int32_t nsel, float* out, void* workspace, size_t workspace_bytes, int32_t* status, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!q || !K || !V || !lens || !blocks || !out || misaligned16(q) || misaligned16(K) || misaligned16(V)) return CORM_EINVAL;
+  if (misaligned4(lens) || misaligned4(blocks) || misaligned4(out) || misaligned4(status)) return CORM_EINVAL;
+  if (nsel < 1 || nsel > max_listed(desc)) return CORM_EINVAL;
+  rc = check_blocks_workspace(desc, workspace, workspace_bytes);
+  if (rc) return rc;
+  BlockAttendArgs a;
+  a.q = reinterpret_cast<const char*>(q); a.K = reinterpret_cast<const char*>(K); a.V = reinterpret_cast<const char*>(V);
+  a.lens = lens; a.blocks = blocks; a.partials = reinterpret_cast<float*>(workspace); a.status = status;
+  a.Lcap = desc->Lcap; a.nsel = nsel; a.scale_log2 = scale_log2(desc);
+  const long units = (long)desc->B * desc->Hkv;
+  const int room = max_parts(desc);
+  a.part_blocks = 1;
+  while (a.part_blocks < LIST_PART &&
+         (units * ((nsel + a.part_blocks - 1) / a.part_blocks) > 4L * device_cus() || (nsel + a.part_blocks - 1) / a.part_blocks > room))
+    a.part_blocks *= 2;
+  const int parts = (nsel + a.part_blocks - 1) / a.part_blocks;
+  a.npart = parts;
+  hipStream_t s = (hipStream_t)stream;
+  rc = by_row(desc, [&](auto dt, auto dd) {
+    return by_group(desc, [&](auto g) {
+      hipLaunchKernelGGL((corm_block_attend_kernel<decltype(dt), decltype(dd)::value, decltype(g)::value>), dim3(parts, (unsigned)units),
+                         dim3(WG), 0, s, a);
+      return launch_status();
+    });
+  });
+  if (rc) return rc;
+  return merge_parts(desc, a.partials, lens, out, parts, 0, parts, false, s);
+}
+
+int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int32_t* lens, int32_t budget, uint8_t* keep, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!weight || !lens || !keep || misaligned4(weight) || misaligned4(lens) || budget < desc->r) return CORM_EINVAL;
+  rc = check_blocks_workspace(desc, workspace, workspace_bytes);
+  if (rc) return rc;
+  hipLaunchKernelGGL(corm_evict_weight_kernel, dim3(desc->B * desc->Hkv), dim3(EVW_WG), 0, (hipStream_t)stream, weight, lens, keep,
+                     desc->Lcap, desc->r, budget);
+  return launch_status();
+}
+
+}  // extern "C"

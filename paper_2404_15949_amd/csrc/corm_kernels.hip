@@ -37,9 +37,11 @@
 #include "unit.hpp"
 #include "small.hpp"
 #include "record.hpp"
+#include "weigh.hpp"
 #include "compact.hpp"
 #include "prefill.hpp"
 #include "standalone.hpp"
+#include "checks.hpp"
 #include "host.hpp"
 
 // ---- corm_decode_attend_static: the attend call for callers that cannot allocate
@@ -202,6 +204,28 @@ int corm_decode_attend_static(const corm_desc* desc, const void* q, const void* 
   p.do_append = 0; p.do_evict = 0;
   bind_params(desc, wl, ws, p);
   return launch_attend_record(desc, p, ctx, (hipStream_t)stream);
+}
+
+int corm_decode_attend_weigh(const corm_desc* desc, const void* q, const void* K, const void* V, const int32_t* lens,
+                             const float* weight_in, float* weight, float* out, void* workspace, size_t workspace_bytes,
+                             int32_t* status, const corm_launch_opts* opts, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  rc = check_step_pointers(q, K, V, K, V, lens, lens, lens, lens, lens, nullptr, out, nullptr, status);
+  if (rc) return rc;
+  if (!weight_in || !weight || misaligned4(weight_in) || misaligned4(weight)) return CORM_EINVAL;
+  WorkspaceLayout wl;
+  rc = check_workspace(desc, workspace, workspace_bytes, &wl);
+  if (rc) return rc;
+  LaunchCtx ctx;
+  rc = make_ctx(opts, &ctx);
+  if (rc) return rc;
+  Params p = {};
+  p.q = q; p.k_new = K; p.v_new = V;  // (as in corm_decode_attend; pos, last_hit and t are not read without an append and a ring)
+  p.K = const_cast<void*>(K); p.V = const_cast<void*>(V);
+  p.lens = const_cast<int32_t*>(lens); p.t = lens; p.t_first = lens; p.out = out; p.status = status;
+  bind_params(desc, wl, workspace, p);
+  return launch_attend_weigh(desc, p, ctx, weight_in, weight, (hipStream_t)stream);
 }
 
 int corm_evict_mask(const corm_desc* desc, const void* score_ring, const int32_t* lens, const int32_t* pos,

@@ -14,10 +14,6 @@ struct WorkspaceLayout {
   int seed_kb, seed_nkb;   // prompt seeding: keys per workgroup, key blocks per unit
 };
 
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
-
-int row_bytes(const corm_desc* d) { return d->d * (d->kv_dtype == CORM_F32 ? 4 : 2); }
-
 WorkspaceLayout workspace_layout(const corm_desc& d) {
   WorkspaceLayout w;
   w.nsplit = (d.Lcap + CHUNK - 1) / CHUNK;
@@ -41,28 +37,6 @@ WorkspaceLayout workspace_layout(const corm_desc& d) {
   return w;
 }
 
-int validate_desc(const corm_desc* d) {
-  if (!d) return CORM_EINVAL;
-  if (d->B < 1 || d->Hq < 1 || d->Hkv < 1 || d->Lcap < 1 || d->Tcap < 1 || d->w < 1 || d->r < 1) return CORM_EINVAL;
-  if (d->Hq % d->Hkv != 0) return CORM_EINVAL;
-  if (!(d->thr_scale >= 0.f) || !std::isfinite(d->thr_scale)) return CORM_EINVAL;
-  if (!(d->sm_scale >= 0.f) || !std::isfinite(d->sm_scale)) return CORM_EINVAL;
-  if ((long long)d->B * d->Hkv > 2147483647LL / 2 || (long long)d->B * d->Hq > 2147483647LL / 2) return CORM_EINVAL;
-  if (d->B * d->Hkv > 65535) return CORM_EUNSUPPORTED;  // grid.y limit
-  if ((long long)d->Lcap * 512 >= (1LL << 31)) return CORM_EUNSUPPORTED;  // byte offsets inside a unit are 32-bit
-  if (d->kv_dtype != CORM_F32 && d->kv_dtype != CORM_BF16) return CORM_EUNSUPPORTED;
-  if (d->score_dtype != CORM_F32 && d->score_dtype != CORM_BF16 && d->score_dtype != CORM_BIT) return CORM_EUNSUPPORTED;
-  if (d->d != 64 && d->d != 128) return CORM_EUNSUPPORTED;
-  const int G = d->Hq / d->Hkv;
-  if (G != 1 && G != 2 && G != 4 && G != 8) return CORM_EUNSUPPORTED;
-  return CORM_OK;
-}
-
-bool misaligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-bool misaligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) != 0; }
-
-int launch_status() { return hipGetLastError() == hipSuccess ? CORM_OK : CORM_EHIP; }
-
 // Per-call launch context: what corm_launch_opts asks for, plus the compute-unit count of the current
 // device.  Nothing here outlives the call.
 struct LaunchCtx {
@@ -72,23 +46,6 @@ struct LaunchCtx {
   hipEvent_t ev0 = nullptr, ev1 = nullptr;    // recorded around the launch that streams K and V
   int cus = 256;
 };
-
-// Compute units of the current device, asked once per device (thread safe); 256 where no device answers.
-constexpr int MAX_DEVICES = 64;
-std::mutex g_device_mutex;
-int g_device_cus[MAX_DEVICES] = {};
-
-int device_cus() {
-  int dev = -1;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= MAX_DEVICES) return 256;
-  std::lock_guard<std::mutex> lock(g_device_mutex);
-  if (g_device_cus[dev] == 0) {
-    int n = 0;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0) n = 256;
-    g_device_cus[dev] = n;
-  }
-  return g_device_cus[dev];
-}
 
 int make_ctx(const corm_launch_opts* o, LaunchCtx* c) {
   *c = LaunchCtx();
@@ -318,6 +275,32 @@ int launch_attend_record(const corm_desc* d, const Params& p0, const LaunchCtx& 
   const int rc = launch_attend(d, p, c, s);
   if (rc) return rc;
   return launch_record(d, p, c, s);
+}
+
+// The split attend launch, and behind it the weights and out.
+template <int NT>
+int launch_weigh(const corm_desc* d, const Params& p, const float* weight_in, float* weight, hipStream_t s) {
+  const int G = d->Hq / d->Hkv;
+  const int items = G * (d->d / 64);
+  const int n_out = (d->Lcap + p.part_keys - 1) / p.part_keys <= OUT_WAVE_PARTS ? (items + NT / 64 - 1) / (NT / 64) : items;
+  const dim3 grid(d->B * d->Hkv, p.nsplit + n_out);
+  switch (G) {
+    case 1: hipLaunchKernelGGL((corm_weigh_kernel<1, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 2: hipLaunchKernelGGL((corm_weigh_kernel<2, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 4: hipLaunchKernelGGL((corm_weigh_kernel<4, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 8: hipLaunchKernelGGL((corm_weigh_kernel<8, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
+    default: return CORM_EUNSUPPORTED;
+  }
+  return launch_status();
+}
+
+int launch_attend_weigh(const corm_desc* d, const Params& p0, const LaunchCtx& c, const float* weight_in, float* weight, hipStream_t s) {
+  Params p = p0;
+  p.part_keys = attend_part_keys(d, c);
+  p.head_groups = attend_head_groups(d, c, p.part_keys);
+  const int rc = launch_attend(d, p, c, s);
+  if (rc) return rc;
+  return launch_weigh<CHUNK>(d, p, weight_in, weight, s);
 }
 
 // A whole step in one launch (small.hpp)?  A unit is then one workgroup's alone, so only while its rows are few.  Whole steps in a
