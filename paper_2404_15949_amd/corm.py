@@ -326,18 +326,22 @@ def _code(x) -> int:
     return x if isinstance(x, int) else _code_ids[x]
 
 
-def _dev(x, n: int, dtypes, name: str) -> Optional[int]:
+def _device() -> int:
+    """The current device, asked once per call; no tensor is on -2, the answer before anything is on one."""
+    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+
+
+def _dev(x, n: int, dtypes, name: str, device: int) -> Optional[int]:
     """Pointer of an argument whose layout the call takes for granted.  A tensor has to be whole, of the right type, large enough and on the
     current device (the call goes to one of its streams); a raw pointer is taken as it is."""
+    if x is None:
+        return None
     if not isinstance(x, torch.Tensor):
-        return None if x is None else int(x)
-    if x.dtype not in dtypes:
-        raise ValueError(f"{name}: expected {dtypes}, got {x.dtype}")
-    if not x.is_contiguous() or x.numel() < n:
-        raise ValueError(f"{name}: expected {n} contiguous elements, got {tuple(x.shape)} with strides {x.stride()}")
-    if not x.is_cuda or x.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{name}: is on {x.device}, not on the current device")
-    return x.data_ptr()
+        return int(x)
+    if x.dtype in dtypes and x.numel() >= n and x.is_contiguous() and x.get_device() == device:
+        return x.data_ptr()
+    raise ValueError(f"{name}: expected {n} contiguous elements of {dtypes} on the current device, got {x.dtype} {tuple(x.shape)} with "
+                     f"strides {x.stride()} on {x.device}")
 
 
 _I32, _F4, _U8 = (torch.int32,), (torch.float32,), (torch.uint8, torch.bool)
@@ -362,14 +366,15 @@ def corm_q8_append(desc, code, k_new, v_new, n, n_new, K_codes, V_codes, k_scale
     """code: "i8" or "e4m3"; n_new: rows per sequence, None = n for all."""
     code = _code(code)
     units, _, nblk, kv = _sizes(desc)
+    at = _device()
     ct, d = _CODES.get(code, ()), desc.d
-    rc = lib().corm_q8_append(ctypes.byref(desc), code, _dev(k_new, units * n * d, kv, "k_new"), _dev(v_new, units * n * d, kv, "v_new"),
-                              n, _dev(n_new, desc.B, _I32, "n_new"), _dev(K_codes, units * nblk * BLOCK * d, ct, "K_codes"),
-                              _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes"), _dev(k_scale, units * nblk, _F4, "k_scale"),
-                              _dev(v_scale, units * nblk, _F4, "v_scale"), _dev(K_tail, units * BLOCK * d, kv, "K_tail"),
-                              _dev(V_tail, units * BLOCK * d, kv, "V_tail"), _dev(lens, units, _I32, "lens"),
-                              _dev(lens_out, units, _I32, "lens_out"), _dev(bounds, units * nblk * 2 * d, kv, "bounds"),
-                              _dev(status, 1, _I32, "status"), _stream(stream))
+    rc = lib().corm_q8_append(ctypes.byref(desc), code, _dev(k_new, units * n * d, kv, "k_new", at), _dev(v_new, units * n * d, kv, "v_new", at),
+                              n, _dev(n_new, desc.B, _I32, "n_new", at), _dev(K_codes, units * nblk * BLOCK * d, ct, "K_codes", at),
+                              _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes", at), _dev(k_scale, units * nblk, _F4, "k_scale", at),
+                              _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
+                              _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
+                              _dev(lens_out, units, _I32, "lens_out", at), _dev(bounds, units * nblk * 2 * d, kv, "bounds", at),
+                              _dev(status, 1, _I32, "status", at), _stream(stream))
     return _check(rc, "corm_q8_append") if check else rc
 
 
@@ -377,28 +382,31 @@ def corm_q8_attend(desc, code, q, K_codes, V_codes, k_scale, v_scale, K_tail, V_
                    blocks=None, nsel=0, status=None, stream=None, check=True) -> int:
     code = _code(code)
     units, heads, nblk, kv = _sizes(desc)
+    at = _device()
     ct, d = _CODES.get(code, ()), desc.d
-    rc = lib().corm_q8_attend(ctypes.byref(desc), code, _dev(q, heads * d, kv, "q"), _dev(K_codes, units * nblk * BLOCK * d, ct, "K_codes"),
-                              _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes"), _dev(k_scale, units * nblk, _F4, "k_scale"),
-                              _dev(v_scale, units * nblk, _F4, "v_scale"), _dev(K_tail, units * BLOCK * d, kv, "K_tail"),
-                              _dev(V_tail, units * BLOCK * d, kv, "V_tail"), _dev(lens, units, _I32, "lens"),
-                              _dev(blocks, units * nsel, _I32, "blocks"), nsel, _dev(out, heads * d, _F4, "out"), _ptr(workspace),
-                              _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status"), _stream(stream))
+    rc = lib().corm_q8_attend(ctypes.byref(desc), code, _dev(q, heads * d, kv, "q", at), _dev(K_codes, units * nblk * BLOCK * d, ct, "K_codes", at),
+                              _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes", at), _dev(k_scale, units * nblk, _F4, "k_scale", at),
+                              _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
+                              _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
+                              _dev(blocks, units * nsel, _I32, "blocks", at), nsel, _dev(out, heads * d, _F4, "out", at), _ptr(workspace),
+                              _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at), _stream(stream))
     return _check(rc, "corm_q8_attend") if check else rc
 
 
 def corm_block_bounds(desc, K, lens, bounds, newest=0, stream=None, check=True) -> int:
     """newest: renew the blocks that hold one of the newest `newest` slots; 0 = every block."""
     units, _, nblk, kv = _sizes(desc)
-    rc = lib().corm_block_bounds(ctypes.byref(desc), _dev(K, units * desc.Lcap * desc.d, kv, "K"), _dev(lens, units, _I32, "lens"), newest,
-                                 _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds"), _stream(stream))
+    at = _device()
+    rc = lib().corm_block_bounds(ctypes.byref(desc), _dev(K, units * desc.Lcap * desc.d, kv, "K", at), _dev(lens, units, _I32, "lens", at), newest,
+                                 _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at), _stream(stream))
     return _check(rc, "corm_block_bounds") if check else rc
 
 
 def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace=None, workspace_bytes=None, stream=None, check=True) -> int:
     units, heads, nblk, kv = _sizes(desc)
-    rc = lib().corm_block_select(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q"), _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds"),
-                                 _dev(lens, units, _I32, "lens"), nsel, nlast, _dev(blocks, units * nsel, _I32, "blocks"), _ptr(workspace),
+    at = _device()
+    rc = lib().corm_block_select(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at),
+                                 _dev(lens, units, _I32, "lens", at), nsel, nlast, _dev(blocks, units * nsel, _I32, "blocks", at), _ptr(workspace),
                                  _nbytes(workspace, workspace_bytes), _stream(stream))
     return _check(rc, "corm_block_select") if check else rc
 
@@ -406,30 +414,32 @@ def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace=None
 def corm_block_attend(desc, q, K, V, lens, blocks, nsel, out, workspace, workspace_bytes=None, status=None, stream=None,
                       check=True) -> int:
     units, heads, _, kv = _sizes(desc)
+    at = _device()
     rows = units * desc.Lcap * desc.d
-    rc = lib().corm_block_attend(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q"), _dev(K, rows, kv, "K"), _dev(V, rows, kv, "V"),
-                                 _dev(lens, units, _I32, "lens"), _dev(blocks, units * nsel, _I32, "blocks"), nsel,
-                                 _dev(out, heads * desc.d, _F4, "out"), _ptr(workspace), _nbytes(workspace, workspace_bytes),
-                                 _dev(status, 1, _I32, "status"), _stream(stream))
+    rc = lib().corm_block_attend(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
+                                 _dev(lens, units, _I32, "lens", at), _dev(blocks, units * nsel, _I32, "blocks", at), nsel,
+                                 _dev(out, heads * desc.d, _F4, "out", at), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                 _dev(status, 1, _I32, "status", at), _stream(stream))
     return _check(rc, "corm_block_attend") if check else rc
 
 
 def corm_decode_attend_weigh(desc, q, K, V, lens, weight_in, weight, out, workspace, workspace_bytes=None, status=None, stream=None,
                              check=True, opts=None) -> int:
     units, heads, _, kv = _sizes(desc)
+    at = _device()
     rows = units * desc.Lcap * desc.d
-    rc = lib().corm_decode_attend_weigh(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q"), _dev(K, rows, kv, "K"), _dev(V, rows, kv, "V"),
-                                        _dev(lens, units, _I32, "lens"), _dev(weight_in, units * desc.Lcap, _F4, "weight_in"),
-                                        _dev(weight, units * desc.Lcap, _F4, "weight"), _dev(out, heads * desc.d, _F4, "out"),
-                                        _ptr(workspace), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status"),
+    rc = lib().corm_decode_attend_weigh(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
+                                        _dev(lens, units, _I32, "lens", at), _dev(weight_in, units * desc.Lcap, _F4, "weight_in", at),
+                                        _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(out, heads * desc.d, _F4, "out", at),
+                                        _ptr(workspace), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at),
                                         _opts(opts), _stream(stream))
     return _check(rc, "corm_decode_attend_weigh") if check else rc
 
 
 def corm_evict_mask_weight(desc, weight, lens, budget, keep, workspace, workspace_bytes=None, stream=None, check=True) -> int:
-    units = desc.B * desc.Hkv
-    rc = lib().corm_evict_mask_weight(ctypes.byref(desc), _dev(weight, units * desc.Lcap, _F4, "weight"), _dev(lens, units, _I32, "lens"),
-                                      budget, _dev(keep, units * desc.Lcap, _U8, "keep"), _ptr(workspace),
+    units, at = desc.B * desc.Hkv, _device()
+    rc = lib().corm_evict_mask_weight(ctypes.byref(desc), _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(lens, units, _I32, "lens", at),
+                                      budget, _dev(keep, units * desc.Lcap, _U8, "keep", at), _ptr(workspace),
                                       _nbytes(workspace, workspace_bytes), _stream(stream))
     return _check(rc, "corm_evict_mask_weight") if check else rc
 

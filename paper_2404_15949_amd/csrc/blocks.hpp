@@ -122,64 +122,14 @@ __global__ __launch_bounds__(WG) void corm_block_score_kernel(const char* q, con
   }
 }
 
-// An fp32 number as an unsigned one of the same order (-0 as 0, what is not a number below all others).
-__device__ __forceinline__ uint32_t order_key(float x) {
-  if (x != x) return 0u;
-  const uint32_t u = __float_as_uint(x + 0.f);
-  return (u >> 31) ? ~u : u | 0x80000000u;
-}
-
-// The k-th largest of n keys (1 <= k <= n), by the whole workgroup: digits of 8 bits from the top, counted in LDS.  key(i) is asked
-// for anew in each of the four rounds.  -> (key, how many of the keys equal to it belong to the k largest)
-template <int NT, typename Key>
-__device__ __forceinline__ uint2 kth_largest(int n, int k, const Key& key, uint32_t* sh_hist, uint32_t* sh_pick) {
-  uint32_t prefix = 0u, need = (uint32_t)k;
-  for (int shift = 24; shift >= 0; shift -= 8) {
-    for (int i = threadIdx.x; i < 256; i += NT) sh_hist[i] = 0u;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += NT) {
-      const uint32_t x = key(i);
-      if (shift == 24 || (x >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&sh_hist[(x >> shift) & 255u], 1u);
-    }
-    __syncthreads();
-    if (threadIdx.x < 64) {   // lane l: digits 255-4l .. 252-4l
-      const int l = threadIdx.x;
-      uint32_t c[4], sum = 0u;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        c[j] = sh_hist[255 - 4 * l - j];
-        sum += c[j];
-      }
-      uint32_t before = sum;
-#pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const uint32_t x = __shfl_up(before, o);
-        if (l >= o) before += x;
-      }
-      before -= sum;   // keys with a larger digit than this lane's
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (before < need && before + c[j] >= need) {
-          sh_pick[0] = (uint32_t)(255 - 4 * l - j);
-          sh_pick[1] = need - before;
-        }
-        before += c[j];
-      }
-    }
-    __syncthreads();
-    prefix |= sh_pick[0] << shift;
-    need = sh_pick[1];
-    __syncthreads();
-  }
-  return make_uint2(prefix, need);
-}
-
 // Grid (units): the nlast newest blocks and the best of the others, ascending, -1 behind them.
-constexpr int PICK_WG = 256;
+// The keys are read once where they fit in LDS (scores of 262144 slots), else in every round from memory.
+constexpr int PICK_WG = 256, PICK_BITS = 8, PICK_KEYS = 4096;
 __global__ __launch_bounds__(PICK_WG) void corm_block_pick_kernel(const float* scores, const int32_t* lens, int32_t* blocks, int Lcap,
                                                                   int nblk, int nsel, int nlast) {
-  __shared__ uint32_t sh_hist[256], sh_pick[2];
-  __shared__ int sh_cnt[PICK_WG / 64][2];
+  __shared__ CutLds<PICK_WG, PICK_BITS> sh;
+  __shared__ uint32_t sh_key[PICK_KEYS];
+  __shared__ int sh_cnt[PICK_WG / 64];
   const int unit = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK;
   const float* sc = scores + (size_t)unit * nblk;
@@ -193,33 +143,31 @@ __global__ __launch_bounds__(PICK_WG) void corm_block_pick_kernel(const float* s
   }
   for (int i = tid; i < used - open; i += PICK_WG) to[k + i] = open + i;
   if (k == 0) return;
-  const uint2 cut = kth_largest<PICK_WG>(open, k, [&](int i) { return order_key(sc[i]); }, sh_hist, sh_pick);
-  int above = 0, equal = 0;   // in front of this tile
+  const bool held = open <= PICK_KEYS;
+  if (held)
+    for (int i = tid; i < open; i += PICK_WG) sh_key[i] = order_key(sc[i]);   // (a thread reads back its own)
+  auto item = [&](int i, uint32_t& x, uint32_t& slot) {
+    x = held ? sh_key[i] : order_key(sc[i]);
+    slot = (uint32_t)i;
+    return true;
+  };
+  const Cut cut = find_cut<PICK_WG, PICK_BITS, 32>(open, (uint32_t)k, item, sh);
+  int before = 0;   // chosen in front of this tile
   for (int i0 = 0; i0 < open; i0 += PICK_WG) {
     const int i = i0 + tid;
-    const uint32_t x = i < open ? order_key(sc[i]) : 0u;
-    const bool gt = i < open && x > cut.x, eq = i < open && x == cut.x;
-    const unsigned long long mg = __ballot(gt), me = __ballot(eq);
+    uint32_t x = 0u, slot;
+    if (i < open) item(i, x, slot);
+    const bool in = i < open && (x > cut.key || (x == cut.key && (uint32_t)i <= cut.last));
+    const unsigned long long mask = __ballot(in);
     __syncthreads();
-    if (lane == 0) {
-      sh_cnt[wv][0] = __popcll(mg);
-      sh_cnt[wv][1] = __popcll(me);
-    }
+    if (lane == 0) sh_cnt[wv] = __popcll(mask);
     __syncthreads();
-    int ng = above, ne = equal;
+    int at = before + __popcll(mask & ((1ull << lane) - 1ull));
     for (int w = 0; w < PICK_WG / 64; ++w) {
-      if (w < wv) {
-        ng += sh_cnt[w][0];
-        ne += sh_cnt[w][1];
-      }
-      above += sh_cnt[w][0];
-      equal += sh_cnt[w][1];
+      at += w < wv ? sh_cnt[w] : 0;
+      before += sh_cnt[w];
     }
-    const unsigned long long below = (1ull << lane) - 1ull;
-    ng += __popcll(mg & below);
-    ne += __popcll(me & below);
-    // equal ones: the first cut.y of them
-    if (gt || (eq && ne < (int)cut.y)) to[ng + min(ne, (int)cut.y)] = i;
+    if (in) to[at] = i;
   }
 }
 
@@ -239,6 +187,51 @@ struct BlockAttendArgs {
 
 constexpr int LIST_PART = 8;   // listed blocks per workgroup, at most
 
+// The workgroup's part of the list: sh_first = first slot of each block, L where there is none.  Returns the unit's length L.  Ends with a barrier.
+__device__ __forceinline__ int listed_blocks(const BlockAttendArgs& a, int unit, int* sh_first) {
+  const int tid = threadIdx.x, at = blockIdx.x * a.part_blocks + tid;
+  int L = a.lens[unit], flags = 0;
+  if (L < 0 || L > a.Lcap) {
+    flags = CORM_DEV_BAD_LENS;
+    L = L < 0 ? 0 : a.Lcap;
+  }
+  if (tid < LIST_PART) {
+    const int id = tid < a.part_blocks && at < a.nsel ? a.blocks[(size_t)unit * a.nsel + at] : -1;
+    const bool ok = id >= 0 && id < (L + QBLK - 1) / QBLK;
+    if (!ok && id != -1) flags |= CORM_DEV_BAD_BLOCK;
+    sh_first[tid] = ok ? id * QBLK : L;
+    if (flags && a.status) atomicOr(a.status, flags);
+  }
+  __syncthreads();
+  return L;
+}
+
+// The waves' sums, folded into the workgroup's partial.
+template <int D, int G>
+__device__ __forceinline__ void block_partial(const BlockAttendArgs& a, int unit, const float (&sh_m)[G][WAVES], const float (&sh_z)[G][WAVES],
+                                              const float (&sh_acc)[G][WAVES][D]) {
+  for (int idx = threadIdx.x; idx < G * D; idx += WG) {
+    const int g = idx / D, c = idx - g * D;
+    float mx = neg_inf();
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, sh_m[g][i]);
+    const float ms = mx == neg_inf() ? 0.f : mx;
+    float zt = 0.f, at = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) {
+      const float f = fast_exp2(sh_m[g][i] - ms);
+      zt = fmaf(sh_z[g][i], f, zt);
+      at = fmaf(sh_acc[g][i][c], f, at);
+    }
+    float* part = partial_of(a.partials, unit * G + g, a.npart, blockIdx.x, D);
+    part[2 + c] = at;
+    if (c == 0) {
+      part[0] = mx;
+      part[1] = zt;
+    }
+  }
+}
+
 // Grid (parts of the list, units).  The rows of the listed blocks, one behind the other, are streamed as corm_attend_kernel streams a chunk;
 // a lane looks the block of its row up in LDS, and rows that are not in use get an offset past the descriptor's end.
 template <typename DT, int D, int G>
@@ -249,24 +242,11 @@ __global__ __launch_bounds__(WG) void corm_block_attend_kernel(const BlockAttend
   __shared__ float sh_m[G][WAVES], sh_z[G][WAVES];
   __shared__ float sh_acc[G][WAVES][D];
   __shared__ float sh_logit[G][ROWS];
-  __shared__ int sh_first[LIST_PART + 1];   // first slot of a listed block, or Lcap
+  __shared__ int sh_first[LIST_PART];
   const int unit = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int sub = lane / LPR, cl = lane % LPR;
-  int L = a.lens[unit];
-  int flags = 0;
-  if (L < 0 || L > a.Lcap) {
-    flags = CORM_DEV_BAD_LENS;
-    L = L < 0 ? 0 : a.Lcap;
-  }
-  const int first = blockIdx.x * a.part_blocks, count = min(a.part_blocks, a.nsel - first);
-  if (tid < LIST_PART) {
-    const int id = tid < count ? a.blocks[(size_t)unit * a.nsel + first + tid] : -1;
-    const bool ok = id >= 0 && id < (L + QBLK - 1) / QBLK;
-    if (!ok && id != -1) flags |= CORM_DEV_BAD_BLOCK;
-    sh_first[tid] = ok ? id * QBLK : L;
-  }
-  if (flags && a.status) atomicOr(a.status, flags);
-  __syncthreads();
+  const int L = listed_blocks(a, unit, sh_first);
+  const int count = min(a.part_blocks, a.nsel - (int)blockIdx.x * a.part_blocks);
 
   uint4 qreg[G];
 #pragma unroll
@@ -327,26 +307,78 @@ __global__ __launch_bounds__(WG) void corm_block_attend_kernel(const BlockAttend
     }
   }
   __syncthreads();
-  for (int idx = tid; idx < G * D; idx += WG) {
-    const int g = idx / D, c = idx - g * D;
-    float mx = neg_inf();
+  block_partial<D, G>(a, unit, sh_m, sh_z, sh_acc);
+}
+
+// Grouped bf16 queries of d 128: q.K^T on the matrix cores, as corm_attend_gqa_kernel does it (a wave takes 16 rows of each listed block).
+template <int G>
+__global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(G <= 4 ? 3 : 2)))
+void corm_block_attend_gqa_kernel(const BlockAttendArgs a) {
+  using A = AttendGqa<G>;
+  constexpr int D = A::D, ROWB = A::ROWB, EPL = A::EPL;
+  static_assert(A::STAGE_ROWS == QBLK, "a stage is a block");
+  __shared__ float sh_m[G][WAVES], sh_z[G][WAVES];
+  __shared__ float sh_acc[G][WAVES][D];
+  __shared__ __attribute__((aligned(16))) float sh_logit[G][A::TILE];   // (written by compute, not read)
+  __shared__ uint4 sh_kt[WAVES][A::TILE * 16];
+  __shared__ __attribute__((aligned(16))) float sh_p[WAVES][A::TILE * G];
+  __shared__ __attribute__((aligned(16))) float sh_alpha[WAVES][G];
+  __shared__ int sh_first[LIST_PART];
+  const int unit = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int n = lane & 15, lg = lane >> 4;
+  uint4 qb[4];
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, sh_m[g][i]);
-    const float ms = mx == neg_inf() ? 0.f : mx;
-    float zt = 0.f, at = 0.f;
+  for (int kb = 0; kb < 4; ++kb) {
+    qb[kb] = make_uint4(0u, 0u, 0u, 0u);
+    if (n < G) qb[kb] = *reinterpret_cast<const uint4*>(a.q + ((size_t)unit * G + n) * ROWB + (size_t)(64 * kb + 16 * lg));
+  }
+  const int L = listed_blocks(a, unit, sh_first);
+  const int count = min(a.part_blocks, a.nsel - (int)blockIdx.x * a.part_blocks);
+  const __amdgpu_buffer_rsrc_t rk = make_rsrc(a.K + (size_t)unit * a.Lcap * ROWB, (uint32_t)L * ROWB);
+  const __amdgpu_buffer_rsrc_t rv = make_rsrc(a.V + (size_t)unit * a.Lcap * ROWB, (uint32_t)L * ROWB);
+  float m_run = neg_inf(), z_run = 0.f, acc[G][EPL];
 #pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
-      const float f = fast_exp2(sh_m[g][i] - ms);
-      zt = fmaf(sh_z[g][i], f, zt);
-      at = fmaf(sh_acc[g][i][c], f, at);
+  for (int g = 0; g < G; ++g)
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) acc[g][e] = 0.f;
+  auto load = [&](typename A::Stage& st, int i) {   // (rows at or above L lie behind the descriptor: zeros, and no memory traffic)
+    const int row = __builtin_amdgcn_readfirstlane(sh_first[i]) + wv * A::TILE;
+    A::template load<false>(st, rk, rv, (uint32_t)(row + lg) * ROWB + (uint32_t)(16 * n), nullptr, 0, lg);
+  };
+  auto compute = [&](const typename A::Stage& st, int i) {
+    A::compute(st, __builtin_amdgcn_readfirstlane(sh_first[i]) + wv * A::TILE, 0, L, n, lg, qb, a.scale_log2, &sh_logit[0][0], A::TILE, sh_kt[wv],
+               sh_p[wv], sh_alpha[wv], m_run, z_run, acc);
+  };
+  typename A::Stage s0, s1;
+  load(s0, 0);
+#pragma unroll
+  for (int i = 0; i < LIST_PART; i += 2) {
+    if (i >= count) break;
+    load(s1, i + 1);
+    compute(s0, i);
+    if (i + 2 < LIST_PART) load(s0, i + 2);
+    compute(s1, i + 1);
+  }
+  z_run += __shfl_xor(z_run, 16);
+  z_run += __shfl_xor(z_run, 32);
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+#pragma unroll
+    for (int e = 0; e < EPL; ++e) {
+      acc[g][e] += __shfl_xor(acc[g][e], 16);
+      acc[g][e] += __shfl_xor(acc[g][e], 32);
     }
-    float* part = partial_of(a.partials, unit * G + g, a.npart, blockIdx.x, D);
-    part[2 + c] = at;
-    if (c == 0) {
-      part[0] = mx;
-      part[1] = zt;
+    if (lg == 0) {
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) sh_acc[g][wv][n * EPL + e] = acc[g][e];
     }
   }
+  if (lg == 0 && n < G) {
+    sh_m[n][wv] = m_run;
+    sh_z[n][wv] = z_run;
+  }
+  __syncthreads();
+  block_partial<D, G>(a, unit, sh_m, sh_z, sh_acc);
 }
 
 }  // namespace

@@ -2,6 +2,7 @@
 // bits, attention over chosen blocks of it or of the plain cache, and the eviction decision by accumulated attention weight.
 // One translation unit:
 //   q8.hpp             rows quantised into blocks of 64, and attention over them (q.K^T and p.V on the matrix cores)
+//   select.hpp         the k-th largest of many numbers
 //   blocks.hpp         bounds of the blocks' keys, the choice, attention over the chosen ones
 //   evict_weight.hpp   the decision by weight (the weights themselves are summed behind corm_kernels.hip's attend launch)
 // Kernel boundaries are the only synchronization between workgroups, and nothing is kept from one call for the next.
@@ -17,6 +18,7 @@
 #include "common.hpp"
 #include "attend.hpp"
 #include "q8.hpp"
+#include "select.hpp"
 #include "blocks.hpp"
 #include "evict_weight.hpp"
 #include "checks.hpp"
@@ -25,15 +27,34 @@ namespace {
 
 int blocks_of(const corm_desc* d) { return (d->Lcap + QBLK - 1) / QBLK; }
 
-// Partials a head can have: parts of at least four blocks, or of a list of up to 512 (the tail's is the last).
+// Partials a head can have: parts of at least four blocks, or of a list of up to 512, and the tail.
 int max_parts(const corm_desc* d) { return std::max((blocks_of(d) + 3) / 4, 128) + 1; }
 int max_listed(const corm_desc* d) { return std::max(blocks_of(d), 512); }
 
-// Each of the calls below has the whole workspace to itself: partials, or scores.
+// Splits of a unit in the eviction decision of few long units, 0 where a workgroup takes a unit alone.
+struct EvictSplits {
+  int splits, slots;
+  size_t listed_off, counts_off, digit_off, total;
+};
+EvictSplits evict_splits(const corm_desc* d) {
+  EvictSplits e = {};
+  const size_t units = (size_t)d->B * d->Hkv;
+  if (d->Lcap <= EVW_KEYS) return e;
+  e.slots = std::max(EVW_SPLIT, ((d->Lcap + 63) / 64 + EVW_WG - 1) / EVW_WG * EVW_WG);
+  e.splits = (d->Lcap + e.slots - 1) / e.slots;
+  if (units * e.splits > EVW_MOST_SPLITS) return EvictSplits{};
+  e.listed_off = align_up(units * e.splits * (sizeof(uint32_t) << EVW_BITS), 256);
+  e.counts_off = e.listed_off + align_up(units * d->Lcap * sizeof(uint32_t), 256);
+  e.digit_off = e.counts_off + align_up(units * e.splits * sizeof(uint32_t), 256);
+  e.total = e.digit_off + align_up(units * sizeof(uint2), 256);
+  return e;
+}
+
+// Each of the calls below has the whole workspace to itself: partials, scores, or what the eviction of long units hands on.
 size_t blocks_workspace(const corm_desc* d) {
   const size_t partials = (size_t)d->B * d->Hq * max_parts(d) * (d->d + 2) * sizeof(float);
   const size_t scores = (size_t)d->B * d->Hkv * blocks_of(d) * sizeof(float);
-  return align_up(std::max(partials, scores), 256);
+  return align_up(std::max({partials, scores, evict_splits(d).total}), 256);
 }
 
 int check_blocks_workspace(const corm_desc* d, const void* workspace, size_t bytes) {
@@ -43,16 +64,12 @@ int check_blocks_workspace(const corm_desc* d, const void* workspace, size_t byt
 
 float scale_log2(const corm_desc* d) { return (d->sm_scale > 0.f ? d->sm_scale : 1.0f / sqrtf((float)d->d)) * LOG2E; }
 
-int merge_parts(const corm_desc* d, const float* partials, const int32_t* lens, float* out, int npart, int part_slots, int all_parts,
-                bool last_apart, hipStream_t s) {
+int merge_parts(const corm_desc* d, const float* partials, const int32_t* lens, float* out, int npart, int part_blocks, hipStream_t s) {
   const int G = d->Hq / d->Hkv;
   const dim3 grid(d->B * d->Hq);
-  if (d->d == 64)
-    hipLaunchKernelGGL(corm_parts_merge_kernel<64>, grid, dim3(64), 0, s, partials, lens, out, G, npart, part_slots, d->Lcap, all_parts,
-                       (int)last_apart);
-  else
-    hipLaunchKernelGGL(corm_parts_merge_kernel<128>, grid, dim3(128), 0, s, partials, lens, out, G, npart, part_slots, d->Lcap,
-                       all_parts, (int)last_apart);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(MERGE_WG), 0, s, partials, lens, out, G, npart, part_blocks, d->Lcap); };
+  if (d->d == 64) launch(corm_parts_merge_kernel<64>);
+  else launch(corm_parts_merge_kernel<128>);
   return launch_status();
 }
 
@@ -118,12 +135,13 @@ int corm_q8_append(const corm_desc* desc, int32_t code_dtype, const void* k_new,
   a.Hkv = desc->Hkv; a.Lcap = desc->Lcap; a.nblk = blocks_of(desc); a.n = n;
   const int units = desc->B * desc->Hkv;
   const dim3 grid((n + 2 * QBLK - 2) / QBLK, units);   // blocks that n rows behind up to 63 others can touch
+  a.lens_here = grid.x == 1 || lens_out != lens;
   hipStream_t s = (hipStream_t)stream;
   rc = by_types(desc, code_dtype, [&](auto c, auto dt, auto dd) {
     hipLaunchKernelGGL((corm_q8_append_kernel<decltype(c), decltype(dt), decltype(dd)::value>), grid, dim3(WG), 0, s, a);
     return launch_status();
   });
-  if (rc || grid.x == 1) return rc;
+  if (rc || a.lens_here) return rc;
   hipLaunchKernelGGL(corm_q8_lens_kernel, dim3((units + WG - 1) / WG), dim3(WG), 0, s, a, units);
   return launch_status();
 }
@@ -151,19 +169,27 @@ int corm_q8_attend(const corm_desc* desc, int32_t code_dtype, const void* q, con
   a.scale_log2 = scale_log2(desc);
   const long units = (long)desc->B * desc->Hkv;
   const int listed = blocks ? nsel : a.nblk;
-  // parts: about four workgroups per compute unit, of whole rounds of blocks over the waves
-  const int want = (int)std::min<long>((4L * device_cus() + units - 1) / units, (listed + WAVES - 1) / WAVES);
-  a.part_blocks = std::min(256, ((listed + want - 1) / want + WAVES - 1) / WAVES * WAVES);
-  const int parts = (listed + a.part_blocks - 1) / a.part_blocks;
-  a.npart = parts + 1;
+  const long cus = device_cus();
+  if (units >= 2 * cus && listed <= Q8_MOST) {
+    a.part_blocks = (listed + WAVES - 1) / WAVES * WAVES;
+    a.npart = 1;
+  } else {
+    const int least = units * ((listed + 2 * WAVES - 1) / (2 * WAVES)) < 2 * cus ? WAVES : 2 * WAVES;
+    const int want = (int)std::min<long>((16 * cus + units - 1) / units, (listed + least - 1) / least);
+    a.part_blocks = std::min(Q8_MOST, ((listed + want - 1) / want + WAVES - 1) / WAVES * WAVES);
+    a.npart = (listed + a.part_blocks - 1) / a.part_blocks + 1;
+  }
+  a.units = (int)units;
+  const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
+  if (groups > 2147483647L) return CORM_EUNSUPPORTED;
   hipStream_t s = (hipStream_t)stream;
   rc = by_types(desc, code_dtype, [&](auto c, auto dt, auto dd) {
-    hipLaunchKernelGGL((corm_q8_attend_kernel<decltype(c), decltype(dt), decltype(dd)::value>), dim3(parts + 1, (unsigned)units), dim3(WG), 0,
-                       s, a);
+    hipLaunchKernelGGL((corm_q8_attend_kernel<decltype(c), decltype(dt), decltype(dd)::value>), dim3((unsigned)groups), dim3(WG), 0, s, a);
     return launch_status();
   });
   if (rc) return rc;
-  return merge_parts(desc, a.partials, lens, out, a.npart, blocks ? 0 : a.part_blocks * QBLK, parts, true, s);
+  if (a.npart == 1) return CORM_OK;
+  return merge_parts(desc, a.partials, lens, out, a.npart, blocks ? 0 : a.part_blocks, s);
 }
 
 int corm_block_bounds(const corm_desc* desc, const void* K, const int32_t* lens, int32_t newest, void* bounds, void* stream) {
@@ -227,15 +253,23 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
   const int parts = (nsel + a.part_blocks - 1) / a.part_blocks;
   a.npart = parts;
   hipStream_t s = (hipStream_t)stream;
-  rc = by_row(desc, [&](auto dt, auto dd) {
-    return by_group(desc, [&](auto g) {
-      hipLaunchKernelGGL((corm_block_attend_kernel<decltype(dt), decltype(dd)::value, decltype(g)::value>), dim3(parts, (unsigned)units),
-                         dim3(WG), 0, s, a);
+  const dim3 grid(parts, (unsigned)units);
+  rc = by_group(desc, [&](auto g) {
+    constexpr int G = decltype(g)::value;
+    // (whole steps, vector ALU | matrix cores: 64 units of eight heads 61.5 | 49.9 us, 128 of four 71.9 | 69.8, 256 of two 108.9 | 109.3)
+    if constexpr (G >= 4) {
+      if (desc->kv_dtype == CORM_BF16 && desc->d == 128) {
+        hipLaunchKernelGGL((corm_block_attend_gqa_kernel<G>), grid, dim3(WG), 0, s, a);
+        return launch_status();
+      }
+    }
+    return by_row(desc, [&](auto dt, auto dd) {
+      hipLaunchKernelGGL((corm_block_attend_kernel<decltype(dt), decltype(dd)::value, G>), grid, dim3(WG), 0, s, a);
       return launch_status();
     });
   });
   if (rc) return rc;
-  return merge_parts(desc, a.partials, lens, out, parts, 0, parts, false, s);
+  return merge_parts(desc, a.partials, lens, out, parts, 0, s);
 }
 
 int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int32_t* lens, int32_t budget, uint8_t* keep, void* workspace,
@@ -245,8 +279,26 @@ int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int
   if (!weight || !lens || !keep || misaligned4(weight) || misaligned4(lens) || budget < desc->r) return CORM_EINVAL;
   rc = check_blocks_workspace(desc, workspace, workspace_bytes);
   if (rc) return rc;
-  hipLaunchKernelGGL(corm_evict_weight_kernel, dim3(desc->B * desc->Hkv), dim3(EVW_WG), 0, (hipStream_t)stream, weight, lens, keep,
-                     desc->Lcap, desc->r, budget);
+  const int units = desc->B * desc->Hkv;
+  hipStream_t s = (hipStream_t)stream;
+  const EvictSplits e = evict_splits(desc);
+  if (e.splits == 0) {
+    const bool held = desc->Lcap <= EVW_KEYS;
+    hipLaunchKernelGGL(corm_evict_weight_kernel, dim3(units), dim3(EVW_WG), held ? (size_t)desc->Lcap * sizeof(uint32_t) : 0, s, weight, lens,
+                       keep, desc->Lcap, desc->r, budget, (int)held);
+    return launch_status();
+  }
+  char* ws = reinterpret_cast<char*>(workspace);
+  EvictLongArgs a;
+  a.weight = weight; a.lens = lens; a.keep = keep;
+  a.hist = reinterpret_cast<uint32_t*>(ws);
+  a.listed = reinterpret_cast<uint32_t*>(ws + e.listed_off);
+  a.counts = reinterpret_cast<uint32_t*>(ws + e.counts_off);
+  a.digit = reinterpret_cast<uint2*>(ws + e.digit_off);
+  a.Lcap = desc->Lcap; a.r = desc->r; a.budget = budget; a.splits = e.splits; a.split_slots = e.slots;
+  hipLaunchKernelGGL(corm_evict_count_kernel, dim3(e.splits, units), dim3(EVW_WG), 0, s, a);
+  hipLaunchKernelGGL(corm_evict_part_kernel, dim3(e.splits, units), dim3(EVW_WG), 0, s, a);
+  hipLaunchKernelGGL(corm_evict_settle_kernel, dim3(units), dim3(EVW_WG), 0, s, a);
   return launch_status();
 }
 

@@ -278,17 +278,17 @@ int launch_attend_record(const corm_desc* d, const Params& p0, const LaunchCtx& 
 }
 
 // The split attend launch, and behind it the weights and out.
-template <int NT>
+template <int ROUNDS>
 int launch_weigh(const corm_desc* d, const Params& p, const float* weight_in, float* weight, hipStream_t s) {
   const int G = d->Hq / d->Hkv;
   const int items = G * (d->d / 64);
-  const int n_out = (d->Lcap + p.part_keys - 1) / p.part_keys <= OUT_WAVE_PARTS ? (items + NT / 64 - 1) / (NT / 64) : items;
-  const dim3 grid(d->B * d->Hkv, p.nsplit + n_out);
+  const int n_out = (d->Lcap + p.part_keys - 1) / p.part_keys <= OUT_WAVE_PARTS ? (items + WAVES - 1) / WAVES : items;
+  const dim3 grid(d->B * d->Hkv, (d->Lcap + ROUNDS * WEIGH_KEYS - 1) / (ROUNDS * WEIGH_KEYS) + n_out), wg(WG);
   switch (G) {
-    case 1: hipLaunchKernelGGL((corm_weigh_kernel<1, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
-    case 2: hipLaunchKernelGGL((corm_weigh_kernel<2, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
-    case 4: hipLaunchKernelGGL((corm_weigh_kernel<4, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
-    case 8: hipLaunchKernelGGL((corm_weigh_kernel<8, NT>), grid, dim3(NT), 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 1: hipLaunchKernelGGL((corm_weigh_kernel<1, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 2: hipLaunchKernelGGL((corm_weigh_kernel<2, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 4: hipLaunchKernelGGL((corm_weigh_kernel<4, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 8: hipLaunchKernelGGL((corm_weigh_kernel<8, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
     default: return CORM_EUNSUPPORTED;
   }
   return launch_status();
@@ -300,7 +300,8 @@ int launch_attend_weigh(const corm_desc* d, const Params& p0, const LaunchCtx& c
   p.head_groups = attend_head_groups(d, c, p.part_keys);
   const int rc = launch_attend(d, p, c, s);
   if (rc) return rc;
-  return launch_weigh<CHUNK>(d, p, weight_in, weight, s);
+  const long two = (long)d->B * d->Hkv * ((d->Lcap + 2 * WEIGH_KEYS - 1) / (2 * WEIGH_KEYS));
+  return two >= 4L * c.cus ? launch_weigh<2>(d, p, weight_in, weight, s) : launch_weigh<1>(d, p, weight_in, weight, s);
 }
 
 // A whole step in one launch (small.hpp)?  A unit is then one workgroup's alone, so only while its rows are few.  Whole steps in a

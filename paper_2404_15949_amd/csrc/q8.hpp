@@ -13,9 +13,18 @@
 namespace {
 
 constexpr int QBLK = 64;   // slots per block
+constexpr int Q8_XCDS = 8;
+constexpr int Q8_MOST = 256;   // blocks of a part, at most
 
 typedef _Float16 half2_t __attribute__((ext_vector_type(2)));
 typedef _Float16 half8_t __attribute__((ext_vector_type(8)));
+
+// Element i of a 16-byte slice of a row.
+template <typename DT>
+__device__ __forceinline__ float element(const uint4& x, int i) {
+  const uint32_t w = (&x.x)[DT::ESZ == 2 ? i >> 1 : i];
+  return DT::ESZ == 2 ? ((i & 1) ? bf16_hi(w) : bf16_lo(w)) : __uint_as_float(w);
+}
 
 struct Q8Args {
   const void* q;
@@ -30,9 +39,9 @@ struct Q8Args {
   float* out;
   float* partials;         // [B*Hq, npart, d+2]
   int32_t* status;
-  int32_t Hq, Hkv, Lcap, nblk, nsel;
+  int32_t units, Hq, Hkv, Lcap, nblk, nsel;
   int32_t part_blocks;     // blocks per workgroup
-  int32_t npart;           // partials per head; the last one is the tail's
+  int32_t npart;           // partials per head, the last one the tail's; with one the workgroup has the tail too and writes out itself
   float scale_log2;
 };
 
@@ -77,10 +86,14 @@ __device__ __forceinline__ half8_t unpack8(uint32_t x, uint32_t y) {
                                  1, 2, 3, 4, 5, 6, 7);
 }
 
-// x = hi + lo in halves: hi towards zero, so that the difference is exact; together 22 bits
+// x = hi + lo in halves: hi towards zero, so that the difference is exact; together 22 bits.  NEAREST: lo to the nearest (queries, whose error grows with
+// the score; for probabilities, of which there is one for every key, the packed conversion will do)
+template <bool NEAREST>
 __device__ __forceinline__ void split_half(float x, float y, half2_t& hi, half2_t& lo) {
   hi = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(x, y));
-  lo = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(x - (float)hi[0], y - (float)hi[1]));
+  const float a = x - (float)hi[0], b = y - (float)hi[1];
+  if (NEAREST) lo = half2_t{(_Float16)a, (_Float16)b};
+  else lo = __builtin_bit_cast(half2_t, __builtin_amdgcn_cvt_pkrtz(a, b));
 }
 
 // ---------------------------------------------------------------- attention
@@ -90,38 +103,56 @@ __device__ __forceinline__ float* partial_of(float* partials, int head, int npar
   return partials + ((size_t)head * npart + part) * (D + 2);
 }
 
-// The rows of the unfinished block, which are in the KV type: a wave takes a query head at a time (vector ALU: at most 63 rows).
-template <typename DT, int D>
-__device__ __forceinline__ void tail_attend(const void* q, const char* Kt, const char* Vt, float* partials, int rows, int head0,
-                                            int G, int npart, int part, float times, float scale_log2, float* sh_logit) {
+// The rows of the unfinished block, which are in the KV type (vector ALU: at most 63 rows).  With one or two heads the waves share the rows, else
+// the heads: folding the lanes of a head's rows costs more than reading them again.  What a wave finds goes to sh_*[set], `times` over;
+// returns the sets that are filled.
+template <typename DT, int D, typename Acc, typename Row>
+__device__ __forceinline__ int tail_attend(const void* q, const char* Kt, const char* Vt, int rows, int head0, int G, float times,
+                                           float scale_log2, float* sh_junk, Row* sh_m, Row* sh_z, Acc* sh_acc) {
   using A = Attend<DT, D, 1, 1>;
   constexpr int EPL = A::EPL, ROWB = A::ROWB, LPR = A::LPR;
-  constexpr int STAGES = (QBLK + A::STAGE_ROWS - 1) / A::STAGE_ROWS;
+  constexpr int STAGES = QBLK / A::STAGE_ROWS, BATCH = STAGES < 4 ? STAGES : 4;   // of the block; in flight together
   const int lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int sub = lane / LPR, cl = lane % LPR;
   const __amdgpu_buffer_rsrc_t rk = make_rsrc(Kt, (uint32_t)rows * ROWB), rv = make_rsrc(Vt, (uint32_t)rows * ROWB);
-  const uint32_t off = (uint32_t)sub * ROWB + (uint32_t)cl * 16;
-  for (int g = wv; g < G; g += WAVES) {
+  auto load = [&](typename A::Stage& st, int s) {   // (rows past the last lie behind the descriptor: zeros, and no memory traffic)
+    A::template load<false>(st, rk, rv, (uint32_t)(s * A::STAGE_ROWS + sub) * ROWB + (uint32_t)cl * 16, nullptr, 0);
+  };
+  const bool by_rows = G <= 2;
+  for (int g = by_rows ? 0 : wv; g < G; g += by_rows ? 1 : WAVES) {
     const uint4 qreg[1] = {*reinterpret_cast<const uint4*>(reinterpret_cast<const char*>(q) + (size_t)(head0 + g) * ROWB + (size_t)cl * 16)};
     float m[1] = {neg_inf()}, z[1] = {0.f}, acc[1][EPL] = {};
+    auto compute = [&](const typename A::Stage& st, int s) {
+      A::compute(st, s * A::STAGE_ROWS + sub, sub, rows, cl, qreg, scale_log2, sh_junk, 0, m, z, acc);
+    };
+    if (by_rows) {
+      for (int s = wv; s < STAGES; s += WAVES) {
+        typename A::Stage st;
+        load(st, s);
+        compute(st, s);
+      }
+    } else {
 #pragma unroll
-    for (int s = 0; s < STAGES; ++s) {
-      if (s * A::STAGE_ROWS >= rows) break;
-      typename A::Stage st;
-      A::template load<false>(st, rk, rv, off + (uint32_t)(s * A::STAGE_ROWS * ROWB), nullptr, 0);
-      A::compute(st, s * A::STAGE_ROWS + sub, s * A::STAGE_ROWS + sub, rows, cl, qreg, scale_log2, sh_logit + wv * 2 * QBLK, 0, m, z, acc);
+      for (int s0 = 0; s0 < STAGES; s0 += BATCH) {
+        typename A::Stage st[BATCH];
+#pragma unroll
+        for (int s = 0; s < BATCH; ++s) load(st[s], s0 + s);
+#pragma unroll
+        for (int s = 0; s < BATCH; ++s) compute(st[s], s0 + s);
+      }
     }
     A::merge_rows(m[0], z[0], acc[0]);
-    float* p = partial_of(partials, head0 + g, npart, part, D);
+    const int set = by_rows ? wv : 0;
     if (sub == 0) {
 #pragma unroll
-      for (int e = 0; e < EPL; ++e) p[2 + cl * EPL + e] = acc[0][e] * times;
+      for (int e = 0; e < EPL; ++e) sh_acc[set][g][cl * EPL + e] = acc[0][e] * times;
       if (cl == 0) {
-        p[0] = m[0];
-        p[1] = z[0] * times;
+        sh_m[set][g] = m[0];
+        sh_z[set][g] = z[0] * times;
       }
     }
   }
+  return by_rows ? WAVES : 1;
 }
 
 // A query head in the B operand of the products: lane (n = l%16, lg = l/16) holds channels 64*(kb/2) + 16*lg + 8*(kb%2) .. +8 of head n in step
@@ -132,36 +163,30 @@ struct QueryOperand {
   static constexpr int PARTS = DT::ESZ == 4 ? 2 : 1;
   half8_t part[PARTS][STEPS];
   float undo;   // 1 / the power of two
+  uint4 raw[STEPS][DT::ESZ / 2];
 
   __device__ __forceinline__ void load(const char* q, int n, int lg, int G) {
-    float x[STEPS][8];
-    float top = 0.f;
 #pragma unroll
     for (int kb = 0; kb < STEPS; ++kb) {
       const int c = 64 * (kb / 2) + 16 * lg + 8 * (kb % 2);
-      if (n < G) {
-        const uint4* at = reinterpret_cast<const uint4*>(q + ((size_t)n * D + c) * DT::ESZ);
-        const uint4 a = at[0];
-        if (DT::ESZ == 2) {
-          const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            x[kb][2 * i] = bf16_lo(w[i]);
-            x[kb][2 * i + 1] = bf16_hi(w[i]);
-          }
-        } else {
-          const uint4 b = at[1];
-          const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-#pragma unroll
-          for (int i = 0; i < 8; ++i) x[kb][i] = __uint_as_float(w[i]);
-        }
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[kb][i] = 0.f;
+      for (int i = 0; i < DT::ESZ / 2; ++i) {
+        raw[kb][i] = make_uint4(0u, 0u, 0u, 0u);
+        if (n < G) raw[kb][i] = reinterpret_cast<const uint4*>(q + ((size_t)n * D + c) * DT::ESZ)[i];
       }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[kb][i]));
     }
+  }
+
+  __device__ __forceinline__ void convert() {
+    float x[STEPS][8];
+    float top = 0.f;
+#pragma unroll
+    for (int kb = 0; kb < STEPS; ++kb)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        x[kb][i] = element<DT>(raw[kb][i / DT::EPL], i % DT::EPL);
+        top = fmaxf(top, fabsf(x[kb][i]));
+      }
     top = rows_allreduce_max(top);
     const uint32_t e = min(max(__float_as_uint(top) >> 23, 14u), 254u);
     const float up = __uint_as_float((267u - e) << 23);
@@ -170,7 +195,7 @@ struct QueryOperand {
     for (int kb = 0; kb < STEPS; ++kb) {
       half2_t hi[4], lo[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) split_half(x[kb][2 * i] * up, x[kb][2 * i + 1] * up, hi[i], lo[i]);
+      for (int i = 0; i < 4; ++i) split_half<true>(x[kb][2 * i] * up, x[kb][2 * i + 1] * up, hi[i], lo[i]);
       auto join = [](const half2_t(&h)[4]) {
         return __builtin_shufflevector(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3), __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3),
                                        0, 1, 2, 3, 4, 5, 6, 7);
@@ -181,7 +206,8 @@ struct QueryOperand {
   }
 };
 
-// Grid (parts + 1, units); a wave takes every fourth block of its workgroup's part, the last column of the grid the tail.
+// A workgroup is a part of a unit, a wave takes every fourth block of it; the tail is the last part, or a workgroup has the whole unit.  Workgroups go to the 8 dies in
+// turn: each die gets whole units, one after the other, so that no die has all first or all last parts, nor all units of a head.
 //
 // S^T = K q^T: four tiles of 16 keys, A = 16 keys x 32 channels of codes, B = the heads of the unit in columns 0 .. G-1.  Row m of
 // tile t is key 16*(m/4) + 4*t + m%4, so that lane (n, lg) gets the scores of head n for keys 16*lg .. +16 in the order of its 16 registers --
@@ -191,50 +217,50 @@ struct QueryOperand {
 // what is 2^-40 of the largest), so the products with the codes are exact and everything is summed in fp32.  The scales are
 // taken in where they cost least: a block's key scale with the softmax scale (one product a score), its value scale with the sum of the block.
 template <typename C, typename DT, int D>
-__global__ __launch_bounds__(WG, 2) void corm_q8_attend_kernel(const Q8Args a) {
+__global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   constexpr int PANELS = D / 64, CT = D / 16, STEPS = D / 32;
   constexpr float RAISE = 15.f;
-  __shared__ float sh_acc[WAVES][8][D];
-  __shared__ float sh_m[WAVES][8], sh_z[WAVES][8];
-  __shared__ int sh_ids[256];
-  __shared__ int sh_n;
-  const int unit = blockIdx.y, G = a.Hq / a.Hkv;
+  __shared__ float sh_acc[2 * WAVES][8][D];   // of the waves' blocks; of their rows of the tail
+  __shared__ float sh_m[2 * WAVES][8], sh_z[2 * WAVES][8];
+  __shared__ float sh_junk[QBLK];
+  __shared__ int sh_ids[Q8_MOST];
+  __shared__ int sh_n, sh_times;
+  const int G = a.Hq / a.Hkv;
+  const int item = (int)(blockIdx.x % Q8_XCDS) * (int)(gridDim.x / Q8_XCDS) + (int)(blockIdx.x / Q8_XCDS);
+  const int unit = item / a.npart, part = item - unit * a.npart;
+  if (unit >= a.units) return;
   const int head0 = unit * G;   // b * Hq + hkv * G
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, lg = lane >> 4;
+  QueryOperand<DT, D> qo;
+  qo.load(reinterpret_cast<const char*>(a.q) + (size_t)head0 * D * DT::ESZ, n, lg, G);
   int L = a.lens[unit];
   if (L < 0 || L > a.Lcap) {
-    if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, CORM_DEV_BAD_LENS);
+    if (part == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, CORM_DEV_BAD_LENS);
     L = L < 0 ? 0 : a.Lcap;
   }
   const int full = L / QBLK, rest = L % QBLK;
   const int32_t* list = a.blocks ? a.blocks + (size_t)unit * a.nsel : nullptr;
-
-  if (blockIdx.x == gridDim.x - 1) {   // the tail
-    int times = rest > 0 ? 1 : 0;
-    if (list) {   // as often as it is listed
-      if (threadIdx.x == 0) sh_n = 0;
-      __syncthreads();
-      int mine = 0;
-      bool bad = false;
-      for (int i = threadIdx.x; i < a.nsel; i += WG) {
-        const int id = list[i];
-        mine += rest > 0 && id == full;
-        bad |= id < -1 || id >= full + (rest > 0);
-      }
-      if (mine) atomicAdd(&sh_n, mine);
-      if (bad && a.status) atomicOr(a.status, CORM_DEV_BAD_BLOCK);
-      __syncthreads();
-      times = sh_n;
+  const bool has_tail = part == a.npart - 1;
+  int times = has_tail && rest > 0 ? 1 : 0;   // the tail counts as often as it is listed
+  if (list && has_tail) {
+    if (threadIdx.x == 0) sh_times = 0;
+    __syncthreads();
+    int mine = 0;
+    bool bad = false;
+    for (int i = threadIdx.x; i < a.nsel; i += WG) {
+      const int id = list[i];
+      mine += rest > 0 && id == full;
+      bad |= id < -1 || id >= full + (rest > 0);
     }
-    const char* Kt = reinterpret_cast<const char*>(a.Kt) + (size_t)unit * QBLK * D * DT::ESZ;
-    const char* Vt = reinterpret_cast<const char*>(a.Vt) + (size_t)unit * QBLK * D * DT::ESZ;
-    tail_attend<DT, D>(a.q, Kt, Vt, a.partials, times ? rest : 0, head0, G, a.npart, a.npart - 1, (float)times,
-                       a.scale_log2, &sh_acc[0][0][0]);
-    return;
+    if (mine) atomicAdd(&sh_times, mine);
+    if (bad && a.status) atomicOr(a.status, CORM_DEV_BAD_BLOCK);
+    __syncthreads();
+    times = sh_times;
   }
 
   // this workgroup's blocks
-  const int first = blockIdx.x * a.part_blocks;
+  const int first = part * a.part_blocks;
   int count;
   if (list) {
     if (wv == 0) {
@@ -253,13 +279,8 @@ __global__ __launch_bounds__(WG, 2) void corm_q8_attend_kernel(const Q8Args a) {
     count = sh_n;
   } else {
     count = min(a.part_blocks, full - first);
-    if (count <= 0) return;
+    if (count <= 0 && !has_tail) return;
   }
-
-  const int n = lane & 15, lg = lane >> 4;
-  QueryOperand<DT, D> qo;
-  qo.load(reinterpret_cast<const char*>(a.q) + (size_t)head0 * D * DT::ESZ, n, lg, G);
-  const float qscale = qo.undo * a.scale_log2;
 
   constexpr uint32_t BLKB = QBLK * D;   // bytes of a block's codes
   const __amdgpu_buffer_rsrc_t rk = make_rsrc(a.Kc + (size_t)unit * a.nblk * BLKB, (uint32_t)full * BLKB);
@@ -286,129 +307,167 @@ __global__ __launch_bounds__(WG, 2) void corm_q8_attend_kernel(const Q8Args a) {
 
   float m_run = neg_inf(), z_run = 0.f;   // of head n; the sum is of this lane's keys
   f32x4_t acc[CT] = {};                   // channels 16*ct + 4*lg .. +4 of head n
-  int id = id_of(wv);
-  load_k(id);
-  load_v(id);
-  float knext = ks[min(id, a.nblk - 1)], vnext = vs[min(id, a.nblk - 1)];
-  for (int i = wv; i < count; i += WAVES) {
-    const float kscale = knext * qscale, vscale = vnext;
-    id = id_of(i + WAVES);
-    knext = ks[min(id, a.nblk - 1)];
-    vnext = vs[min(id, a.nblk - 1)];
-    f32x4_t s[4];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      f32x4_t d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int kb = 0; kb < STEPS; ++kb) {
-        const u32x4_t k = K[t][kb / 2];
-        const half8_t x = kb % 2 ? unpack8<C>(k.z, k.w) : unpack8<C>(k.x, k.y);
-#pragma unroll
-        for (int w = 0; w < qo.PARTS; ++w) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qo.part[w][kb], d, 0, 0, 0);
-      }
-      s[t] = d;
-    }
+  if (count > 0) {   // (not the part that is the tail alone)
+    int id = id_of(wv);
     load_k(id);
-    float top = neg_inf();
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        s[t][j] *= kscale;
-        top = fmaxf(top, s[t][j]);
-      }
-    top = rows_allreduce_max(top);
-    const float m = fmaxf(m_run, top);
-    const float less = (m == neg_inf() ? 0.f : m) - RAISE;
-    const float fade = fast_exp2(m_run - RAISE - less);
-    m_run = m;
-    half2_t hi[8], lo[8];
-    float zs = 0.f;
-#pragma unroll
-    for (int t = 0; t < 4; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; j += 2) {
-        const float x = fast_exp2(s[t][j] - less), y = fast_exp2(s[t][j + 1] - less);
-        zs += x + y;
-        split_half(x, y, hi[2 * t + j / 2], lo[2 * t + j / 2]);
-      }
-    z_run = fmaf(z_run, fade, zs);
-    auto join = [](const half2_t* h) {
-      return __builtin_shufflevector(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3), __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3), 0,
-                                     1, 2, 3, 4, 5, 6, 7);
-    };
-    const half8_t ph[2] = {join(hi), join(hi + 4)}, pl[2] = {join(lo), join(lo + 4)};
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-      f32x4_t d = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const half8_t x = u ? unpack8<C>(V[c].z, V[c].w) : unpack8<C>(V[c].x, V[c].y);
-        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, ph[u], d, 0, 0, 0);
-        d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pl[u], d, 0, 0, 0);
-      }
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[c][j] = fmaf(d[j], vscale, acc[c][j] * fade);
-    }
     load_v(id);
+    qo.convert();   // (behind the loads of the first block: its time is hidden in theirs)
+    const float qscale = qo.undo * a.scale_log2;
+    float knext = ks[min(id, a.nblk - 1)], vnext = vs[min(id, a.nblk - 1)];
+    for (int i = wv; i < count; i += WAVES) {
+      const float kscale = knext * qscale, vscale = vnext;
+      id = id_of(i + WAVES);
+      knext = ks[min(id, a.nblk - 1)];
+      vnext = vs[min(id, a.nblk - 1)];
+      f32x4_t s[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        f32x4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kb = 0; kb < STEPS; ++kb) {
+          const u32x4_t k = K[t][kb / 2];
+          const half8_t x = kb % 2 ? unpack8<C>(k.z, k.w) : unpack8<C>(k.x, k.y);
+#pragma unroll
+          for (int w = 0; w < qo.PARTS; ++w) d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, qo.part[w][kb], d, 0, 0, 0);
+        }
+        s[t] = d;
+      }
+      load_k(id);
+      float top = neg_inf();
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          s[t][j] *= kscale;
+          top = fmaxf(top, s[t][j]);
+        }
+      top = rows_allreduce_max(top);
+      const float m = fmaxf(m_run, top);
+      const float less = (m == neg_inf() ? 0.f : m) - RAISE;
+      const float fade = fast_exp2(m_run - RAISE - less);
+      m_run = m;
+      half2_t hi[8], lo[8];
+      float zs = 0.f;
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+          const float x = fast_exp2(s[t][j] - less), y = fast_exp2(s[t][j + 1] - less);
+          zs += x + y;
+          split_half<false>(x, y, hi[2 * t + j / 2], lo[2 * t + j / 2]);
+        }
+      z_run = fmaf(z_run, fade, zs);
+      auto join = [](const half2_t* h) {
+        return __builtin_shufflevector(__builtin_shufflevector(h[0], h[1], 0, 1, 2, 3), __builtin_shufflevector(h[2], h[3], 0, 1, 2, 3), 0,
+                                       1, 2, 3, 4, 5, 6, 7);
+      };
+      const half8_t ph[2] = {join(hi), join(hi + 4)}, pl[2] = {join(lo), join(lo + 4)};
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        f32x4_t d = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const half8_t x = u ? unpack8<C>(V[c].z, V[c].w) : unpack8<C>(V[c].x, V[c].y);
+          d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, ph[u], d, 0, 0, 0);
+          d = __builtin_amdgcn_mfma_f32_16x16x32_f16(x, pl[u], d, 0, 0, 0);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[c][j] = fmaf(d[j], vscale, acc[c][j] * fade);
+      }
+      load_v(id);
+    }
   }
 
-  // the waves meet
+  // the waves meet, and the tail
   z_run = rows_allreduce_sum(z_run);
   if (n < G) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4_t*>(&sh_acc[wv][n][16 * c + 4 * lg]) = acc[c];
-    if (lg == 0) {
-      sh_m[wv][n] = m_run;
+    if (lg == 0) {   // (sum and products are 2^15 times those of the maximum)
+      sh_m[wv][n] = m_run - RAISE;
       sh_z[wv][n] = z_run;
     }
+  }
+  int sets = WAVES;
+  if (times) {
+    const char* Kt = reinterpret_cast<const char*>(a.Kt) + (size_t)unit * QBLK * D * DT::ESZ;
+    const char* Vt = reinterpret_cast<const char*>(a.Vt) + (size_t)unit * QBLK * D * DT::ESZ;
+    sets += tail_attend<DT, D>(a.q, Kt, Vt, rest, head0, G, (float)times, a.scale_log2, sh_junk, sh_m + WAVES, sh_z + WAVES, sh_acc + WAVES);
   }
   __syncthreads();
   for (int idx = threadIdx.x; idx < G * D; idx += WG) {
     const int g = idx / D, c = idx - g * D;
     float mx = neg_inf();
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) mx = fmaxf(mx, sh_m[i][g]);
+    for (int i = 0; i < sets; ++i) mx = fmaxf(mx, sh_m[i][g]);
     const float ms = mx == neg_inf() ? 0.f : mx;
     float zt = 0.f, at = 0.f;
-#pragma unroll
-    for (int i = 0; i < WAVES; ++i) {
+    for (int i = 0; i < sets; ++i) {
       const float f = fast_exp2(sh_m[i][g] - ms);
       zt = fmaf(sh_z[i][g], f, zt);
       at = fmaf(sh_acc[i][g][c], f, at);
     }
-    float* part = partial_of(a.partials, head0 + g, a.npart, blockIdx.x, D);
-    part[2 + c] = at;
-    if (c == 0) {
-      part[0] = mx - RAISE;   // (sum and products are 2^15 times those of max mx)
-      part[1] = zt;
+    if (a.npart == 1) {
+      a.out[(size_t)(head0 + g) * D + c] = zt > 0.f ? at / zt : 0.f;
+    } else {
+      float* to = partial_of(a.partials, head0 + g, a.npart, part, D);
+      to[2 + c] = at;
+      if (c == 0) {
+        to[0] = mx;
+        to[1] = zt;
+      }
     }
   }
 }
 
-// out of a head from its partials [0, parts) and, if given, one more (the tail's): a thread per channel.
+// out of a head from its partials: npart of them, or (part_blocks > 0) one for every so many full blocks of the unit and the last.  A few kilobytes a head, so its time is its
+// chain of latencies: every wave finds the head's maximum and sum with a lane a partial; then a thread has a channel, the groups of D threads
+// share the partials and take eight at a time.  (One after the other by D threads alone: 32 partials 16 us, so 4.)
+constexpr int MERGE_WG = 256, MERGE_BATCH = 8;
 template <int D>
-__global__ __launch_bounds__(D) void corm_parts_merge_kernel(const float* partials, const int32_t* lens, float* out, int G, int npart,
-                                                             int part_slots, int Lcap, int all_parts, int last_apart) {
-  const int head = blockIdx.x, c = threadIdx.x;
+__global__ __launch_bounds__(MERGE_WG) void corm_parts_merge_kernel(const float* partials, const int32_t* lens, float* out, int G,
+                                                                    int npart, int part_blocks, int Lcap) {
+  constexpr int GROUPS = MERGE_WG / D;
+  __shared__ float sh[GROUPS][D];
+  const int head = blockIdx.x, lane = threadIdx.x & 63;
   const float* p0 = partials + (size_t)head * npart * (D + 2);
-  int parts = all_parts;
-  if (part_slots > 0) {   // parts that hold whole blocks
-    const int L = min(max(lens[head / G], 0), Lcap);
-    parts = (L / QBLK * QBLK + part_slots - 1) / part_slots;
+  int n = npart;
+  if (part_blocks > 0) n = (min(max(lens[head / G], 0), Lcap) / QBLK + part_blocks - 1) / part_blocks + 1;
+  auto at = [&](int s) { return p0 + (size_t)(s < n - 1 ? s : npart - 1) * (D + 2); };
+  float mx = neg_inf(), z = 0.f;
+  for (int s = lane; s < n; s += 64) {
+    const float2 x = *reinterpret_cast<const float2*>(at(s));
+    const float m = fmaxf(mx, x.x), ms = m == neg_inf() ? 0.f : m;
+    z = fmaf(z, fast_exp2(mx - ms), x.y * fast_exp2(x.x - ms));
+    mx = m;
   }
-  float mx = last_apart ? p0[(size_t)(npart - 1) * (D + 2)] : neg_inf();
-  for (int s = 0; s < parts; ++s) mx = fmaxf(mx, p0[(size_t)s * (D + 2)]);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const float mo = __shfl_xor(mx, o), zo = __shfl_xor(z, o);
+    const float m = fmaxf(mx, mo), ms = m == neg_inf() ? 0.f : m;
+    z = fmaf(z, fast_exp2(mx - ms), zo * fast_exp2(mo - ms));
+    mx = m;
+  }
   const float ms = mx == neg_inf() ? 0.f : mx;
-  float z = 0.f, at = 0.f;
-  auto add = [&](const float* p) {
-    const float f = fast_exp2(p[0] - ms);
-    z = fmaf(p[1], f, z);
-    at = fmaf(p[2 + c], f, at);
-  };
-  for (int s = 0; s < parts; ++s) add(p0 + (size_t)s * (D + 2));
-  if (last_apart) add(p0 + (size_t)(npart - 1) * (D + 2));
-  out[(size_t)head * D + c] = z > 0.f ? at / z : 0.f;
+  const int grp = threadIdx.x / D, c = threadIdx.x % D;
+  float sum = 0.f;
+  for (int s0 = grp; s0 < n; s0 += GROUPS * MERGE_BATCH) {
+    float m[MERGE_BATCH], v[MERGE_BATCH];
+#pragma unroll
+    for (int u = 0; u < MERGE_BATCH; ++u) {
+      const float* p = at(min(s0 + u * GROUPS, n - 1));
+      m[u] = p[0];
+      v[u] = p[2 + c];
+    }
+#pragma unroll
+    for (int u = 0; u < MERGE_BATCH; ++u) sum = fmaf(s0 + u * GROUPS < n ? v[u] : 0.f, fast_exp2(m[u] - ms), sum);
+  }
+  sh[grp][c] = sum;
+  __syncthreads();
+  if (grp == 0) {
+#pragma unroll
+    for (int i = 1; i < GROUPS; ++i) sum += sh[i][c];
+    out[(size_t)head * D + c] = z > 0.f ? sum / z : 0.f;
+  }
 }
 
 // ---------------------------------------------------------------- rows into the cache
@@ -428,6 +487,7 @@ struct Q8AppendArgs {
   char* bounds;            // optional [units, nblk, 2, d]
   int32_t* status;
   int32_t Hkv, Lcap, nblk, n;
+  int32_t lens_here;       // this launch writes the new lengths (not where they replace the old ones and a unit has several workgroups)
 };
 
 // What a unit gets from this call: its length before, and the rows that come (0 where they do not fit, or lens is none).
@@ -458,11 +518,6 @@ __global__ __launch_bounds__(WG) void corm_q8_lens_kernel(const Q8AppendArgs a, 
 }
 
 template <typename DT>
-__device__ __forceinline__ float element(const uint4& x, int i) {
-  const uint32_t w = (&x.x)[DT::ESZ == 2 ? i >> 1 : i];
-  return DT::ESZ == 2 ? ((i & 1) ? bf16_hi(w) : bf16_lo(w)) : __uint_as_float(w);
-}
-template <typename DT>
 __device__ __forceinline__ void put_element(char* at, float v) {   // (v is an element: nothing is rounded)
   if (DT::ESZ == 2) *reinterpret_cast<uint16_t*>(at) = (uint16_t)(__float_as_uint(v) >> 16);
   else *reinterpret_cast<float*>(at) = v;
@@ -471,7 +526,7 @@ __device__ __forceinline__ void put_element(char* at, float v) {   // (v is an e
 // Grid (blocks a call can touch, units).  A workgroup takes a block that gets full: a thread has four consecutive rows of a
 // 16-byte column slice, so that it packs four channels of a key and four keys of a channel into words; the value words take a turn
 // through LDS to lie by channel.  The first workgroup of a unit also writes the rows that stay unfinished (behind its own
-// loads: the block it has may be made of the old tail) and, where it is alone, the new length.
+// loads: the block it has may be made of the old tail) and, unless others still have to read the old one, the new length.
 template <typename C, typename DT, int D>
 __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a) {
   constexpr int ESZ = DT::ESZ, EPL = DT::EPL, ROWB = D * ESZ, SL = ROWB / 16;   // 16-byte slices of a row
@@ -624,7 +679,7 @@ __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a
     }
   }
   __syncthreads();   // (lens_out may be lens: every wave has read it)
-  if (gridDim.x == 1 && tid == 0) {
+  if (a.lens_here && tid == 0) {
     if (r.flags && a.status) atomicOr(a.status, r.flags);
     a.lens_out[unit] = r.L0 + r.n;
   }

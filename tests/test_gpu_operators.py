@@ -314,7 +314,8 @@ def test_attend_weigh(B, Hq, Hkv, d, cap, dtype, path):
 
 
 @pytest.mark.parametrize("units,cap,r,budget", [(3, 50, 1, 1), (4, 700, 16, 200), (2, 1024, 1, 1023), (5, 1500, 100, 100), (13, 4100, 64, 1000),
-                                                (1, 9000, 3, 5000), (2, 40000, 500, 2000), (1, 200000, 5, 70000)])
+                                                (1, 9000, 3, 5000), (2, 16384, 10, 3000), (2, 16385, 50, 50), (2, 40000, 500, 2000), (3, 30001, 7, 9000),
+                                                (1, 200000, 5, 70000)])
 def test_evict_mask_weight(units, cap, r, budget):
     """Heavy-tailed accounts with zeros and many equal ones; lengths on both sides of the budget."""
     g = _gen(cap)
