@@ -450,7 +450,8 @@ class LayerState:
     """The device arrays of one layer, allocated with torch, in the layouts corm.h documents."""
 
     def __init__(self, B, Hq, Hkv, d, Lcap, Tcap, w, r, dtype, thr_scale=1.0, device="cuda",
-                 workspace: Optional[torch.Tensor] = None, want_masks=False, want_ring=True, score_dtype=None):
+                 workspace: Optional[torch.Tensor] = None, want_masks=False, want_ring=True, score_dtype=None, want_bounds=False,
+                 want_weight=False):
         tdt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         self.desc = make_desc(B, Hq, Hkv, d, Lcap, Tcap, w, r, dtype, score_dtype=score_dtype, thr_scale=thr_scale)
         self.ring_bits = self.desc.score_dtype == CORM_BIT
@@ -480,6 +481,15 @@ class LayerState:
             workspace = torch.empty(corm_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
             corm_workspace_init(self.desc, workspace)
         self.workspace = workspace
+        # want_bounds: bounds of the blocks' keys, for step_blocks; want_weight: the keys' accounts, for step_weigh
+        nblk = (Lcap + BLOCK - 1) // BLOCK
+        self.bounds = torch.zeros(B, Hkv, nblk, 2, d, dtype=tdt, device=device) if want_bounds else None
+        self._blocks = {}
+        self.weight = torch.zeros(B, Hkv, Lcap, dtype=torch.float32, device=device) if want_weight else None
+        self.weight_keep = torch.zeros(B, Hkv, Lcap, dtype=torch.uint8, device=device) if want_weight else None
+        self.blocks_workspace = None
+        if want_bounds or want_weight:
+            self.blocks_workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
 
     def preload(self, K0: torch.Tensor, V0: torch.Tensor) -> None:
         """Copy n prompt keys/values [B,Hkv,n,d] into slots 0..n-1 (positions 0..n-1, never important yet)."""
@@ -517,48 +527,44 @@ class LayerState:
                           t_first, self.ring, self.keep, self.kept_idx,
                           self.workspace if workspace is None else workspace, status=self.status, stream=stream)
 
-    # The two steps below keep what they need in arrays of their own, allocated at first use; neither touches the ring.
-
-    def _blocks_workspace(self):
-        need = corm_blocks_workspace_bytes(self.desc)
-        if getattr(self, "blocks_workspace", None) is None:
-            self.blocks_workspace = torch.empty(need, dtype=torch.uint8, device=self.K.device)
-        return self.blocks_workspace
-
     def renew_bounds(self, newest=0, stream=None) -> None:
         """Bounds of the blocks' keys (all of them, or those of the newest slots): after a prompt, and after rows have moved."""
-        if getattr(self, "bounds", None) is None:
-            self.bounds = torch.zeros(self.B, self.Hkv, (self.Lcap + BLOCK - 1) // BLOCK, 2, self.d, dtype=self.dtype, device=self.K.device)
+        if self.bounds is None:
+            raise RuntimeError("made without want_bounds")
         corm_block_bounds(self.desc, self.K, self.lens, self.bounds, newest, stream=stream)
 
     def step_blocks(self, q, k_new, v_new, t, nsel, nlast=1, stream=None) -> None:
         """One decode step that attends to nsel blocks of 64 slots (the nlast newest and those with the highest score bounds): append,
-        the newest block's bounds, choice, attention.  Nothing is recorded or evicted.  renew_bounds() first, after the prompt."""
-        if getattr(self, "bounds", None) is None:
-            raise RuntimeError("renew_bounds() first")
-        if getattr(self, "blocks", None) is None or self.blocks.shape[2] != nsel:
-            self.blocks = torch.empty(self.B, self.Hkv, nsel, dtype=torch.int32, device=self.K.device)
-        ws = self._blocks_workspace()
+        the newest block's bounds, choice (self.blocks), attention.  Nothing is recorded or evicted.  renew_bounds() first, after the prompt."""
+        if self.bounds is None:
+            raise RuntimeError("made without want_bounds")
+        self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.K.device)
+        ws = self.blocks_workspace
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, self.last_hit, k_new, v_new, t, self.status, stream=stream)
         self.renew_bounds(1, stream=stream)
         corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, ws, stream=stream)
         corm_block_attend(self.desc, q, self.K, self.V, self.lens, self.blocks, nsel, self.out, ws, status=self.status, stream=stream)
 
     def step_weigh(self, q, k_new, v_new, t, budget=None, stream=None) -> None:
-        """One decode step of eviction by accumulated attention weight: append, attend and account, and with a budget cut every
-        longer unit to it (the r newest slots and the heaviest others).  weight [B,Hkv,Lcap] holds the accounts."""
-        if getattr(self, "weight", None) is None:
-            self.weight = torch.zeros(self.B, self.Hkv, self.Lcap, dtype=torch.float32, device=self.K.device)
+        """One decode step of eviction by accumulated attention weight: append, attend and account (self.weight), and with a budget cut every
+        longer unit to it (the r newest slots and the heaviest others; self.weight_keep: the slots that stayed)."""
+        if self.weight is None:
+            raise RuntimeError("made without want_weight")
         account = self.weight   # 4-byte entries: append and the gather carry them in the place of last_hit
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, account, k_new, v_new, t, self.status, stream=stream)
         corm_decode_attend_weigh(self.desc, q, self.K, self.V, self.lens, account, account, self.out, self.workspace,
                                  status=self.status, stream=stream)
-        if budget is None:
-            return
-        if getattr(self, "keep", None) is None:
-            self.keep = torch.zeros(self.B, self.Hkv, self.Lcap, dtype=torch.uint8, device=self.K.device)
-        corm_evict_mask_weight(self.desc, account, self.lens, budget, self.keep, self._blocks_workspace(), stream=stream)
-        corm_compact(self.desc, self.K, self.V, self.pos, account, self.lens, self.keep, self.kept_idx, self.workspace, stream=stream)
+        if budget is not None:
+            corm_evict_mask_weight(self.desc, account, self.lens, budget, self.weight_keep, self.blocks_workspace, stream=stream)
+            corm_compact(self.desc, self.K, self.V, self.pos, account, self.lens, self.weight_keep, self.kept_idx, self.workspace,
+                         stream=stream)
+
+
+def _block_list(lists, B, Hkv, nsel, device) -> torch.Tensor:
+    """The array for nsel chosen blocks; none is given back while a step on some stream may still read it."""
+    if nsel not in lists:
+        lists[nsel] = torch.empty(B, Hkv, nsel, dtype=torch.int32, device=device)
+    return lists[nsel]
 
 
 class Q8State:
@@ -581,7 +587,7 @@ class Q8State:
         self.out = torch.zeros(B, Hq, d, dtype=torch.float32, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.bounds = torch.zeros(B, Hkv, n, 2, d, dtype=tdt, device=device) if want_bounds else None
-        self.blocks = None
+        self._blocks = {}
         if workspace is None:
             workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
         self.workspace = workspace
@@ -597,8 +603,7 @@ class Q8State:
         if nsel:
             if self.bounds is None:
                 raise RuntimeError("made without want_bounds")
-            if self.blocks is None or self.blocks.shape[2] != nsel:
-                self.blocks = torch.empty(self.B, self.Hkv, nsel, dtype=torch.int32, device=self.lens.device)
+            self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.lens.device)
             corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, self.workspace, stream=stream)
         corm_q8_attend(self.desc, self.code, q, self.K_codes, self.V_codes, self.k_scale, self.v_scale, self.K_tail, self.V_tail,
                        self.lens, self.out, self.workspace, blocks=self.blocks if nsel else None, nsel=nsel, status=self.status,

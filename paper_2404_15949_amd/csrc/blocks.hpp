@@ -180,30 +180,46 @@ struct BlockAttendArgs {
   const int32_t* lens;
   const int32_t* blocks;
   float* partials;
+  float* out;
   int32_t* status;
-  int32_t Lcap, nsel, part_blocks, npart;
+  int32_t Lcap, nsel, part_blocks;
+  int32_t npart;   // partials per head; with one the workgroup writes out itself
   float scale_log2;
 };
 
 constexpr int LIST_PART = 8;   // listed blocks per workgroup, at most
 
-// The workgroup's part of the list: sh_first = first slot of each block, L where there is none.  Returns the unit's length L.  Ends with a barrier.
-__device__ __forceinline__ int listed_blocks(const BlockAttendArgs& a, int unit, int* sh_first) {
-  const int tid = threadIdx.x, at = blockIdx.x * a.part_blocks + tid;
+// The workgroup's part of the list: sh_first = first slot of each block, L where there is none.  Returns the unit's length L, and how many places
+// of the part are to be looked at (up to its last block).  Ends with a barrier.
+__device__ __forceinline__ int2 listed_blocks(const BlockAttendArgs& a, int unit, int* sh_first) {
+  const int lane = threadIdx.x & 63, at = blockIdx.x * a.part_blocks + lane;
   int L = a.lens[unit], flags = 0;
   if (L < 0 || L > a.Lcap) {
     flags = CORM_DEV_BAD_LENS;
     L = L < 0 ? 0 : a.Lcap;
   }
-  if (tid < LIST_PART) {
-    const int id = tid < a.part_blocks && at < a.nsel ? a.blocks[(size_t)unit * a.nsel + at] : -1;
-    const bool ok = id >= 0 && id < (L + QBLK - 1) / QBLK;
-    if (!ok && id != -1) flags |= CORM_DEV_BAD_BLOCK;
-    sh_first[tid] = ok ? id * QBLK : L;
+  const int id = lane < a.part_blocks && at < a.nsel ? a.blocks[(size_t)unit * a.nsel + at] : -1;   // (every wave asks, for the count)
+  const bool ok = id >= 0 && id < (L + QBLK - 1) / QBLK;
+  if (!ok && id != -1) flags |= CORM_DEV_BAD_BLOCK;
+  const unsigned long long mask = __ballot(ok);
+  if (threadIdx.x < LIST_PART) {
+    sh_first[lane] = ok ? id * QBLK : L;
     if (flags && a.status) atomicOr(a.status, flags);
   }
   __syncthreads();
-  return L;
+  return make_int2(L, mask ? 64 - __clzll((long long)mask) : 0);
+}
+
+// A part without blocks: nothing to add.
+template <int D, int G>
+__device__ __forceinline__ void empty_partial(const BlockAttendArgs& a, int unit) {
+  if (a.npart == 1) {
+    for (int i = threadIdx.x; i < G * D; i += WG) a.out[(size_t)unit * G * D + i] = 0.f;
+  } else if (threadIdx.x < G) {   // (the merge takes no sums of a partial with this maximum)
+    float* part = partial_of(a.partials, unit * G + threadIdx.x, a.npart, blockIdx.x, D);
+    part[0] = neg_inf();
+    part[1] = 0.f;
+  }
 }
 
 // The waves' sums, folded into the workgroup's partial.
@@ -222,6 +238,10 @@ __device__ __forceinline__ void block_partial(const BlockAttendArgs& a, int unit
       const float f = fast_exp2(sh_m[g][i] - ms);
       zt = fmaf(sh_z[g][i], f, zt);
       at = fmaf(sh_acc[g][i][c], f, at);
+    }
+    if (a.npart == 1) {
+      a.out[(size_t)(unit * G + g) * D + c] = zt > 0.f ? at / zt : 0.f;
+      continue;
     }
     float* part = partial_of(a.partials, unit * G + g, a.npart, blockIdx.x, D);
     part[2 + c] = at;
@@ -245,8 +265,9 @@ __global__ __launch_bounds__(WG) void corm_block_attend_kernel(const BlockAttend
   __shared__ int sh_first[LIST_PART];
   const int unit = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
   const int sub = lane / LPR, cl = lane % LPR;
-  const int L = listed_blocks(a, unit, sh_first);
-  const int count = min(a.part_blocks, a.nsel - (int)blockIdx.x * a.part_blocks);
+  const int2 listed = listed_blocks(a, unit, sh_first);
+  const int L = listed.x, count = listed.y;
+  if (count == 0) return empty_partial<D, G>(a, unit);
 
   uint4 qreg[G];
 #pragma unroll
@@ -291,7 +312,7 @@ __global__ __launch_bounds__(WG) void corm_block_attend_kernel(const BlockAttend
     load(s1, 2 * i + 1);
     compute(s0, 2 * i);
     if (i + 1 < PAIRS) load(s0, 2 * i + 2);
-    compute(s1, 2 * i + 1);
+    if ((2 * i + 1) * A::STAGE_ROWS < count * QBLK) compute(s1, 2 * i + 1);
   }
 
 #pragma unroll
@@ -332,8 +353,9 @@ void corm_block_attend_gqa_kernel(const BlockAttendArgs a) {
     qb[kb] = make_uint4(0u, 0u, 0u, 0u);
     if (n < G) qb[kb] = *reinterpret_cast<const uint4*>(a.q + ((size_t)unit * G + n) * ROWB + (size_t)(64 * kb + 16 * lg));
   }
-  const int L = listed_blocks(a, unit, sh_first);
-  const int count = min(a.part_blocks, a.nsel - (int)blockIdx.x * a.part_blocks);
+  const int2 listed = listed_blocks(a, unit, sh_first);
+  const int L = listed.x, count = listed.y;
+  if (count == 0) return empty_partial<D, G>(a, unit);
   const __amdgpu_buffer_rsrc_t rk = make_rsrc(a.K + (size_t)unit * a.Lcap * ROWB, (uint32_t)L * ROWB);
   const __amdgpu_buffer_rsrc_t rv = make_rsrc(a.V + (size_t)unit * a.Lcap * ROWB, (uint32_t)L * ROWB);
   float m_run = neg_inf(), z_run = 0.f, acc[G][EPL];
@@ -357,7 +379,7 @@ void corm_block_attend_gqa_kernel(const BlockAttendArgs a) {
     load(s1, i + 1);
     compute(s0, i);
     if (i + 2 < LIST_PART) load(s0, i + 2);
-    compute(s1, i + 1);
+    if (i + 1 < count) compute(s1, i + 1);
   }
   z_run += __shfl_xor(z_run, 16);
   z_run += __shfl_xor(z_run, 32);

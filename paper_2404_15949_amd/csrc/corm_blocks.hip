@@ -43,7 +43,7 @@ EvictSplits evict_splits(const corm_desc* d) {
   e.slots = std::max(EVW_SPLIT, ((d->Lcap + 63) / 64 + EVW_WG - 1) / EVW_WG * EVW_WG);
   e.splits = (d->Lcap + e.slots - 1) / e.slots;
   if (units * e.splits > EVW_MOST_SPLITS) return EvictSplits{};
-  e.listed_off = align_up(units * e.splits * (sizeof(uint32_t) << EVW_BITS), 256);
+  e.listed_off = align_up(units * e.splits * EVW_COUNTS * sizeof(uint32_t), 256);
   e.counts_off = e.listed_off + align_up(units * d->Lcap * sizeof(uint32_t), 256);
   e.digit_off = e.counts_off + align_up(units * e.splits * sizeof(uint32_t), 256);
   e.total = e.digit_off + align_up(units * sizeof(uint2), 256);
@@ -181,7 +181,7 @@ int corm_q8_attend(const corm_desc* desc, int32_t code_dtype, const void* q, con
   }
   a.units = (int)units;
   const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
-  if (groups > 2147483647L) return CORM_EUNSUPPORTED;
+  if (groups * WG > 4294967295L) return CORM_EUNSUPPORTED;   // (threads of a launch)
   hipStream_t s = (hipStream_t)stream;
   rc = by_types(desc, code_dtype, [&](auto c, auto dt, auto dd) {
     hipLaunchKernelGGL((corm_q8_attend_kernel<decltype(c), decltype(dt), decltype(dd)::value>), dim3((unsigned)groups), dim3(WG), 0, s, a);
@@ -242,15 +242,18 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
   if (rc) return rc;
   BlockAttendArgs a;
   a.q = reinterpret_cast<const char*>(q); a.K = reinterpret_cast<const char*>(K); a.V = reinterpret_cast<const char*>(V);
-  a.lens = lens; a.blocks = blocks; a.partials = reinterpret_cast<float*>(workspace); a.status = status;
+  a.lens = lens; a.blocks = blocks; a.partials = reinterpret_cast<float*>(workspace); a.out = out; a.status = status;
   a.Lcap = desc->Lcap; a.nsel = nsel; a.scale_log2 = scale_log2(desc);
   const long units = (long)desc->B * desc->Hkv;
-  const int room = max_parts(desc);
+  // The longest parts of up to 8 blocks that leave two workgroups for each compute unit, four where rows are 512 bytes (a list holds at most the
+  // unit's blocks in earnest).  Whole steps, us, two | four | eight workgroups: bf16 128 units x 64 blocks 69.8 | 69.7 | 71.7, 64 x 64 of eight heads
+  // 47.6 | 50.8 | 57.2, 288 units of up to 4 blocks in a list of 65 27.7 | 37.6 | 53.5; fp32 64 x 32 42.7 | 39.1 | 39.2.
+  const int room = max_parts(desc), real = std::min(nsel, blocks_of(desc));
+  const long wgs = (row_bytes(desc) > 256 ? 4L : 2L) * device_cus();
+  auto parts_of = [&](int n) { return (n + a.part_blocks - 1) / a.part_blocks; };
   a.part_blocks = 1;
-  while (a.part_blocks < LIST_PART &&
-         (units * ((nsel + a.part_blocks - 1) / a.part_blocks) > 4L * device_cus() || (nsel + a.part_blocks - 1) / a.part_blocks > room))
-    a.part_blocks *= 2;
-  const int parts = (nsel + a.part_blocks - 1) / a.part_blocks;
+  while (a.part_blocks < LIST_PART && (units * parts_of(real) > wgs || parts_of(nsel) > room)) a.part_blocks *= 2;
+  const int parts = parts_of(nsel);
   a.npart = parts;
   hipStream_t s = (hipStream_t)stream;
   const dim3 grid(parts, (unsigned)units);
@@ -268,7 +271,7 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
       return launch_status();
     });
   });
-  if (rc) return rc;
+  if (rc || parts == 1) return rc;
   return merge_parts(desc, a.partials, lens, out, parts, 0, s);
 }
 

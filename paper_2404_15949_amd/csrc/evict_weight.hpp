@@ -10,6 +10,20 @@ namespace {
 constexpr int EVW_WG = 1024, EVW_BITS = 11;
 constexpr int EVW_KEYS = 16384;       // keys a workgroup holds in LDS (64 KB)
 
+// f(i, key of w[i]) for the thread's i in [first, end); several loads in flight, as nothing in f has to be done first.
+template <typename F>
+__device__ __forceinline__ void for_keys(const float* w, int first, int end, const F& f) {
+  constexpr int N = 4;
+  for (int i0 = first + threadIdx.x; i0 < end; i0 += N * EVW_WG) {
+    float x[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) x[j] = w[min(i0 + j * EVW_WG, end - 1)];
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+      if (i0 + j * EVW_WG < end) f(i0 + j * EVW_WG, order_key(x[j]));
+  }
+}
+
 // Grid (units).
 __global__ __launch_bounds__(EVW_WG) void corm_evict_weight_kernel(const float* weight, const int32_t* lens, uint8_t* keep, int Lcap,
                                                                    int r, int budget, int held) {
@@ -31,8 +45,7 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_weight_kernel(const float* 
     return true;
   };
   if (k > 0) {
-    if (held)
-      for (int i = tid; i < open; i += EVW_WG) sh_key[i] = order_key(w[i]);   // (a thread asks for its own)
+    if (held) for_keys(w, 0, open, [&](int i, uint32_t x) { sh_key[i] = x; });   // (a thread asks for its own)
     cut = find_cut<EVW_WG, EVW_BITS, 32>(open, (uint32_t)k, item, sh);
   }
   for (int i = tid; i < L; i += EVW_WG) {
@@ -43,7 +56,8 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_weight_kernel(const float* 
 }
 
 // Few long units: three launches, of which the first two share a unit among workgroups ("splits" of split_slots slots).
-//   count    the top 11 bits of a split's keys
+//   count    the top 11 bits of a split's keys, and the top 6 of those (so that the next launch reads a few kilobytes of a unit's counts and not
+//            8 for every split: the dies' caches do not see each other's, and 16 units of 131072 slots took 12 us there)
 //   part     which of these digits the cut lies in; slots with a larger or a smaller one are decided, the others (as a rule a few percent)
 //            are listed
 //   settle   a workgroup a unit: the cut among the listed ones
@@ -52,13 +66,14 @@ struct EvictLongArgs {
   const float* weight;
   const int32_t* lens;
   uint8_t* keep;
-  uint32_t* hist;      // [units, splits, 2048]
+  uint32_t* hist;      // [units, splits, 64 + 2048]: coarse counts, then fine ones
   uint32_t* listed;    // [units, Lcap]: slots, a split's from its first slot on
   uint32_t* counts;    // [units, splits]
   uint2* digit;        // [units]: the digit of the cut, keys needed of it
   int32_t Lcap, r, budget, splits, split_slots;
 };
 constexpr int SETTLE_KEYS = 8192;
+constexpr int EVW_COARSE = 64, EVW_FINE = (1 << EVW_BITS) / EVW_COARSE, EVW_COUNTS = EVW_COARSE + (1 << EVW_BITS);   // counts of a split
 constexpr int EVW_SPLIT = 8192, EVW_MOST_SPLITS = 2048;   // slots of a split, at least (64 splits at most); splits of all units
 
 __global__ __launch_bounds__(EVW_WG) void corm_evict_count_kernel(const EvictLongArgs a) {
@@ -70,14 +85,21 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_count_kernel(const EvictLon
   const int first = split * a.split_slots, end = min(first + a.split_slots, L - a.r);
   for (int i = tid; i < (1 << EVW_BITS); i += EVW_WG) sh_hist[i] = 0u;
   __syncthreads();
-  for (int i = first + tid; i < end; i += EVW_WG) atomicAdd(&sh_hist[order_key(w[i]) >> (32 - EVW_BITS)], 1u);
+  for_keys(w, first, end, [&](int, uint32_t x) { atomicAdd(&sh_hist[x >> (32 - EVW_BITS)], 1u); });
   __syncthreads();
-  uint32_t* to = a.hist + ((size_t)unit * a.splits + split) * (1 << EVW_BITS);
-  for (int i = tid; i < (1 << EVW_BITS); i += EVW_WG) to[i] = sh_hist[i];
+  uint32_t* to = a.hist + ((size_t)unit * a.splits + split) * EVW_COUNTS;
+  for (int i = tid; i < (1 << EVW_BITS); i += EVW_WG) {   // EVW_FINE neighbouring lanes have a coarse digit
+    const uint32_t c = sh_hist[i];
+    to[EVW_COARSE + i] = c;
+    uint32_t sum = c;
+#pragma unroll
+    for (int o = 1; o < EVW_FINE; o <<= 1) sum += __shfl_xor(sum, o);
+    if (i % EVW_FINE == 0) to[i / EVW_FINE] = sum;
+  }
 }
 
 __global__ __launch_bounds__(EVW_WG) void corm_evict_part_kernel(const EvictLongArgs a) {
-  __shared__ uint32_t sh_hist[1 << EVW_BITS], sh_pick[3], sh_n;
+  __shared__ uint32_t sh_hist[EVW_COARSE], sh_pick[3], sh_n;
   const int unit = blockIdx.y, split = blockIdx.x, tid = threadIdx.x;
   const int L = min(max(a.lens[unit], 0), a.Lcap);
   const int first = split * a.split_slots, end = min(first + a.split_slots, L), open = L - a.r, k = a.budget - a.r;
@@ -88,27 +110,39 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_part_kernel(const EvictLong
     return;
   }
   const float* w = a.weight + (size_t)unit * a.Lcap;
-  const uint32_t* hist = a.hist + (size_t)unit * a.splits * (1 << EVW_BITS);
-  for (int i = tid; i < (1 << EVW_BITS); i += EVW_WG) {
-    uint32_t sum = 0u;
-#pragma unroll 16
-    for (int s = 0; s < a.splits; ++s) sum += hist[(size_t)s * (1 << EVW_BITS) + i];
-    sh_hist[i] = sum;
-  }
+  const uint32_t* hist = a.hist + (size_t)unit * a.splits * EVW_COUNTS;
+  // the coarse digit of the cut, then the fine one in it; 64 counts of every split at a time (fine ones: half of them none)
+  uint32_t need = (uint32_t)k, digit = 0u;
   if (tid == 0) sh_n = 0u;
-  __syncthreads();
-  find_digit<EVW_WG, EVW_BITS>(sh_hist, sh_pick, (uint32_t)k);
-  const uint32_t digit = sh_pick[0];
+#pragma unroll
+  for (int round = 0; round < 2; ++round) {
+    if (tid < EVW_COARSE) sh_hist[tid] = 0u;
+    __syncthreads();
+    const int c = tid % EVW_COARSE;
+    uint32_t sum = 0u;
+    if (round == 0 || c < EVW_FINE) {
+      const int at = round == 0 ? c : EVW_COARSE + (int)digit * EVW_FINE + c;
+#pragma unroll
+      for (int s = tid / EVW_COARSE; s < 64; s += EVW_WG / EVW_COARSE)
+        if (s < a.splits) sum += hist[(size_t)s * EVW_COUNTS + at];
+    }
+    if (sum) atomicAdd(&sh_hist[c], sum);
+    __syncthreads();
+    find_digit<EVW_WG, 6>(sh_hist, sh_pick, need);
+    digit = digit * EVW_FINE + sh_pick[0];
+    need = sh_pick[1];
+    __syncthreads();
+  }
   uint32_t* list = a.listed + (size_t)unit * a.Lcap + first;
-  for (int i = first + tid; i < end; i += EVW_WG) {
-    const uint32_t x = i < open ? order_key(w[i]) >> (32 - EVW_BITS) : digit + 1u;
+  for_keys(w, first, end, [&](int i, uint32_t x) {
+    x = i < open ? x >> (32 - EVW_BITS) : digit + 1u;
     if (x == digit) list[atomicAdd(&sh_n, 1u)] = (uint32_t)i;
     else to[i] = x > digit;
-  }
+  });
   __syncthreads();
   if (tid == 0) {
     a.counts[(size_t)unit * a.splits + split] = sh_n;
-    if (split == 0) a.digit[unit] = make_uint2(digit, sh_pick[1]);
+    if (split == 0) a.digit[unit] = make_uint2(digit, need);
   }
 }
 

@@ -279,7 +279,15 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
     count = sh_n;
   } else {
     count = min(a.part_blocks, full - first);
-    if (count <= 0 && !has_tail) return;
+    if (count <= 0 && !has_tail) return;   // (a partial that the merge does not ask for)
+  }
+  if (count <= 0 && !times && a.npart > 1) {   // nothing to add (the merge takes no sums of a partial with this maximum)
+    if (threadIdx.x < G) {
+      float* to = partial_of(a.partials, head0 + threadIdx.x, a.npart, part, D);
+      to[0] = neg_inf();
+      to[1] = 0.f;
+    }
+    return;
   }
 
   constexpr uint32_t BLKB = QBLK * D;   // bytes of a block's codes
@@ -459,7 +467,7 @@ __global__ __launch_bounds__(MERGE_WG) void corm_parts_merge_kernel(const float*
       v[u] = p[2 + c];
     }
 #pragma unroll
-    for (int u = 0; u < MERGE_BATCH; ++u) sum = fmaf(s0 + u * GROUPS < n ? v[u] : 0.f, fast_exp2(m[u] - ms), sum);
+    for (int u = 0; u < MERGE_BATCH; ++u) sum = fmaf(s0 + u * GROUPS < n && m[u] > neg_inf() ? v[u] : 0.f, fast_exp2(m[u] - ms), sum);
   }
   sh[grp][c] = sum;
   __syncthreads();

@@ -35,7 +35,7 @@ __device__ __forceinline__ uint32_t wave_prefix_sum(uint32_t x) {
 // needed, how many it has).  By NT threads; sh_pick is ready behind the barrier at the end.
 template <int NT, int BITS>
 __device__ __forceinline__ void find_digit(const uint32_t* sh_hist, uint32_t* sh_pick, uint32_t need) {
-  constexpr int BINS = 1 << BITS, W = BINS / 4 < NT ? BINS / 4 : NT, PER = BINS / W;   // threads with digits, digits of a thread
+  constexpr int BINS = 1 << BITS, W = BINS <= 256 ? 64 : BINS / 4 < NT ? BINS / 4 : NT, PER = BINS / W;   // threads with digits, digits of a thread
   __shared__ uint32_t sh_sum[W / 64];
   const int t = threadIdx.x;
   uint32_t c[PER], sum = 0u, before = 0u;

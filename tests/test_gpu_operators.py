@@ -71,6 +71,9 @@ class Q8:
                     assert torch.equal(Kc[b, h, i].permute(1, 0, 2).reshape(64, self.d), c.codes[0][i]), where
                     assert torch.equal(Vc[b, h, i].t(), c.codes[1][i]), where
                     assert float(ks[b, h, i]) == float(c.scales[0][i]) and float(vs[b, h, i]) == float(c.scales[1][i]), where
+                full = len(c.codes[0])                    # blocks that are not full are left as they were
+                assert bool((self.Kc.view(torch.int8)[b, h, full:] == 0x7F).all()) and bool((self.Vc.view(torch.int8)[b, h, full:] == 0x7F).all()), where
+                assert bool(ks[b, h, full:].isnan().all()) and bool(vs[b, h, full:].isnan().all()), where
                 m = c.n % 64
                 if m:
                     assert torch.equal(Kt[b, h, :m], torch.stack(c.tail[0])) and torch.equal(Vt[b, h, :m], torch.stack(c.tail[1])), where
@@ -106,7 +109,7 @@ def test_q8_append_in_pieces(dtype, d, code):
     g = _gen(1)
     c = Q8(3, 2, 2, d, 64 * 6 + 17, dtype, code, bounds=True)
     for n, n_new in ((1, None), (62, None), (1, [1, 0, 1]), (1, None), (64, [64, 63, 1]), (65, [65, 0, 64]), (130, [3, 130, 129]), (1, None),
-                     (63, [63, 62, 0])):
+                     (63, [63, 62, 0]), (5, [-3, 99, 2])):
         c.append(_rows(g, dtype, 3, 2, n, d), _rows(g, dtype, 3, 2, n, d, scale=30.0), n_new)
         c.check_state()
     assert int(c.status) == 0
@@ -313,6 +316,23 @@ def test_attend_weigh(B, Hq, Hkv, d, cap, dtype, path):
     assert int(status) == 0
 
 
+def test_weigh_with_accounts_at_odd_addresses():
+    """Accounts whose rows begin at no multiple of 16 bytes: the bits of the aligned ones."""
+    g, B, Hq, Hkv, d, cap = _gen(4), 2, 4, 2, 64, 900
+    lens = torch.tensor([[900, 77], [4, 899]], dtype=torch.int32)
+    K, V, q = (x.to(DEV) for x in _state(g, B, Hq, Hkv, d, cap, "f32", lens))
+    desc = corm.make_desc(B, Hq, Hkv, d, cap, cap, 1, 1, "f32")
+    ws = torch.empty(corm.corm_workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    w0 = torch.rand(B, Hkv, cap, generator=g).to(DEV)
+    out, want = torch.empty(B, Hq, d, device=DEV), torch.zeros_like(w0)
+    corm.corm_decode_attend_weigh(desc, q, K, V, lens.to(DEV), w0, want, out, ws)
+    for off in (1, 2, 3):
+        a, b = (torch.zeros(w0.numel() + 4, device=DEV)[off:off + w0.numel()].view_as(w0) for _ in range(2))
+        a.copy_(w0)
+        corm.corm_decode_attend_weigh(desc, q, K, V, lens.to(DEV), a, b, out, ws)
+        assert torch.equal(b, want)
+
+
 @pytest.mark.parametrize("units,cap,r,budget", [(3, 50, 1, 1), (4, 700, 16, 200), (2, 1024, 1, 1023), (5, 1500, 100, 100), (13, 4100, 64, 1000),
                                                 (1, 9000, 3, 5000), (2, 16384, 10, 3000), (2, 16385, 50, 50), (2, 40000, 500, 2000), (3, 30001, 7, 9000),
                                                 (1, 200000, 5, 70000)])
@@ -338,7 +358,7 @@ def test_evict_mask_weight(units, cap, r, budget):
 # ---------------------------------------------------------------- together, as they would be used
 
 def _layer(B, Hq, Hkv, d, cap, dtype, P, g, r=8):
-    st = corm.LayerState(B, Hq, Hkv, d, cap, cap, 4, r, dtype, device=DEV, want_ring=False)
+    st = corm.LayerState(B, Hq, Hkv, d, cap, cap, 4, r, dtype, device=DEV, want_ring=False, want_bounds=True, want_weight=True)
     K, V = _rows(g, dtype, B, Hkv, P, d), _rows(g, dtype, B, Hkv, P, d)
     st.preload(K.to(DEV), V.to(DEV))
     return st, K, V
@@ -356,7 +376,7 @@ def test_weigh_steps_evict_and_go_on():
         q, k, v = _rows(g, "f32", B, Hq, d, scale=2.0), _rows(g, "f32", B, Hkv, d), _rows(g, "f32", B, Hkv, d)
         t = torch.full((B,), P + 1 + s, dtype=torch.int32, device=DEV)
         cut = s % 3 == 2
-        before = torch.zeros(B, Hkv, 160) if s == 0 else st.weight.cpu().clone()
+        before = st.weight.cpu().clone()
         lens0 = st.lens.cpu().clone()
         st.step_weigh(q.to(DEV), k.to(DEV), v.to(DEV), t, budget if cut else None)
         out, acc, lens, pos, Kd, Vd = (x.cpu() for x in (st.out, st.weight, st.lens, st.pos, st.K, st.V))
@@ -372,7 +392,7 @@ def test_weigh_steps_evict_and_go_on():
             e = ref.weight_error(x, Kr, sm) + (L0 + 9) * ref.EPS
             total = torch.cat([before[b, h, :L0], torch.zeros(1)]).double() + p.sum(0)
             if cut and L0 + 1 > budget:
-                keep = st.keep[b, h, :L0 + 1].cpu().bool()
+                keep = st.weight_keep[b, h, :L0 + 1].cpu().bool()
                 idx = keep.nonzero().flatten().tolist()
                 assert len(idx) == budget and all(i in idx for i in range(L0 + 1 - r, L0 + 1))
                 # no key that went had clearly more than one that stayed (accounts are within e of the plain ones)
@@ -387,14 +407,16 @@ def test_weigh_steps_evict_and_go_on():
             assert torch.equal(Kd[b, h, :L], torch.stack(ks)) and torch.equal(Vd[b, h, :L], torch.stack(vs))
             assert bool(((acc[b, h, :L].double() - total).abs() <= p.sum(0) * e + (G + 1) * ref.EPS * total).all())
     assert evicted > 0 and int(st.status) == 0
+    bare = corm.LayerState(1, 1, 1, 64, 64, 64, 4, 4, "f32", device=DEV, want_ring=False)
+    for step in (lambda: bare.step_weigh(None, None, None, None), lambda: bare.step_blocks(None, None, None, None, 1), bare.renew_bounds):
+        with pytest.raises(RuntimeError):
+            step()
 
 
 def test_block_steps_follow_the_chosen_blocks():
     g, B, Hq, Hkv, d, P, nsel, nlast = _gen(12), 2, 8, 2, 128, 64 * 9 - 3, 4, 2
     st, K, V = _layer(B, Hq, Hkv, d, 64 * 11, "bf16", P, g)
     sm, G = 1.0 / math.sqrt(d), Hq // Hkv
-    with pytest.raises(RuntimeError):
-        st.step_blocks(None, None, None, None, nsel)
     st.renew_bounds()
     for s in range(8):
         q, k, v = _rows(g, "bf16", B, Hq, d, scale=2.0), _rows(g, "bf16", B, Hkv, d), _rows(g, "bf16", B, Hkv, d)
@@ -524,3 +546,49 @@ def test_tensors_that_do_not_fit_the_call_are_refused():
                       ("blocks", blocks[:, :, :1])):
         with pytest.raises(ValueError):
             corm.corm_block_attend(desc, **{**good, name: bad})
+
+
+def test_units_beyond_four_gigabytes():
+    """Forty units of a million slots: the last one lies 5 GB (codes) and 10 GB (rows) into its array, its keys at the end of a unit."""
+    g, units, cap, d, G = _gen(15), 40, 1 << 20, 128, 2
+    desc = corm.make_desc(units, G, 1, d, cap, cap, 1, 1, "bf16")
+    n, u, sm = cap // 64, units - 1, 1.0 / math.sqrt(d)
+    lens = torch.zeros(units, 1, dtype=torch.int32, device=DEV)
+    lens[u] = cap - 3
+    last = [n - 1, n - 2, 5]
+    k, v, q = _rows(g, "bf16", 64 * 3, d), _rows(g, "bf16", 64 * 3, d), _rows(g, "bf16", units, G, d)
+    ws, out = _ws(desc), torch.full((units, G, d), float("nan"), device=DEV)
+    blocks = torch.full((units, 1, 4), -1, dtype=torch.int32, device=DEV)
+    blocks[u, 0, :3] = torch.tensor(last, dtype=torch.int32)
+    K = torch.empty(units, 1, n, 64, d, dtype=torch.bfloat16, device=DEV)
+    V = torch.empty_like(K)
+    for i, blk in enumerate(last):
+        K[u, 0, blk], V[u, 0, blk] = k[64 * i:64 * i + 64].to(DEV), v[64 * i:64 * i + 64].to(DEV)
+    corm.corm_block_attend(desc, q.to(DEV), K, V, lens, blocks, 4, out, ws)
+    live = [i for i in range(192) if not 61 <= i < 64]          # (three slots of the last block are not in use)
+    x, Kr, Vr = q[u].double(), k[live].double(), v[live].double()
+    want, _ = ref.attention(x, Kr, Vr, sm)
+    assert float((out[u].cpu().double() - want).abs().max()) <= ref.out_error(x, Kr, Vr, sm) and not out[:u].any()
+    bounds = torch.empty(units, 1, n, 2, d, dtype=torch.bfloat16, device=DEV)
+    corm.corm_block_bounds(desc, K, lens, bounds, newest=1)
+    assert torch.equal(bounds[u, 0, n - 1].cpu().float(), ref.bounds_of(k[:61].float())[0])
+    del K, V, bounds
+    Kc = torch.empty(units, 1, n, 2, 64, 64, dtype=torch.int8, device=DEV)
+    Vc = torch.empty(units, 1, n, d, 64, dtype=torch.int8, device=DEV)
+    ks, vs = torch.zeros(units, 1, n, device=DEV), torch.zeros(units, 1, n, device=DEV)
+    Kt, Vt = torch.zeros(units, 1, 64, d, dtype=torch.bfloat16, device=DEV), torch.zeros(units, 1, 64, d, dtype=torch.bfloat16, device=DEV)
+    for i, blk in enumerate((n - 2, 5)):                        # the append that fills block n - 2, and block 5 by hand
+        lens[u] = blk * 64
+        rows = [torch.zeros(units, 1, 64, d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+        rows[0][u, 0], rows[1][u, 0] = k[64 * i:64 * i + 64].to(DEV), v[64 * i:64 * i + 64].to(DEV)
+        only = torch.zeros(units, dtype=torch.int32, device=DEV)
+        only[u] = 64
+        corm.corm_q8_append(desc, "i8", *rows, 64, only, Kc, Vc, ks, vs, Kt, Vt, lens, lens)
+    lens[u] = (n - 1) * 64
+    blocks[u, 0, :3] = torch.tensor([n - 2, 5, -1], dtype=torch.int32)
+    corm.corm_q8_attend(desc, "i8", q.to(DEV), Kc, Vc, ks, vs, Kt, Vt, lens, out, ws, blocks=blocks, nsel=4)
+    c = ref.Cache8(d, "i8")
+    for i in range(128):
+        c.append(k[i], v[i])
+    want, _ = ref.attention(x, c.rows(0), c.rows(1), sm)
+    assert float((out[u].cpu().double() - want).abs().max()) <= ref.out_error(x, c.rows(0), c.rows(1), sm) and not out[:u].any()
