@@ -48,6 +48,11 @@ struct Params {
   int32_t lazy;         // lazy mode: dead slots are skipped
 };
 
+// corm_decode_attend_weigh needs neither positions nor hits: there these two fields hold the keys' accounts [B,Hkv,Lcap], before the call and after.
+// (Fields of their own would change the kernel arguments, and with them the registers, of every other kernel.)
+__device__ __forceinline__ const float* accounts_in(const Params& p) { return reinterpret_cast<const float*>(p.pos); }
+__device__ __forceinline__ float* accounts_out(const Params& p) { return reinterpret_cast<float*>(p.last_hit); }
+
 // ---------------------------------------------------------------- small device helpers
 
 __device__ __forceinline__ float bf16_lo(uint32_t x) { return __uint_as_float(x << 16); }

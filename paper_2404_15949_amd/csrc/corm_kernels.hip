@@ -221,11 +221,13 @@ int corm_decode_attend_weigh(const corm_desc* desc, const void* q, const void* K
   rc = make_ctx(opts, &ctx);
   if (rc) return rc;
   Params p = {};
-  p.q = q; p.k_new = K; p.v_new = V;  // (as in corm_decode_attend; pos, last_hit and t are not read without an append and a ring)
+  p.q = q; p.k_new = K; p.v_new = V;  // (as in corm_decode_attend; t is not used without a ring)
   p.K = const_cast<void*>(K); p.V = const_cast<void*>(V);
   p.lens = const_cast<int32_t*>(lens); p.t = lens; p.t_first = lens; p.out = out; p.status = status;
+  p.pos = reinterpret_cast<int32_t*>(const_cast<float*>(weight_in)); p.last_hit = reinterpret_cast<int32_t*>(weight);   // (accounts_in, accounts_out)
+  ctx.weigh = true;
   bind_params(desc, wl, workspace, p);
-  return launch_attend_weigh(desc, p, ctx, weight_in, weight, (hipStream_t)stream);
+  return launch_attend_weigh(desc, p, ctx, (hipStream_t)stream);
 }
 
 int corm_evict_mask(const corm_desc* desc, const void* score_ring, const int32_t* lens, const int32_t* pos,

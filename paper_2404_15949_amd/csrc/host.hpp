@@ -45,6 +45,7 @@ struct LaunchCtx {
                                               // where the MFMA kernel applies
   hipEvent_t ev0 = nullptr, ev1 = nullptr;    // recorded around the launch that streams K and V
   int cus = 256;
+  bool weigh = false;                         // corm_decode_attend_weigh
 };
 
 int make_ctx(const corm_launch_opts* o, LaunchCtx* c) {
@@ -153,7 +154,7 @@ bool use_unit_path(const corm_desc* d, const LaunchCtx& c) {
   return d->B * d->Hkv >= c.cus;
 }
 
-template <typename DT, int D, bool LAZY>
+template <typename DT, int D, bool LAZY, bool WEIGH>
 int launch_unit_g(const Params& p, const LaunchCtx& c, int G, int units, size_t lds, int lstride, hipStream_t s) {
   // grouped queries: the small-stage instance (two workgroups per compute unit) once there are two units per
   // compute unit; measured on 32 query / 8 KV heads: 1024 units 161 -> 134 us per step, 512 units 139 -> 133 us,
@@ -161,28 +162,28 @@ int launch_unit_g(const Params& p, const LaunchCtx& c, int G, int units, size_t 
   const bool small = (long)p.B * p.Hkv >= 2L * c.cus;
   const dim3 grid(units), wg(UNIT_WG);
   switch (G) {
-    case 1: hipLaunchKernelGGL((corm_unit_kernel<DT, D, 1, LAZY, UNROLL>), grid, wg, lds, s, p, lstride); break;
+    case 1: hipLaunchKernelGGL((corm_unit_kernel<DT, D, 1, LAZY, UNROLL, WEIGH>), grid, wg, lds, s, p, lstride); break;
     case 2:
-      if (small) hipLaunchKernelGGL((corm_unit_kernel<DT, D, 2, LAZY, UNROLL / 2>), grid, wg, lds, s, p, lstride);
-      else hipLaunchKernelGGL((corm_unit_kernel<DT, D, 2, LAZY, UNROLL>), grid, wg, lds, s, p, lstride);
+      if (small) hipLaunchKernelGGL((corm_unit_kernel<DT, D, 2, LAZY, UNROLL / 2, WEIGH>), grid, wg, lds, s, p, lstride);
+      else hipLaunchKernelGGL((corm_unit_kernel<DT, D, 2, LAZY, UNROLL, WEIGH>), grid, wg, lds, s, p, lstride);
       break;
     case 4:
-      if (small) hipLaunchKernelGGL((corm_unit_kernel<DT, D, 4, LAZY, UNROLL / 4>), grid, wg, lds, s, p, lstride);
-      else hipLaunchKernelGGL((corm_unit_kernel<DT, D, 4, LAZY, UNROLL>), grid, wg, lds, s, p, lstride);
+      if (small) hipLaunchKernelGGL((corm_unit_kernel<DT, D, 4, LAZY, UNROLL / 4, WEIGH>), grid, wg, lds, s, p, lstride);
+      else hipLaunchKernelGGL((corm_unit_kernel<DT, D, 4, LAZY, UNROLL, WEIGH>), grid, wg, lds, s, p, lstride);
       break;
     default: return CORM_EUNSUPPORTED;
   }
   return launch_status();
 }
 
-template <bool LAZY>
+template <bool LAZY, bool WEIGH>
 int launch_unit_dt(const corm_desc* d, const Params& p, const LaunchCtx& c, int G, int units, size_t lds, int lstride,
                    hipStream_t s) {
   if (d->kv_dtype == CORM_F32)
-    return d->d == 64 ? launch_unit_g<F32, 64, LAZY>(p, c, G, units, lds, lstride, s)
-                      : launch_unit_g<F32, 128, LAZY>(p, c, G, units, lds, lstride, s);
-  return d->d == 64 ? launch_unit_g<BF16, 64, LAZY>(p, c, G, units, lds, lstride, s)
-                    : launch_unit_g<BF16, 128, LAZY>(p, c, G, units, lds, lstride, s);
+    return d->d == 64 ? launch_unit_g<F32, 64, LAZY, WEIGH>(p, c, G, units, lds, lstride, s)
+                      : launch_unit_g<F32, 128, LAZY, WEIGH>(p, c, G, units, lds, lstride, s);
+  return d->d == 64 ? launch_unit_g<BF16, 64, LAZY, WEIGH>(p, c, G, units, lds, lstride, s)
+                    : launch_unit_g<BF16, 128, LAZY, WEIGH>(p, c, G, units, lds, lstride, s);
 }
 
 int launch_unit(const corm_desc* d, const Params& p, const LaunchCtx& c, hipStream_t s) {
@@ -191,8 +192,9 @@ int launch_unit(const corm_desc* d, const Params& p, const LaunchCtx& c, hipStre
   const int G = d->Hq / d->Hkv;
   const int units = (d->B * d->Hkv + UNIT_XCDS - 1) / UNIT_XCDS * UNIT_XCDS;   // grid: whole rounds over the XCDs
   if (c.ev0 && hipEventRecord(c.ev0, s) != hipSuccess) return CORM_EHIP;
-  const int rc = p.lazy ? launch_unit_dt<true>(d, p, c, G, units, lds, lstride, s)
-                        : launch_unit_dt<false>(d, p, c, G, units, lds, lstride, s);
+  const int rc = c.weigh ? launch_unit_dt<false, true>(d, p, c, G, units, lds, lstride, s)
+                 : p.lazy ? launch_unit_dt<true, false>(d, p, c, G, units, lds, lstride, s)
+                          : launch_unit_dt<false, false>(d, p, c, G, units, lds, lstride, s);
   if (rc) return rc;
   if (c.ev1 && hipEventRecord(c.ev1, s) != hipSuccess) return CORM_EHIP;
   return CORM_OK;
@@ -277,31 +279,36 @@ int launch_attend_record(const corm_desc* d, const Params& p0, const LaunchCtx& 
   return launch_record(d, p, c, s);
 }
 
-// The split attend launch, and behind it the weights and out.
+// Behind the split attend launch: the weights and out.
 template <int ROUNDS>
-int launch_weigh(const corm_desc* d, const Params& p, const float* weight_in, float* weight, hipStream_t s) {
+int launch_weigh(const corm_desc* d, const Params& p, hipStream_t s) {
   const int G = d->Hq / d->Hkv;
   const int items = G * (d->d / 64);
   const int n_out = (d->Lcap + p.part_keys - 1) / p.part_keys <= OUT_WAVE_PARTS ? (items + WAVES - 1) / WAVES : items;
   const dim3 grid(d->B * d->Hkv, (d->Lcap + ROUNDS * WEIGH_KEYS - 1) / (ROUNDS * WEIGH_KEYS) + n_out), wg(WG);
   switch (G) {
-    case 1: hipLaunchKernelGGL((corm_weigh_kernel<1, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
-    case 2: hipLaunchKernelGGL((corm_weigh_kernel<2, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
-    case 4: hipLaunchKernelGGL((corm_weigh_kernel<4, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
-    case 8: hipLaunchKernelGGL((corm_weigh_kernel<8, ROUNDS>), grid, wg, 0, s, p, weight_in, weight, d->d, n_out); break;
+    case 1: hipLaunchKernelGGL((corm_weigh_kernel<1, ROUNDS>), grid, wg, 0, s, p, d->d, n_out); break;
+    case 2: hipLaunchKernelGGL((corm_weigh_kernel<2, ROUNDS>), grid, wg, 0, s, p, d->d, n_out); break;
+    case 4: hipLaunchKernelGGL((corm_weigh_kernel<4, ROUNDS>), grid, wg, 0, s, p, d->d, n_out); break;
+    case 8: hipLaunchKernelGGL((corm_weigh_kernel<8, ROUNDS>), grid, wg, 0, s, p, d->d, n_out); break;
     default: return CORM_EUNSUPPORTED;
   }
   return launch_status();
 }
 
-int launch_attend_weigh(const corm_desc* d, const Params& p0, const LaunchCtx& c, const float* weight_in, float* weight, hipStream_t s) {
+// attend + account: one launch, a workgroup a unit, where corm_decode_attend takes it and a unit has more than a chunk or two; else two launches.
+// One launch | two, us: 512 units x 4352 keys of one head 179 | 194, 1280 x 550 67 | 82, 1280 x 390 50 | 49, 1280 x 200 36 | 30; fp32 256 units x
+// 5000 of two heads 106 | 118; four heads 512 x 1500 81 | 85, 640 x 850 65 | 61, 640 x 390 40 | 35.
+int launch_attend_weigh(const corm_desc* d, const Params& p0, const LaunchCtx& c, hipStream_t s) {
+  const bool long_units = d->Lcap > (d->Hq / d->Hkv < 4 ? CHUNK : 2 * CHUNK);
+  if (use_unit_path(d, c) && (long_units || c.path == 2)) return launch_unit(d, p0, c, s);
   Params p = p0;
   p.part_keys = attend_part_keys(d, c);
   p.head_groups = attend_head_groups(d, c, p.part_keys);
   const int rc = launch_attend(d, p, c, s);
   if (rc) return rc;
   const long two = (long)d->B * d->Hkv * ((d->Lcap + 2 * WEIGH_KEYS - 1) / (2 * WEIGH_KEYS));
-  return two >= 4L * c.cus ? launch_weigh<2>(d, p, weight_in, weight, s) : launch_weigh<1>(d, p, weight_in, weight, s);
+  return two >= 4L * c.cus ? launch_weigh<2>(d, p, s) : launch_weigh<1>(d, p, s);
 }
 
 // A whole step in one launch (small.hpp)?  A unit is then one workgroup's alone, so only while its rows are few.  Whole steps in a

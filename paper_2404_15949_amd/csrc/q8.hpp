@@ -232,8 +232,9 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   const int head0 = unit * G;   // b * Hq + hkv * G
   const int lane = threadIdx.x & 63, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int n = lane & 15, lg = lane >> 4;
+  const bool has_tail = part == a.npart - 1, has_blocks = !has_tail || a.npart == 1;
   QueryOperand<DT, D> qo;
-  qo.load(reinterpret_cast<const char*>(a.q) + (size_t)head0 * D * DT::ESZ, n, lg, G);
+  if (has_blocks) qo.load(reinterpret_cast<const char*>(a.q) + (size_t)head0 * D * DT::ESZ, n, lg, G);
   int L = a.lens[unit];
   if (L < 0 || L > a.Lcap) {
     if (part == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, CORM_DEV_BAD_LENS);
@@ -241,7 +242,6 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   }
   const int full = L / QBLK, rest = L % QBLK;
   const int32_t* list = a.blocks ? a.blocks + (size_t)unit * a.nsel : nullptr;
-  const bool has_tail = part == a.npart - 1;
   int times = has_tail && rest > 0 ? 1 : 0;   // the tail counts as often as it is listed
   if (list && has_tail) {
     if (threadIdx.x == 0) sh_times = 0;
@@ -261,8 +261,9 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
 
   // this workgroup's blocks
   const int first = part * a.part_blocks;
-  int count;
-  if (list) {
+  int count = 0;
+  if (!has_blocks) {
+  } else if (list) {
     if (wv == 0) {
       int n = 0;
       for (int i0 = 0; i0 < a.part_blocks; i0 += 64) {
@@ -279,7 +280,7 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
     count = sh_n;
   } else {
     count = min(a.part_blocks, full - first);
-    if (count <= 0 && !has_tail) return;   // (a partial that the merge does not ask for)
+    if (count <= 0 && a.npart > 1) return;   // (a partial that the merge does not ask for)
   }
   if (count <= 0 && !times && a.npart > 1) {   // nothing to add (the merge takes no sums of a partial with this maximum)
     if (threadIdx.x < G) {
@@ -387,8 +388,9 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   }
 
   // the waves meet, and the tail
+  const int from = count > 0 ? 0 : WAVES;
   z_run = rows_allreduce_sum(z_run);
-  if (n < G) {
+  if (n < G && count > 0) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4_t*>(&sh_acc[wv][n][16 * c + 4 * lg]) = acc[c];
     if (lg == 0) {   // (sum and products are 2^15 times those of the maximum)
@@ -405,14 +407,22 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   __syncthreads();
   for (int idx = threadIdx.x; idx < G * D; idx += WG) {
     const int g = idx / D, c = idx - g * D;
-    float mx = neg_inf();
-    for (int i = 0; i < sets; ++i) mx = fmaxf(mx, sh_m[i][g]);
+    float m[2 * WAVES], z[2 * WAVES], x[2 * WAVES], mx = neg_inf();
+#pragma unroll
+    for (int i = 0; i < 2 * WAVES; ++i) {   // (all at once: one latency)
+      const bool in = i >= from && i < sets;
+      m[i] = in ? sh_m[i][g] : neg_inf();
+      z[i] = in ? sh_z[i][g] : 0.f;
+      x[i] = in ? sh_acc[i][g][c] : 0.f;
+      mx = fmaxf(mx, m[i]);
+    }
     const float ms = mx == neg_inf() ? 0.f : mx;
     float zt = 0.f, at = 0.f;
-    for (int i = 0; i < sets; ++i) {
-      const float f = fast_exp2(sh_m[i][g] - ms);
-      zt = fmaf(sh_z[i][g], f, zt);
-      at = fmaf(sh_acc[i][g][c], f, at);
+#pragma unroll
+    for (int i = 0; i < 2 * WAVES; ++i) {
+      const float f = fast_exp2(m[i] - ms);
+      zt = fmaf(z[i], f, zt);
+      at = fmaf(x[i], f, at);
     }
     if (a.npart == 1) {
       a.out[(size_t)(head0 + g) * D + c] = zt > 0.f ? at / zt : 0.f;

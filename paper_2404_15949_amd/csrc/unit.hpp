@@ -24,7 +24,8 @@ static_assert(UNIT_WG == CHUNK, "the unit kernel reports survivors per CHUNK slo
 // launches that have about one unit per compute unit anyway, and a small stage (UNROLL / G) that keeps the G
 // accumulator sets and two stages within 128 registers, so that two workgroups share a compute unit, for
 // launches with at least two units per compute unit.
-template <typename DT, int D, int G, bool LAZY, int UU>
+// WEIGH: in the place of the record the normalized scores are added to the keys' accounts (corm_decode_attend_weigh; no append, no ring).
+template <typename DT, int D, int G, bool LAZY, int UU, bool WEIGH = false>
 __global__ __launch_bounds__(UNIT_WG) void corm_unit_kernel(const Params p, const int lstride) {
   using A = Attend<DT, D, G, UNIT_WAVES, UU>;
   constexpr int EPL = A::EPL, ROWB = A::ROWB, LPR = A::LPR, RPL = A::RPL;
@@ -189,13 +190,22 @@ __global__ __launch_bounds__(UNIT_WG) void corm_unit_kernel(const Params p, cons
   // one per tile.  The registers of the stream's stages are free by now.
   int pos_r[UNIT_MAX_TILES], lh_r[UNIT_MAX_TILES];
 #pragma unroll
-  for (int kt = 0; kt < UNIT_MAX_TILES; ++kt) {
+  for (int kt = 0; kt < UNIT_MAX_TILES && !WEIGH; ++kt) {
     pos_r[kt] = 0;
     lh_r[kt] = 0;
     if (kt * UNIT_WG < L && !p.ring_bits) {   // uniform over the workgroup (the bit-ring loop loads its own)
       const int in = min(kt * UNIT_WG + tid, L - 1);
       pos_r[kt] = posb[in];
       lh_r[kt] = lhb[in];
+    }
+  }
+
+  float account[WEIGH ? UNIT_MAX_TILES : 1];
+  if constexpr (WEIGH) {
+#pragma unroll
+    for (int kt = 0; kt < UNIT_MAX_TILES; ++kt) {
+      account[kt] = 0.f;
+      if (kt * UNIT_WG < L) account[kt] = accounts_in(p)[(size_t)unit * p.Lcap + min(kt * UNIT_WG + tid, L - 1)];
     }
   }
 
@@ -248,6 +258,22 @@ __global__ __launch_bounds__(UNIT_WG) void corm_unit_kernel(const Params p, cons
     }
   }
   __syncthreads();
+
+  if constexpr (WEIGH) {
+    float inv[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) inv[g] = 1.f / sh_Z[g];
+#pragma unroll
+    for (int kt = 0; kt < UNIT_MAX_TILES; ++kt) {
+      const int i = kt * UNIT_WG + tid;
+      if (kt * UNIT_WG >= L) break;
+      float sum = 0.f;
+#pragma unroll
+      for (int g = 0; g < G; ++g) sum = fmaf(fast_exp2(sh_logit[g * lstride + min(i, L - 1)] - sh_M[g]), inv[g], sum);
+      if (i < L) accounts_out(p)[(size_t)unit * p.Lcap + i] = account[kt] + sum;
+    }
+    return;
+  }
 
   // record (Def. 3.1) and decide (Def. 4.1 + recent r).  Survivors per tile are summed with LDS
   // atomics, so the loop has no barrier.

@@ -1,4 +1,4 @@
-// decode attention that accounts for every key's attention weight: the launch behind the split attend.
+// decode attention that accounts for every key's attention weight: the launch behind the split attend (many units: unit.hpp alone).
 // Part of one translation unit: included by corm_kernels.hip, after record.hpp.
 #ifndef CORM_WEIGH_HPP
 #define CORM_WEIGH_HPP
@@ -10,8 +10,7 @@ namespace {
 // loads where rows of the arrays begin at multiples of 16 bytes); many keys a workgroup, since its time is its chain of latencies.
 constexpr int WEIGH_KEYS = 4 * WG;   // keys of a round
 template <int G, int ROUNDS>
-__global__ __launch_bounds__(WG) void corm_weigh_kernel(const Params p, const float* weight_in, float* weight, const int D,
-                                                        const int n_out) {
+__global__ __launch_bounds__(WG) void corm_weigh_kernel(const Params p, const int D, const int n_out) {
   const int PSTRIDE = D + 2;
   const int unit = blockIdx.x;
   const UnitLen ul = unit_len(p, unit);
@@ -28,10 +27,10 @@ __global__ __launch_bounds__(WG) void corm_weigh_kernel(const Params p, const fl
   if (first >= L) return;
   __shared__ float sh_M[G], sh_Z[G];
   const int head0 = unit * G;
-  const float* in = weight_in + (size_t)unit * p.Lcap;
-  float* out = weight + (size_t)unit * p.Lcap;
+  const float* in = accounts_in(p) + (size_t)unit * p.Lcap;
+  float* out = accounts_out(p) + (size_t)unit * p.Lcap;
   const float* logits = p.logits + (size_t)head0 * p.Lcap;
-  const bool wide = ((p.Lcap & 3) | ((reinterpret_cast<uintptr_t>(weight_in) | reinterpret_cast<uintptr_t>(weight)) & 15)) == 0;
+  const bool wide = ((p.Lcap & 3) | ((reinterpret_cast<uintptr_t>(p.pos) | reinterpret_cast<uintptr_t>(p.last_hit)) & 15)) == 0;
   auto get = [&](const float* a, int i, float (&x)[4]) {
     if (wide && i + 4 <= L) {
       const float4 v = *reinterpret_cast<const float4*>(a + i);
