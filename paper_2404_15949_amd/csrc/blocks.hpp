@@ -71,104 +71,167 @@ __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, co
 // Upper bound of a block's logits: sum over channels of the larger of q*lo and q*hi, which is q+ * hi + q- * lo; the largest over the
 // heads of the group.  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
 // next to each other at the border of the choice differ by 1e-5 of their scores now and then, never by 1e-15).
-// Grid (groups of 64 blocks, units); lane = block, wave = a quarter of the channels, whose products meet in LDS.
+// The queries of the group's heads, halved, in 64 bits.  Ends without a barrier.
+template <typename DT, int D, int G, int NT>
+__device__ __forceinline__ void stage_half_q(const char* qu, double (&sh_q)[G][D]) {
+  for (int i = threadIdx.x; i < G * D; i += NT) {
+    const float x = DT::ESZ == 2 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(qu)[i] << 16)
+                                 : reinterpret_cast<const float*>(qu)[i];
+    sh_q[i / D][i % D] = 0.5 * (double)x;
+  }
+}
+
+// A quarter of the channels of the lane's block (bounds at `at`): its sums for every head.  The larger of q*a and q*b is
+// q/2 (a + b) + |q/2| |a - b|: one number of a query per channel from LDS, whose reads bound the kernel.
+template <typename DT, int D, int G>
+__device__ __forceinline__ void quarter_score(const char* at, int quarter, const double (&sh_q)[G][D], double (&sum)[G]) {
+  constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / WAVES, CH = D / WAVES, STEP = PIECES < 2 ? PIECES : 2;   // pieces of 16 bytes; of them in flight, from both rows
+  at += (size_t)quarter * (PIECES * 16);
+#pragma unroll
+  for (int g = 0; g < G; ++g) sum[g] = 0.;
+#pragma unroll
+  for (int j0 = 0; j0 < PIECES; j0 += STEP) {
+    uint4 x[STEP], y[STEP];
+#pragma unroll
+    for (int j = 0; j < STEP; ++j) {
+      x[j] = *reinterpret_cast<const uint4*>(at + (size_t)(j0 + j) * 16);
+      y[j] = *reinterpret_cast<const uint4*>(at + (size_t)ROWB + (size_t)(j0 + j) * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < STEP; ++j)
+#pragma unroll
+      for (int e = 0; e < EPL; ++e) {
+        const double a = (double)element<DT>(x[j], e), b = (double)element<DT>(y[j], e);
+        const double mid = a + b, apart = fabs(a - b);
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+          const double h = sh_q[g][quarter * CH + (j0 + j) * EPL + e];
+          sum[g] = fma(mid, h, sum[g]);
+          sum[g] = fma(apart, fabs(h), sum[g]);
+        }
+      }
+  }
+}
+
+// The quarters' sums of the lane's block -> its score.
+template <int G>
+__device__ __forceinline__ float joined_score(const double (&part)[WAVES][G][64]) {
+  const int lane = threadIdx.x & 63;
+  double best = 0.;
+#pragma unroll
+  for (int g = 0; g < G; ++g) {
+    const double t = (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
+    best = g == 0 ? t : fmax(best, t);
+  }
+  return (float)best;
+}
+
+// Grid (groups of 64 blocks, units).
 template <typename DT, int D, int G>
 __global__ __launch_bounds__(WG) void corm_block_score_kernel(const char* q, const char* bounds, const int32_t* lens, float* scores,
                                                               int Lcap, int nblk) {
-  constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / WAVES, CH = D / WAVES;
-  __shared__ double sh_q[G][2][D];          // q- (with the smallest elements), q+ (with the largest)
+  constexpr int ROWB = D * DT::ESZ;
+  __shared__ double sh_q[G][D];
   __shared__ double sh_part[WAVES][G][64];
   const int unit = blockIdx.y, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK;
   const int blk = blockIdx.x * 64 + lane;
   if ((int)blockIdx.x * 64 >= used) return;
-  const char* qu = q + (size_t)unit * G * ROWB;
-  for (int i = threadIdx.x; i < G * D; i += WG) {
-    const float x = DT::ESZ == 2 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(qu)[i] << 16)
-                                 : reinterpret_cast<const float*>(qu)[i];
-    sh_q[i / D][0][i % D] = (double)fminf(x, 0.f);
-    sh_q[i / D][1][i % D] = (double)fmaxf(x, 0.f);
-  }
+  stage_half_q<DT, D, G, WG>(q + (size_t)unit * G * ROWB, sh_q);
   __syncthreads();
-  const char* at = bounds + ((size_t)unit * nblk + min(blk, used - 1)) * 2 * ROWB + (size_t)wv * (PIECES * 16);
   double sum[G];
-#pragma unroll
-  for (int g = 0; g < G; ++g) sum[g] = 0.;
-#pragma unroll
-  for (int s = 0; s < 2; ++s) {
-    uint4 x[PIECES];
-#pragma unroll
-    for (int j = 0; j < PIECES; ++j) x[j] = *reinterpret_cast<const uint4*>(at + (size_t)s * ROWB + (size_t)j * 16);
-#pragma unroll
-    for (int j = 0; j < PIECES; ++j)
-#pragma unroll
-      for (int e = 0; e < EPL; ++e) {
-        const double v = (double)element<DT>(x[j], e);
-#pragma unroll
-        for (int g = 0; g < G; ++g) sum[g] = fma(v, sh_q[g][s][wv * CH + j * EPL + e], sum[g]);
-      }
-  }
+  quarter_score<DT, D, G>(bounds + ((size_t)unit * nblk + min(blk, used - 1)) * 2 * ROWB, wv, sh_q, sum);
 #pragma unroll
   for (int g = 0; g < G; ++g) sh_part[wv][g][lane] = sum[g];
   __syncthreads();
-  if (wv == 0 && blk < used) {
-    double best = 0.;
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-      const double t = (sh_part[0][g][lane] + sh_part[1][g][lane]) + (sh_part[2][g][lane] + sh_part[3][g][lane]);
-      best = g == 0 ? t : fmax(best, t);
-    }
-    scores[(size_t)unit * nblk + blk] = (float)best;
-  }
+  if (wv == 0 && blk < used) scores[(size_t)unit * nblk + blk] = joined_score<G>(sh_part);
 }
 
-// Grid (units): the nlast newest blocks and the best of the others, ascending, -1 behind them.
-// The keys are read once where they fit in LDS (scores of 262144 slots), else in every round from memory.
-constexpr int PICK_WG = 256, PICK_BITS = 8, PICK_KEYS = 4096;
-__global__ __launch_bounds__(PICK_WG) void corm_block_pick_kernel(const float* scores, const int32_t* lens, int32_t* blocks, int Lcap,
-                                                                  int nblk, int nsel, int nlast) {
-  __shared__ CutLds<PICK_WG, PICK_BITS> sh;
-  __shared__ uint32_t sh_key[PICK_KEYS];
-  __shared__ int sh_cnt[PICK_WG / 64];
-  const int unit = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK;
-  const float* sc = scores + (size_t)unit * nblk;
-  int32_t* to = blocks + (size_t)unit * nsel;
-  const int chosen = min(used, nsel);
-  for (int i = chosen + tid; i < nsel; i += PICK_WG) to[i] = -1;
-  const int open = used - min(nlast, used), k = chosen - (used - open);   // blocks to choose from, how many
+// The choice of a unit from the order_keys of its blocks below `open` (key(i)), by a workgroup of NT threads.
+template <int NT, typename Key>
+__device__ __forceinline__ void pick_blocks(int used, int nsel, int nlast, int32_t* to, const Key& key, CutLds<NT, 8>& sh, int* sh_cnt) {
+  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
+  const int chosen = min(used, nsel), open = used - min(nlast, used), k = chosen - (used - open);   // blocks to choose from, how many
+  for (int i = chosen + tid; i < nsel; i += NT) to[i] = -1;
   if (k == open) {   // all of them
-    for (int i = tid; i < chosen; i += PICK_WG) to[i] = i;
+    for (int i = tid; i < chosen; i += NT) to[i] = i;
     return;
   }
-  for (int i = tid; i < used - open; i += PICK_WG) to[k + i] = open + i;
+  for (int i = tid; i < used - open; i += NT) to[k + i] = open + i;
   if (k == 0) return;
-  const bool held = open <= PICK_KEYS;
-  if (held)
-    for (int i = tid; i < open; i += PICK_WG) sh_key[i] = order_key(sc[i]);   // (a thread reads back its own)
   auto item = [&](int i, uint32_t& x, uint32_t& slot) {
-    x = held ? sh_key[i] : order_key(sc[i]);
+    x = key(i);
     slot = (uint32_t)i;
     return true;
   };
-  const Cut cut = find_cut<PICK_WG, PICK_BITS, 32>(open, (uint32_t)k, item, sh);
+  const Cut cut = find_cut<NT, 8, 32>(open, (uint32_t)k, item, sh);
   int before = 0;   // chosen in front of this tile
-  for (int i0 = 0; i0 < open; i0 += PICK_WG) {
+  for (int i0 = 0; i0 < open; i0 += NT) {
     const int i = i0 + tid;
-    uint32_t x = 0u, slot;
-    if (i < open) item(i, x, slot);
+    const uint32_t x = i < open ? key(i) : 0u;
     const bool in = i < open && (x > cut.key || (x == cut.key && (uint32_t)i <= cut.last));
     const unsigned long long mask = __ballot(in);
     __syncthreads();
     if (lane == 0) sh_cnt[wv] = __popcll(mask);
     __syncthreads();
     int at = before + __popcll(mask & ((1ull << lane) - 1ull));
-    for (int w = 0; w < PICK_WG / 64; ++w) {
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
       at += w < wv ? sh_cnt[w] : 0;
       before += sh_cnt[w];
     }
     if (in) to[at] = i;
   }
+}
+
+// Grid (units): the nlast newest blocks and the best of the others, ascending, -1 behind them.
+// The keys are read once where they fit in LDS (scores of 262144 slots), else in every round from memory.
+constexpr int PICK_WG = 256, PICK_KEYS = 4096;
+__global__ __launch_bounds__(PICK_WG) void corm_block_pick_kernel(const float* scores, const int32_t* lens, int32_t* blocks, int Lcap,
+                                                                  int nblk, int nsel, int nlast) {
+  __shared__ CutLds<PICK_WG, 8> sh;
+  __shared__ uint32_t sh_key[PICK_KEYS];
+  __shared__ int sh_cnt[PICK_WG / 64];
+  const int unit = blockIdx.x;
+  const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK, open = max(used - nlast, 0);
+  const float* sc = scores + (size_t)unit * nblk;
+  const bool held = open <= PICK_KEYS;
+  if (held)
+    for (int i = threadIdx.x; i < open; i += PICK_WG) sh_key[i] = order_key(sc[i]);   // (a thread reads back its own)
+  pick_blocks<PICK_WG>(used, nsel, nlast, blocks + (size_t)unit * nsel, [&](int i) { return held ? sh_key[i] : order_key(sc[i]); }, sh,
+                       sh_cnt);
+}
+
+// Scores and choice in one launch, a workgroup a unit, where a unit has few blocks: a launch less, but the scores of a unit are then one compute unit's
+// work.  Whole steps, us, one launch | two: 288 units x 5 blocks 23.5 | 28.0, 34 x 10 19.6 | 23.1, 32 x 44 23.2 | 27.2, 256 x 65 39.8 | 42.4, 8 x 127
+// 17.5 | 18.3, 8 x 251 19.3 | 18.0, 64 x 257 50.2 | 48.2, 8 x 513 25.7 | 20.1.
+constexpr int CHOOSE_BLOCKS = 128, CHOOSE_WG = CHOOSE_BLOCKS * WAVES;
+template <typename DT, int D, int G>
+__global__ __launch_bounds__(CHOOSE_WG) void corm_block_choose_kernel(const char* q, const char* bounds, const int32_t* lens,
+                                                                      int32_t* blocks, int Lcap, int nblk, int nsel, int nlast) {
+  constexpr int ROWB = D * DT::ESZ;
+  __shared__ double sh_q[G][D];
+  __shared__ double sh_part[CHOOSE_BLOCKS / 64][WAVES][G][64];
+  __shared__ uint32_t sh_key[CHOOSE_BLOCKS];
+  __shared__ CutLds<CHOOSE_WG, 8> sh;
+  __shared__ int sh_cnt[CHOOSE_WG / 64];
+  const int unit = blockIdx.x, lane = threadIdx.x & 63, wv = threadIdx.x >> 6, grp = wv / WAVES, quarter = wv % WAVES;
+  const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK, open = max(used - nlast, 0);
+  if (nsel < used && open > 0) {   // (else all of them are chosen, or the newest; these need no score)
+    const int blk = grp * 64 + lane;
+    stage_half_q<DT, D, G, CHOOSE_WG>(q + (size_t)unit * G * ROWB, sh_q);
+    __syncthreads();
+    if (grp * 64 < open) {   // (uniform over the wave)
+      double sum[G];
+      quarter_score<DT, D, G>(bounds + ((size_t)unit * nblk + min(blk, open - 1)) * 2 * ROWB, quarter, sh_q, sum);
+#pragma unroll
+      for (int g = 0; g < G; ++g) sh_part[grp][quarter][g][lane] = sum[g];
+    }
+    __syncthreads();
+    if (quarter == 0 && blk < open) sh_key[blk] = order_key(joined_score<G>(sh_part[grp]));
+    __syncthreads();
+  }
+  pick_blocks<CHOOSE_WG>(used, nsel, nlast, blocks + (size_t)unit * nsel, [&](int i) { return sh_key[i]; }, sh, sh_cnt);
 }
 
 // ---------------------------------------------------------------- attention over the listed blocks

@@ -218,15 +218,23 @@ int corm_block_select(const corm_desc* desc, const void* q, const void* bounds, 
   const int nblk = blocks_of(desc), units = desc->B * desc->Hkv;
   float* scores = reinterpret_cast<float*>(workspace);
   hipStream_t s = (hipStream_t)stream;
+  const bool one = nblk <= CHOOSE_BLOCKS;
   rc = by_row(desc, [&](auto dt, auto dd) {
     return by_group(desc, [&](auto g) {
-      hipLaunchKernelGGL((corm_block_score_kernel<decltype(dt), decltype(dd)::value, decltype(g)::value>), dim3((nblk + 63) / 64, units),
-                         dim3(WG), 0, s, reinterpret_cast<const char*>(q), reinterpret_cast<const char*>(bounds), lens, scores,
-                         desc->Lcap, nblk);
+      using T = decltype(dt);
+      constexpr int D = decltype(dd)::value, G = decltype(g)::value;
+      const char* qc = reinterpret_cast<const char*>(q);
+      const char* bc = reinterpret_cast<const char*>(bounds);
+      if (one)
+        hipLaunchKernelGGL((corm_block_choose_kernel<T, D, G>), dim3(units), dim3(CHOOSE_WG), 0, s, qc, bc, lens, blocks, desc->Lcap, nblk,
+                           nsel, nlast);
+      else
+        hipLaunchKernelGGL((corm_block_score_kernel<T, D, G>), dim3((nblk + 63) / 64, units), dim3(WG), 0, s, qc, bc, lens, scores,
+                           desc->Lcap, nblk);
       return launch_status();
     });
   });
-  if (rc) return rc;
+  if (rc || one) return rc;
   hipLaunchKernelGGL(corm_block_pick_kernel, dim3(units), dim3(PICK_WG), 0, s, scores, lens, blocks, desc->Lcap, nblk, nsel, nlast);
   return launch_status();
 }

@@ -215,11 +215,12 @@ struct QueryOperand {
 // they lie, and no lane hands anything to another but the maximum.
 // Softmax in the log2 domain with the running maximum m; p = 2^(s - m + 15) is rounded to hi + lo in halves (22 bits; the 15 keeps
 // what is 2^-40 of the largest), so the products with the codes are exact and everything is summed in fp32.  The scales are
-// taken in where they cost least: a block's key scale with the softmax scale (one product a score), its value scale with the sum of the block.
+// taken in where they cost least: a block's key scale with the softmax scale (one product a score), its value scale (and 2^-15) with the sum of
+// the block.
 template <typename C, typename DT, int D>
 __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   constexpr int PANELS = D / 64, CT = D / 16, STEPS = D / 32;
-  constexpr float RAISE = 15.f;
+  constexpr float RAISE = 15.f, LOWER = 0x1p-15f;
   __shared__ float sh_acc[2 * WAVES][8][D];   // of the waves' blocks; of their rows of the tail
   __shared__ float sh_m[2 * WAVES][8], sh_z[2 * WAVES][8];
   __shared__ float sh_junk[QBLK];
@@ -324,7 +325,7 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
     const float qscale = qo.undo * a.scale_log2;
     float knext = ks[min(id, a.nblk - 1)], vnext = vs[min(id, a.nblk - 1)];
     for (int i = wv; i < count; i += WAVES) {
-      const float kscale = knext * qscale, vscale = vnext;
+      const float kscale = knext * qscale, vscale = vnext * LOWER;
       id = id_of(i + WAVES);
       knext = ks[min(id, a.nblk - 1)];
       vnext = vs[min(id, a.nblk - 1)];
@@ -393,9 +394,9 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   if (n < G && count > 0) {
 #pragma unroll
     for (int c = 0; c < CT; ++c) *reinterpret_cast<f32x4_t*>(&sh_acc[wv][n][16 * c + 4 * lg]) = acc[c];
-    if (lg == 0) {   // (sum and products are 2^15 times those of the maximum)
-      sh_m[wv][n] = m_run - RAISE;
-      sh_z[wv][n] = z_run;
+    if (lg == 0) {
+      sh_m[wv][n] = m_run;
+      sh_z[wv][n] = z_run * LOWER;
     }
   }
   int sets = WAVES;

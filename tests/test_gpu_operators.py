@@ -181,6 +181,18 @@ def test_q8_attend_lengths_one_by_one(dtype, code):
         c.check_out(q)
 
 
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+def test_q8_attend_over_rows_of_very_different_magnitude(code):
+    """Blocks whose keys and values are of magnitude 0, 1e-33, 1e-6, 1 and (values) 1e30: scales of every size."""
+    g, d = _gen(8), 128
+    c = Q8(1, 4, 1, d, 64 * 6, "f32", code)
+    mag = lambda *m: torch.tensor(m).repeat_interleave(64)[:350].view(1, 1, -1, 1)  # noqa: E731
+    c.append(_rows(g, "f32", 1, 1, 350, d) * mag(0.0, 1e-33, 1.0, 1e-6, 1.0, 1.0), _rows(g, "f32", 1, 1, 350, d) * mag(1.0, 0.0, 1e30, 1e-33, 1e30, 1.0))
+    q = _rows(g, "f32", 1, 4, d)
+    c.attend(q)
+    c.check_out(q)
+
+
 def test_q8_attend_over_listed_blocks():
     """Any order, -1 between, blocks beyond the unit's (skipped and flagged), the unfinished block, blocks listed twice, an empty list."""
     g = _gen(7)
@@ -255,6 +267,26 @@ def test_block_select(B, Hq, Hkv, d, cap, dtype, nsel, nlast):
             m = (int(lens[b, h]) + 63) // 64
             want = ref.choose(q[b, h * G:(h + 1) * G], bounds[b, h, :m], nsel, nlast)
             assert blocks[b, h].tolist() == want + [-1] * (nsel - len(want)), (b, h, m)
+
+
+@pytest.mark.parametrize("nblk", [100, 129, 700, 5000])
+def test_block_select_among_equal_and_many_blocks(nblk):
+    """Every block the same: the lowest are chosen.  Then all but a few, and numbers on both sides of what one launch and LDS hold."""
+    g, d, G = _gen(nblk), 64, 2
+    desc = corm.make_desc(3, G, 1, d, nblk * 64, nblk * 64, 1, 1, "f32")
+    lens = torch.tensor([[nblk * 64], [nblk * 64 - 70], [nblk * 32 + 1]], dtype=torch.int32)
+    q = _rows(g, "f32", 3, G, d)
+    bounds = torch.zeros(3, 1, nblk, 2, d)
+    bounds[:, :, :, 0], bounds[:, :, :, 1] = -1.0, 2.0
+    bounds[1, 0, ::17] = torch.randn(len(range(0, nblk, 17)), 2, d, generator=g)
+    bounds[2] = torch.randn(1, nblk, 2, d, generator=g)
+    for nsel, nlast in ((60, 3), (5, 1), (90, 90)):
+        blocks = torch.full((3, 1, nsel), -77, dtype=torch.int32, device=DEV)
+        corm.corm_block_select(desc, q.to(DEV), bounds.to(DEV), lens.to(DEV), nsel, nlast, blocks, _ws(desc))
+        for b in range(3):
+            m = (int(lens[b]) + 63) // 64
+            want = ref.choose(q[b], bounds[b, 0, :m], nsel, nlast)
+            assert blocks[b, 0].tolist() == want + [-1] * (nsel - len(want)), (b, nsel)
 
 
 @pytest.mark.parametrize("B,Hq,Hkv,d,cap,dtype", SHAPES)
