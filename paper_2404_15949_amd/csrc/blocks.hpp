@@ -71,20 +71,20 @@ __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, co
 // Upper bound of a block's logits: sum over channels of the larger of q*lo and q*hi, which is q+ * hi + q- * lo; the largest over the
 // heads of the group.  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
 // next to each other at the border of the choice differ by 1e-5 of their scores now and then, never by 1e-15).
-// The queries of the group's heads, halved, in 64 bits.  Ends without a barrier.
+// q- (taken with the smaller elements) and q+ (with the larger) of the group's heads.  Ends without a barrier.
 template <typename DT, int D, int G, int NT>
-__device__ __forceinline__ void stage_half_q(const char* qu, double (&sh_q)[G][D]) {
+__device__ __forceinline__ void stage_signed_q(const char* qu, double2 (&sh_q)[G][D]) {
   for (int i = threadIdx.x; i < G * D; i += NT) {
     const float x = DT::ESZ == 2 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(qu)[i] << 16)
                                  : reinterpret_cast<const float*>(qu)[i];
-    sh_q[i / D][i % D] = 0.5 * (double)x;
+    sh_q[i / D][i % D] = make_double2((double)fminf(x, 0.f), (double)fmaxf(x, 0.f));
   }
 }
 
-// A quarter of the channels of the lane's block (bounds at `at`): its sums for every head.  The larger of q*a and q*b is
-// q/2 (a + b) + |q/2| |a - b|: one number of a query per channel from LDS, whose reads bound the kernel.
+// A quarter of the channels of the lane's block (bounds at `at`): its sums for every head.  (From the bounds' sum and distance one number of a query per channel
+// would do, a little faster, but one bound of 1e30 would take all digits of the other.)
 template <typename DT, int D, int G>
-__device__ __forceinline__ void quarter_score(const char* at, int quarter, const double (&sh_q)[G][D], double (&sum)[G]) {
+__device__ __forceinline__ void quarter_score(const char* at, int quarter, const double2 (&sh_q)[G][D], double (&sum)[G]) {
   constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / WAVES, CH = D / WAVES, STEP = PIECES < 2 ? PIECES : 2;   // pieces of 16 bytes; of them in flight, from both rows
   at += (size_t)quarter * (PIECES * 16);
 #pragma unroll
@@ -101,13 +101,12 @@ __device__ __forceinline__ void quarter_score(const char* at, int quarter, const
     for (int j = 0; j < STEP; ++j)
 #pragma unroll
       for (int e = 0; e < EPL; ++e) {
-        const double a = (double)element<DT>(x[j], e), b = (double)element<DT>(y[j], e);
-        const double mid = a + b, apart = fabs(a - b);
+        const float a = element<DT>(x[j], e), b = element<DT>(y[j], e);   // (whichever is the smaller)
+        const double lo = (double)fminf(a, b), hi = (double)fmaxf(a, b);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const double h = sh_q[g][quarter * CH + (j0 + j) * EPL + e];
-          sum[g] = fma(mid, h, sum[g]);
-          sum[g] = fma(apart, fabs(h), sum[g]);
+          const double2 h = sh_q[g][quarter * CH + (j0 + j) * EPL + e];
+          sum[g] = fma(hi, h.y, fma(lo, h.x, sum[g]));
         }
       }
   }
@@ -131,13 +130,13 @@ template <typename DT, int D, int G>
 __global__ __launch_bounds__(WG) void corm_block_score_kernel(const char* q, const char* bounds, const int32_t* lens, float* scores,
                                                               int Lcap, int nblk) {
   constexpr int ROWB = D * DT::ESZ;
-  __shared__ double sh_q[G][D];
+  __shared__ double2 sh_q[G][D];
   __shared__ double sh_part[WAVES][G][64];
   const int unit = blockIdx.y, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK;
   const int blk = blockIdx.x * 64 + lane;
   if ((int)blockIdx.x * 64 >= used) return;
-  stage_half_q<DT, D, G, WG>(q + (size_t)unit * G * ROWB, sh_q);
+  stage_signed_q<DT, D, G, WG>(q + (size_t)unit * G * ROWB, sh_q);
   __syncthreads();
   double sum[G];
   quarter_score<DT, D, G>(bounds + ((size_t)unit * nblk + min(blk, used - 1)) * 2 * ROWB, wv, sh_q, sum);
@@ -210,7 +209,7 @@ template <typename DT, int D, int G>
 __global__ __launch_bounds__(CHOOSE_WG) void corm_block_choose_kernel(const char* q, const char* bounds, const int32_t* lens,
                                                                       int32_t* blocks, int Lcap, int nblk, int nsel, int nlast) {
   constexpr int ROWB = D * DT::ESZ;
-  __shared__ double sh_q[G][D];
+  __shared__ double2 sh_q[G][D];
   __shared__ double sh_part[CHOOSE_BLOCKS / 64][WAVES][G][64];
   __shared__ uint32_t sh_key[CHOOSE_BLOCKS];
   __shared__ CutLds<CHOOSE_WG, 8> sh;
@@ -219,7 +218,7 @@ __global__ __launch_bounds__(CHOOSE_WG) void corm_block_choose_kernel(const char
   const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK, open = max(used - nlast, 0);
   if (nsel < used && open > 0) {   // (else all of them are chosen, or the newest; these need no score)
     const int blk = grp * 64 + lane;
-    stage_half_q<DT, D, G, CHOOSE_WG>(q + (size_t)unit * G * ROWB, sh_q);
+    stage_signed_q<DT, D, G, CHOOSE_WG>(q + (size_t)unit * G * ROWB, sh_q);
     __syncthreads();
     if (grp * 64 < open) {   // (uniform over the wave)
       double sum[G];

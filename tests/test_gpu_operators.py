@@ -289,6 +289,22 @@ def test_block_select_among_equal_and_many_blocks(nblk):
             assert blocks[b, 0].tolist() == want + [-1] * (nsel - len(want)), (b, nsel)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_block_select_with_keys_of_the_lowest_value(dtype):
+    """Keys overwritten with the type's lowest value, as a mask: the bounds' other side still decides among blocks where queries are positive, nothing is lost to
+    the large numbers (q >= 0, so the lowest values never enter a score)."""
+    g, d, n = _gen(21), 64, 40
+    K = _rows(g, dtype, 1, 1, n * 64, d)
+    K[0, 0, 5::64] = torch.finfo(DT[dtype]).min
+    q = _rows(g, dtype, 1, 2, d).abs()
+    desc = corm.make_desc(1, 2, 1, d, n * 64, n * 64, 1, 1, dtype)
+    lens = torch.tensor([[n * 64]], dtype=torch.int32, device=DEV)
+    bounds, blocks = torch.empty(1, 1, n, 2, d, dtype=DT[dtype], device=DEV), torch.empty(1, 1, 9, dtype=torch.int32, device=DEV)
+    corm.corm_block_bounds(desc, K.to(DEV), lens, bounds)
+    corm.corm_block_select(desc, q.to(DEV), bounds, lens, 9, 1, blocks, _ws(desc))
+    assert blocks[0, 0].tolist() == ref.choose(q[0], ref.bounds_of(K[0, 0]), 9, 1)
+
+
 @pytest.mark.parametrize("B,Hq,Hkv,d,cap,dtype", SHAPES)
 @pytest.mark.parametrize("nsel", [1, 2, 11, 70])
 def test_block_attend(B, Hq, Hkv, d, cap, dtype, nsel):
