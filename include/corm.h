@@ -338,7 +338,7 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
  *
  * corm_decode_attend_weigh: corm_decode_attend's out, and weight[i] = weight_in[i] + sum over the heads of the group of the
  * normalized scores (Eq. 2), for slots < lens; others are left as they were.  weight may be weight_in.  Workspace, status and
- * opts as corm_decode_attend; neither pos nor t is needed.
+ * opts as corm_decode_attend (by shape, short units go by path 1 where corm_decode_attend takes 2); neither pos nor t is needed.
  *
  * corm_evict_mask_weight: keep [B, Hkv, Lcap] of a unit with lens > budget: the r newest slots (desc->r) and of the others the
  * budget - r with the greatest weight (equal ones: the lower slot first; not a number: least); all of them where lens <= budget.

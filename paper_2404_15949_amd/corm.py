@@ -344,6 +344,13 @@ def _dev(x, n: int, dtypes, name: str, device: int) -> Optional[int]:
                      f"strides {x.stride()} on {x.device}")
 
 
+def _scratch(x, device: int):
+    """Pointer of a workspace: any whole tensor on the current device, or a raw pointer."""
+    if isinstance(x, torch.Tensor) and not (x.is_contiguous() and x.get_device() == device):
+        raise ValueError(f"workspace: expected contiguous memory on the current device, got strides {x.stride()} on {x.device}")
+    return _ptr(x)
+
+
 _I32, _F4, _U8 = (torch.int32,), (torch.float32,), (torch.uint8, torch.bool)
 
 
@@ -388,7 +395,7 @@ def corm_q8_attend(desc, code, q, K_codes, V_codes, k_scale, v_scale, K_tail, V_
                               _dev(V_codes, units * nblk * BLOCK * d, ct, "V_codes", at), _dev(k_scale, units * nblk, _F4, "k_scale", at),
                               _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
                               _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
-                              _dev(blocks, units * nsel, _I32, "blocks", at), nsel, _dev(out, heads * d, _F4, "out", at), _ptr(workspace),
+                              _dev(blocks, units * nsel, _I32, "blocks", at), nsel, _dev(out, heads * d, _F4, "out", at), _scratch(workspace, at),
                               _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at), _stream(stream))
     return _check(rc, "corm_q8_attend") if check else rc
 
@@ -406,7 +413,7 @@ def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace=None
     units, heads, nblk, kv = _sizes(desc)
     at = _device()
     rc = lib().corm_block_select(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at),
-                                 _dev(lens, units, _I32, "lens", at), nsel, nlast, _dev(blocks, units * nsel, _I32, "blocks", at), _ptr(workspace),
+                                 _dev(lens, units, _I32, "lens", at), nsel, nlast, _dev(blocks, units * nsel, _I32, "blocks", at), _scratch(workspace, at),
                                  _nbytes(workspace, workspace_bytes), _stream(stream))
     return _check(rc, "corm_block_select") if check else rc
 
@@ -418,7 +425,7 @@ def corm_block_attend(desc, q, K, V, lens, blocks, nsel, out, workspace, workspa
     rows = units * desc.Lcap * desc.d
     rc = lib().corm_block_attend(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
                                  _dev(lens, units, _I32, "lens", at), _dev(blocks, units * nsel, _I32, "blocks", at), nsel,
-                                 _dev(out, heads * desc.d, _F4, "out", at), _ptr(workspace), _nbytes(workspace, workspace_bytes),
+                                 _dev(out, heads * desc.d, _F4, "out", at), _scratch(workspace, at), _nbytes(workspace, workspace_bytes),
                                  _dev(status, 1, _I32, "status", at), _stream(stream))
     return _check(rc, "corm_block_attend") if check else rc
 
@@ -431,7 +438,7 @@ def corm_decode_attend_weigh(desc, q, K, V, lens, weight_in, weight, out, worksp
     rc = lib().corm_decode_attend_weigh(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
                                         _dev(lens, units, _I32, "lens", at), _dev(weight_in, units * desc.Lcap, _F4, "weight_in", at),
                                         _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(out, heads * desc.d, _F4, "out", at),
-                                        _ptr(workspace), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at),
+                                        _scratch(workspace, at), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at),
                                         _opts(opts), _stream(stream))
     return _check(rc, "corm_decode_attend_weigh") if check else rc
 
@@ -439,7 +446,7 @@ def corm_decode_attend_weigh(desc, q, K, V, lens, weight_in, weight, out, worksp
 def corm_evict_mask_weight(desc, weight, lens, budget, keep, workspace, workspace_bytes=None, stream=None, check=True) -> int:
     units, at = desc.B * desc.Hkv, _device()
     rc = lib().corm_evict_mask_weight(ctypes.byref(desc), _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(lens, units, _I32, "lens", at),
-                                      budget, _dev(keep, units * desc.Lcap, _U8, "keep", at), _ptr(workspace),
+                                      budget, _dev(keep, units * desc.Lcap, _U8, "keep", at), _scratch(workspace, at),
                                       _nbytes(workspace, workspace_bytes), _stream(stream))
     return _check(rc, "corm_evict_mask_weight") if check else rc
 

