@@ -326,9 +326,19 @@ def _code(x) -> int:
     return x if isinstance(x, int) else _code_ids[x]
 
 
+_get_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _device() -> int:
     """The current device, asked once per call; no tensor is on -2, the answer before anything is on one."""
-    return torch.cuda.current_device() if torch.cuda.is_initialized() else -2
+    return _get_device() if torch.cuda.is_initialized() else -2
+
+
+def _on(stream, device: int) -> Optional[int]:
+    """_stream, for a call that knows the current device."""
+    if stream is None and _raw_stream is not None and device >= 0:
+        return _raw_stream(device)
+    return _stream(stream)
 
 
 def _dev(x, n: int, dtypes, name: str, device: int) -> Optional[int]:
@@ -336,10 +346,11 @@ def _dev(x, n: int, dtypes, name: str, device: int) -> Optional[int]:
     current device (the call goes to one of its streams); a raw pointer is taken as it is."""
     if x is None:
         return None
-    if not isinstance(x, torch.Tensor):
+    try:
+        if x.dtype in dtypes and x.numel() >= n and x.is_contiguous() and x.get_device() == device:
+            return x.data_ptr()
+    except AttributeError:   # not a tensor
         return int(x)
-    if x.dtype in dtypes and x.numel() >= n and x.is_contiguous() and x.get_device() == device:
-        return x.data_ptr()
     raise ValueError(f"{name}: expected {n} contiguous elements of {dtypes} on the current device, got {x.dtype} {tuple(x.shape)} with "
                      f"strides {x.stride()} on {x.device}")
 
@@ -381,7 +392,7 @@ def corm_q8_append(desc, code, k_new, v_new, n, n_new, K_codes, V_codes, k_scale
                               _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
                               _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
                               _dev(lens_out, units, _I32, "lens_out", at), _dev(bounds, units * nblk * 2 * d, kv, "bounds", at),
-                              _dev(status, 1, _I32, "status", at), _stream(stream))
+                              _dev(status, 1, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_q8_append") if check else rc
 
 
@@ -396,7 +407,7 @@ def corm_q8_attend(desc, code, q, K_codes, V_codes, k_scale, v_scale, K_tail, V_
                               _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
                               _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
                               _dev(blocks, units * nsel, _I32, "blocks", at), nsel, _dev(out, heads * d, _F4, "out", at), _scratch(workspace, at),
-                              _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at), _stream(stream))
+                              _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_q8_attend") if check else rc
 
 
@@ -405,7 +416,7 @@ def corm_block_bounds(desc, K, lens, bounds, newest=0, stream=None, check=True) 
     units, _, nblk, kv = _sizes(desc)
     at = _device()
     rc = lib().corm_block_bounds(ctypes.byref(desc), _dev(K, units * desc.Lcap * desc.d, kv, "K", at), _dev(lens, units, _I32, "lens", at), newest,
-                                 _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at), _stream(stream))
+                                 _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at), _on(stream, at))
     return _check(rc, "corm_block_bounds") if check else rc
 
 
@@ -414,7 +425,7 @@ def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace=None
     at = _device()
     rc = lib().corm_block_select(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at),
                                  _dev(lens, units, _I32, "lens", at), nsel, nlast, _dev(blocks, units * nsel, _I32, "blocks", at), _scratch(workspace, at),
-                                 _nbytes(workspace, workspace_bytes), _stream(stream))
+                                 _nbytes(workspace, workspace_bytes), _on(stream, at))
     return _check(rc, "corm_block_select") if check else rc
 
 
@@ -426,7 +437,7 @@ def corm_block_attend(desc, q, K, V, lens, blocks, nsel, out, workspace, workspa
     rc = lib().corm_block_attend(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
                                  _dev(lens, units, _I32, "lens", at), _dev(blocks, units * nsel, _I32, "blocks", at), nsel,
                                  _dev(out, heads * desc.d, _F4, "out", at), _scratch(workspace, at), _nbytes(workspace, workspace_bytes),
-                                 _dev(status, 1, _I32, "status", at), _stream(stream))
+                                 _dev(status, 1, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_block_attend") if check else rc
 
 
@@ -439,7 +450,7 @@ def corm_decode_attend_weigh(desc, q, K, V, lens, weight_in, weight, out, worksp
                                         _dev(lens, units, _I32, "lens", at), _dev(weight_in, units * desc.Lcap, _F4, "weight_in", at),
                                         _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(out, heads * desc.d, _F4, "out", at),
                                         _scratch(workspace, at), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at),
-                                        _opts(opts), _stream(stream))
+                                        _opts(opts), _on(stream, at))
     return _check(rc, "corm_decode_attend_weigh") if check else rc
 
 
@@ -447,7 +458,7 @@ def corm_evict_mask_weight(desc, weight, lens, budget, keep, workspace, workspac
     units, at = desc.B * desc.Hkv, _device()
     rc = lib().corm_evict_mask_weight(ctypes.byref(desc), _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(lens, units, _I32, "lens", at),
                                       budget, _dev(keep, units * desc.Lcap, _U8, "keep", at), _scratch(workspace, at),
-                                      _nbytes(workspace, workspace_bytes), _stream(stream))
+                                      _nbytes(workspace, workspace_bytes), _on(stream, at))
     return _check(rc, "corm_evict_mask_weight") if check else rc
 
 

@@ -67,13 +67,14 @@ __device__ __forceinline__ void find_digit(const uint32_t* sh_hist, uint32_t* sh
   __syncthreads();
 }
 
-constexpr int CUT_LISTED = 128;   // keys that are counted against each other (1024 by 1024 threads: 30 us)
+constexpr int CUT_LISTED = 128;   // keys that are counted against each other (512 units x 4352 weights, us: 64 8.9, 128 8.9, 256 9.0; 512 x 1500 10.5, 7.7, 7.1)
 
 // Memory of find_cut.
 template <int NT, int BITS>
 struct CutLds {
-  uint32_t hist[1 << BITS], pick[3], n;
   unsigned long long listed[CUT_LISTED];
+  uint32_t hist[1 << BITS], pick[3], n, front[CUT_LISTED];
+  static_assert(NT % CUT_LISTED == 0, "whole groups of threads");
 };
 
 // One digit: of the keys that item(i, x, slot) gives for i < n (where it says so) and that agree with `prefix` above their low `open` bits, BITS bits
@@ -93,7 +94,7 @@ __device__ __forceinline__ void cut_round(int n, uint32_t need, uint32_t prefix,
 
 // The cut that leaves k (1 <= k <= the number of keys) above it, by the whole workgroup.  item(i, x, slot): key below 2^TOP and slot number i of
 // n, or false; asked several times, for the same i by the same thread.  Digits from the top until few keys are left in the digit of
-// the cut (with weights and scores after one or two); these are listed, and every thread counts the ones in front of its own.  With
+// the cut (with weights and scores after one or two); these are listed, and each is counted against all others.  With
 // many keys 11 bits a digit rather than 8: an exponent alone has few values, so that the lanes of a wave would count in the same words (512 units of
 // 4352 weights 48 us with 8 bits, 9.3 with 11; 512 scores a unit 1.5 us less with 8).
 template <int NT, int BITS, int TOP, typename Item>
@@ -110,6 +111,7 @@ __device__ __forceinline__ Cut find_cut(int n, uint32_t k, const Item& item, Cut
   }
   if (have <= (uint32_t)CUT_LISTED) {
     if (threadIdx.x == 0) sh.n = 0u;
+    if (threadIdx.x < CUT_LISTED) sh.front[threadIdx.x] = 0u;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += NT) {
       uint32_t x, slot;
@@ -117,16 +119,20 @@ __device__ __forceinline__ Cut find_cut(int n, uint32_t k, const Item& item, Cut
         sh.listed[atomicAdd(&sh.n, 1u)] = (unsigned long long)x << 32 | (SLOT_TOP - slot);
     }
     __syncthreads();
-    const uint32_t m = sh.n;
-    if (threadIdx.x < m) {
-      const unsigned long long mine = sh.listed[threadIdx.x];
+    // each listed key against all others, NT / CUT_LISTED threads a key
+    const uint32_t m = sh.n, mine_at = threadIdx.x % CUT_LISTED;
+    if (mine_at < m) {
+      const unsigned long long mine = sh.listed[mine_at];
       uint32_t front = 0u;
-#pragma unroll 8
-      for (uint32_t j = 0; j < m; ++j) front += sh.listed[j] > mine;
-      if (front == need - 1u) {
-        sh.pick[0] = (uint32_t)(mine >> 32);
-        sh.pick[1] = SLOT_TOP - (uint32_t)mine;
-      }
+#pragma unroll 4
+      for (uint32_t j = threadIdx.x / CUT_LISTED; j < m; j += NT / CUT_LISTED) front += sh.listed[j] > mine;
+      if (front) atomicAdd(&sh.front[mine_at], front);
+    }
+    __syncthreads();
+    if (threadIdx.x < m && sh.front[threadIdx.x] == need - 1u) {
+      const unsigned long long mine = sh.listed[threadIdx.x];
+      sh.pick[0] = (uint32_t)(mine >> 32);
+      sh.pick[1] = SLOT_TOP - (uint32_t)mine;
     }
     __syncthreads();
     const Cut cut = {sh.pick[0], sh.pick[1]};
