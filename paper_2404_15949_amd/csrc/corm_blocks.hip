@@ -168,9 +168,14 @@ int corm_q8_attend(const corm_desc* desc, int32_t code_dtype, const void* q, con
   a.Hq = desc->Hq; a.Hkv = desc->Hkv; a.Lcap = desc->Lcap; a.nblk = blocks_of(desc); a.nsel = blocks ? nsel : 0;
   a.scale_log2 = scale_log2(desc);
   const long units = (long)desc->B * desc->Hkv;
-  const int listed = blocks ? nsel : a.nblk;
+  const int listed = blocks ? nsel : a.nblk, real = std::min(listed, a.nblk);   // (a list holds at most the unit's blocks in earnest)
   const long cus = device_cus();
-  if (units >= 2 * cus && listed <= Q8_MOST) {
+  // A workgroup takes a whole unit where there are two units per compute unit, or where a unit has few blocks; else parts of whole rounds of blocks
+  // over the waves, at least two rounds unless the launch would then be small, up to 16 workgroups per compute unit, and a merge.
+  // Whole calls, us, parts | whole: 512 units x 540 .. 2048 slots 47 | 36, 1000 x 1500 113 | 62, 1536 x 200 27 | 17; 256 x 190 .. 8192 56 | 76, 300 x 3000
+  // 42 | 49; 8 to 128 units, 2 blocks 7.4 | 5.5 and 9.1 | 7.1, 5 blocks 8.5 | 7.6 and 10.7 | 8.4, 9 blocks 9.1 | 9.9 and 12.4 | 11.2, 17 blocks
+  // 8.8 | 12.6 and 14.8 | 15.9.  Parts of 4 | 8 blocks: 32 x 4096 12.4 | 13.8, 8 x 32768 24.0 | 20.0.
+  if (listed <= Q8_MOST && (units >= 2 * cus || real <= 2 * WAVES || (2 * units >= cus && real <= 4 * WAVES))) {
     a.part_blocks = (listed + WAVES - 1) / WAVES * WAVES;
     a.npart = 1;
   } else {
@@ -260,7 +265,10 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
   const long wgs = (row_bytes(desc) > 256 ? 4L : 2L) * device_cus();
   auto parts_of = [&](int n) { return (n + a.part_blocks - 1) / a.part_blocks; };
   a.part_blocks = 1;
-  while (a.part_blocks < LIST_PART && (units * parts_of(real) > wgs || parts_of(nsel) > room)) a.part_blocks *= 2;
+  // (few blocks: one part, which writes out itself.  Whole steps, us, parts and merge | one part: bf16, 8 to 128 units, 2 blocks 15.6 | 13.5 and 17.3 | 14.5, 4 blocks
+  // 15.5 | 14.9 and 20.4 | 16.4, 8 blocks 15.5 | 17.6 and 23.0 | 20.1; fp32 2 blocks 15.0 | 13.8 and 17.6 | 16.0, of eight heads 21.3 | 22.2 and 25.3 | 24.5, 4 blocks 15.3 | 18.3)
+  const bool few = nsel <= (desc->kv_dtype == CORM_F32 ? 2 : 4);
+  while (a.part_blocks < LIST_PART && (few || units * parts_of(real) > wgs || parts_of(nsel) > room)) a.part_blocks *= 2;
   const int parts = parts_of(nsel);
   a.npart = parts;
   hipStream_t s = (hipStream_t)stream;
