@@ -341,13 +341,13 @@ def _on(stream, device: int) -> Optional[int]:
     return _stream(stream)
 
 
-def _dev(x, n: int, dtypes, name: str, device: int) -> Optional[int]:
-    """Pointer of an argument whose layout the call takes for granted.  A tensor has to be whole, of the right type, large enough and on the
-    current device (the call goes to one of its streams); a raw pointer is taken as it is."""
+def _dev(x, n: Optional[int], dtypes, name: str, device: int) -> Optional[int]:
+    """Pointer of an argument whose layout the call takes for granted.  A tensor has to be whole, of the right type, of n elements (None: any
+    number) and on the current device (the call goes to one of its streams); a raw pointer is taken as it is."""
     if x is None:
         return None
     try:
-        if x.dtype in dtypes and x.numel() >= n and x.is_contiguous() and x.get_device() == device:
+        if x.dtype in dtypes and (x.numel() == n or n is None) and x.is_contiguous() and x.get_device() == device:
             return x.data_ptr()
     except AttributeError:   # not a tensor
         return int(x)
@@ -392,7 +392,7 @@ def corm_q8_append(desc, code, k_new, v_new, n, n_new, K_codes, V_codes, k_scale
                               _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
                               _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
                               _dev(lens_out, units, _I32, "lens_out", at), _dev(bounds, units * nblk * 2 * d, kv, "bounds", at),
-                              _dev(status, 1, _I32, "status", at), _on(stream, at))
+                              _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_q8_append") if check else rc
 
 
@@ -407,7 +407,7 @@ def corm_q8_attend(desc, code, q, K_codes, V_codes, k_scale, v_scale, K_tail, V_
                               _dev(v_scale, units * nblk, _F4, "v_scale", at), _dev(K_tail, units * BLOCK * d, kv, "K_tail", at),
                               _dev(V_tail, units * BLOCK * d, kv, "V_tail", at), _dev(lens, units, _I32, "lens", at),
                               _dev(blocks, units * nsel, _I32, "blocks", at), nsel, _dev(out, heads * d, _F4, "out", at), _scratch(workspace, at),
-                              _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at), _on(stream, at))
+                              _nbytes(workspace, workspace_bytes), _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_q8_attend") if check else rc
 
 
@@ -437,7 +437,7 @@ def corm_block_attend(desc, q, K, V, lens, blocks, nsel, out, workspace, workspa
     rc = lib().corm_block_attend(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
                                  _dev(lens, units, _I32, "lens", at), _dev(blocks, units * nsel, _I32, "blocks", at), nsel,
                                  _dev(out, heads * desc.d, _F4, "out", at), _scratch(workspace, at), _nbytes(workspace, workspace_bytes),
-                                 _dev(status, 1, _I32, "status", at), _on(stream, at))
+                                 _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_block_attend") if check else rc
 
 
@@ -449,7 +449,7 @@ def corm_decode_attend_weigh(desc, q, K, V, lens, weight_in, weight, out, worksp
     rc = lib().corm_decode_attend_weigh(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(K, rows, kv, "K", at), _dev(V, rows, kv, "V", at),
                                         _dev(lens, units, _I32, "lens", at), _dev(weight_in, units * desc.Lcap, _F4, "weight_in", at),
                                         _dev(weight, units * desc.Lcap, _F4, "weight", at), _dev(out, heads * desc.d, _F4, "out", at),
-                                        _scratch(workspace, at), _nbytes(workspace, workspace_bytes), _dev(status, 1, _I32, "status", at),
+                                        _scratch(workspace, at), _nbytes(workspace, workspace_bytes), _dev(status, None, _I32, "status", at),
                                         _opts(opts), _on(stream, at))
     return _check(rc, "corm_decode_attend_weigh") if check else rc
 

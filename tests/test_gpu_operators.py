@@ -607,7 +607,7 @@ def test_tensors_that_do_not_fit_the_call_are_refused():
     out = torch.zeros(1, 2, 64, device=DEV)
     good = dict(q=q, K=K, V=K, lens=lens, blocks=blocks, nsel=2, out=out, workspace=ws)
     corm.corm_block_attend(desc, **good)
-    for name, bad in (("q", q.float()), ("K", K[:, :, ::2]), ("K", K[:, :, :64].contiguous()), ("lens", lens.long()), ("out", out.cpu()),
+    for name, bad in (("q", q.float()), ("K", K[:, :, ::2]), ("K", K[:, :, :64].contiguous()), ("K", K.repeat(1, 1, 2, 1)), ("lens", lens.long()), ("out", out.cpu()),
                       ("blocks", blocks[:, :, :1]), ("workspace", ws[::2]), ("workspace", ws.cpu())):
         with pytest.raises(ValueError):
             corm.corm_block_attend(desc, **{**good, name: bad})
