@@ -580,6 +580,64 @@ def test_captured_steps_on_another_stream_repeat_the_eager_ones():
         assert torch.equal(x, y)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_lengths_that_are_none_are_clamped_and_flagged(dtype):
+    """-3 and Lcap + 5: what 0 and Lcap give, in every call that reads lengths, and the flag where the call has one."""
+    g, B, Hq, Hkv, d, cap = _gen(31), 2, 4, 1, 64, 64 * 9 + 7
+    good, bad = torch.tensor([[0], [cap]], dtype=torch.int32, device=DEV), torch.tensor([[-3], [cap + 5]], dtype=torch.int32, device=DEV)
+    K, V, q = (x.to(DEV) for x in _state(g, B, Hq, Hkv, d, cap, dtype, torch.full((B, Hkv), cap)))
+    desc = corm.make_desc(B, Hq, Hkv, d, cap, cap, 1, 4, dtype)
+    full = torch.empty(corm.corm_workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    c = Q8(B, Hq, Hkv, d, cap, dtype, "i8")
+    c.append(K.cpu(), V.cpu())
+    w0 = torch.rand(B, Hkv, cap, device=DEV)
+    blocks = torch.arange(10, dtype=torch.int32, device=DEV).view(1, 1, 10).repeat(B, 1, 1)
+    blocks[0] = -1
+    got = []
+    for lens in (good, bad):
+        status = torch.zeros(3, dtype=torch.int32, device=DEV)
+        outs = [torch.full((B, Hq, d), 3.0, device=DEV) for _ in range(3)]
+        bounds = torch.zeros(B, Hkv, 10, 2, d, dtype=DT[dtype], device=DEV)
+        picked, weight = torch.zeros(B, Hkv, 4, dtype=torch.int32, device=DEV), torch.zeros(B, Hkv, cap, device=DEV)
+        keep = torch.zeros(B, Hkv, cap, dtype=torch.uint8, device=DEV)
+        corm.corm_q8_attend(desc, "i8", q, c.Kc, c.Vc, c.ks, c.vs, c.Kt, c.Vt, lens, outs[0], c.ws, status=status[0:1])
+        corm.corm_block_attend(desc, q, K, V, lens, blocks, 10, outs[1], c.ws, status=status[1:2])
+        corm.corm_decode_attend_weigh(desc, q, K, V, lens, w0, weight, outs[2], full, status=status[2:3])
+        corm.corm_block_bounds(desc, K, lens, bounds)
+        corm.corm_block_select(desc, q, bounds, lens, 4, 1, picked, c.ws)
+        corm.corm_evict_mask_weight(desc, w0, lens, 100, keep, c.ws)
+        got.append([*outs, weight, bounds, picked, keep])
+        assert status.tolist() == ([0] * 3 if lens is good else [corm.CORM_DEV_BAD_LENS] * 3)
+    for a, b in zip(*got):
+        assert torch.equal(a, b)
+    assert not got[0][0][0].any() and bool(got[0][0][1].any())
+
+
+@pytest.mark.parametrize("dtype,G", [("bf16", 4), ("bf16", 1), ("f32", 2)])
+def test_lists_of_the_most_blocks(dtype, G):
+    """512 places for a unit of nine blocks, most of them empty, some blocks several times."""
+    g, d, cap, n = _gen(33), 128, 64 * 9, 512
+    lens = torch.tensor([[cap - 10], [200]], dtype=torch.int32)
+    K, V, q = _state(g, 2, G, 1, d, cap, dtype, lens)
+    desc = corm.make_desc(2, G, 1, d, cap, cap, 1, 1, dtype)
+    blocks = torch.full((2, 1, n), -1, dtype=torch.int32)
+    for b, many in ((0, 9), (1, 4)):
+        at = torch.randperm(n, generator=g)[:40]
+        blocks[b, 0, at] = torch.randint(0, many, (40,), generator=g, dtype=torch.int32)
+    sm, ws = 1.0 / math.sqrt(d), _ws(desc)
+    out = torch.full((2, G, d), float("nan"), device=DEV)
+    corm.corm_block_attend(desc, q.to(DEV), K.to(DEV), V.to(DEV), lens.to(DEV), blocks.to(DEV), n, out, ws)
+    c = Q8(2, G, 1, d, cap, dtype, "e4m3")
+    c.append(K.nan_to_num(), V.nan_to_num(), lens.flatten().tolist())
+    c.attend(q, blocks.tolist())
+    c.check_out(q, blocks.tolist())
+    for b in range(2):
+        slots = [s for i in blocks[b, 0].tolist() if i >= 0 for s in range(64 * i, min(64 * i + 64, int(lens[b])))]
+        x, Ks, Vs = q[b].double(), K[b, 0, slots].double(), V[b, 0, slots].double()
+        want, _ = ref.attention(x, Ks, Vs, sm)
+        assert float((out[b].cpu().double() - want).abs().max()) <= ref.out_error(x, Ks, Vs, sm)
+
+
 def test_what_is_not_a_number_stays_none():
     """A query that is not a number gives outputs that are none, of its head alone, also where partials are joined."""
     g, d = _gen(22), 64
