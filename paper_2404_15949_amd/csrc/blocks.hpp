@@ -69,7 +69,7 @@ __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, co
 // ---------------------------------------------------------------- the choice
 
 // Upper bound of a block's logits: sum over channels of the larger of q*lo and q*hi, which is q+ * hi + q- * lo; the largest over the
-// heads of the group.  Bound by the 64-bit products and their queries from LDS (128 units x 440 blocks, four heads: 11.7 us for 29 MB).  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
+// heads of the group.  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
 // next to each other at the border of the choice differ by 1e-5 of their scores now and then, never by 1e-15).
 // q- (taken with the smaller elements) and q+ (with the larger) of the group's heads.  Ends without a barrier.
 template <typename DT, int D, int G, int NT>
@@ -81,12 +81,12 @@ __device__ __forceinline__ void stage_signed_q(const char* qu, double2 (&sh_q)[G
   }
 }
 
-// A quarter of the channels of the lane's block (bounds at `at`): its sums for every head.  (From the bounds' sum and distance one number of a query per channel
+// A share of the channels of the lane's block (bounds at `at`): its sums for every head.  (From the bounds' sum and distance one number of a query per channel
 // would do, a little faster, but one bound of 1e30 would take all digits of the other.)
-template <typename DT, int D, int G>
-__device__ __forceinline__ void quarter_score(const char* at, int quarter, const double2 (&sh_q)[G][D], double (&sum)[G]) {
-  constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / WAVES, CH = D / WAVES, STEP = PIECES < 2 ? PIECES : 2;   // pieces of 16 bytes; of them in flight, from both rows
-  at += (size_t)quarter * (PIECES * 16);
+template <typename DT, int D, int G, int SHARES>
+__device__ __forceinline__ void share_score(const char* at, int share, const double2 (&sh_q)[G][D], double (&sum)[G]) {
+  constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / SHARES, CH = D / SHARES, STEP = PIECES < 2 ? PIECES : 2;   // pieces of 16 bytes; of them in flight, from both rows
+  at += (size_t)share * (PIECES * 16);
 #pragma unroll
   for (int g = 0; g < G; ++g) sum[g] = 0.;
 #pragma unroll
@@ -105,45 +105,49 @@ __device__ __forceinline__ void quarter_score(const char* at, int quarter, const
         const double lo = (double)fminf(a, b), hi = (double)fmaxf(a, b);
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-          const double2 h = sh_q[g][quarter * CH + (j0 + j) * EPL + e];
+          const double2 h = sh_q[g][share * CH + (j0 + j) * EPL + e];
           sum[g] = fma(hi, h.y, fma(lo, h.x, sum[g]));
         }
       }
   }
 }
 
-// The quarters' sums of the lane's block -> its score.
-template <int G>
-__device__ __forceinline__ float joined_score(const double (&part)[WAVES][G][64]) {
+// The shares' sums of the lane's block -> its score.
+template <int G, int SHARES>
+__device__ __forceinline__ float joined_score(const double (&part)[SHARES][G][64]) {
   const int lane = threadIdx.x & 63;
   double best = 0.;
 #pragma unroll
   for (int g = 0; g < G; ++g) {
-    const double t = (part[0][g][lane] + part[1][g][lane]) + (part[2][g][lane] + part[3][g][lane]);
+    double t = part[0][g][lane];
+#pragma unroll
+    for (int s = 1; s < SHARES; ++s) t += part[s][g][lane];
     best = g == 0 ? t : fmax(best, t);
   }
   return (float)best;
 }
 
-// Grid (groups of 64 blocks, units).
+// Grid (groups of 64 blocks, units).  Lane = block, wave = an eighth of the channels: what bounds it are the chains of 64-bit products behind the queries' LDS
+// reads, and more waves have shorter ones (whole steps of 128 units x 440 blocks by 2 | 4 | 8 | 16 waves, us: 73.7 | 71.4 | 68.9 | 70.7).
+constexpr int SCORE_SHARES = 8;
 template <typename DT, int D, int G>
-__global__ __launch_bounds__(WG) void corm_block_score_kernel(const char* q, const char* bounds, const int32_t* lens, float* scores,
+__global__ __launch_bounds__(64 * SCORE_SHARES) void corm_block_score_kernel(const char* q, const char* bounds, const int32_t* lens, float* scores,
                                                               int Lcap, int nblk) {
   constexpr int ROWB = D * DT::ESZ;
   __shared__ double2 sh_q[G][D];
-  __shared__ double sh_part[WAVES][G][64];
+  __shared__ double sh_part[SCORE_SHARES][G][64];
   const int unit = blockIdx.y, lane = threadIdx.x & 63, wv = threadIdx.x >> 6;
   const int L = min(max(lens[unit], 0), Lcap), used = (L + QBLK - 1) / QBLK;
   const int blk = blockIdx.x * 64 + lane;
   if ((int)blockIdx.x * 64 >= used) return;
-  stage_signed_q<DT, D, G, WG>(q + (size_t)unit * G * ROWB, sh_q);
+  stage_signed_q<DT, D, G, 64 * SCORE_SHARES>(q + (size_t)unit * G * ROWB, sh_q);
   __syncthreads();
   double sum[G];
-  quarter_score<DT, D, G>(bounds + ((size_t)unit * nblk + min(blk, used - 1)) * 2 * ROWB, wv, sh_q, sum);
+  share_score<DT, D, G, SCORE_SHARES>(bounds + ((size_t)unit * nblk + min(blk, used - 1)) * 2 * ROWB, wv, sh_q, sum);
 #pragma unroll
   for (int g = 0; g < G; ++g) sh_part[wv][g][lane] = sum[g];
   __syncthreads();
-  if (wv == 0 && blk < used) scores[(size_t)unit * nblk + blk] = joined_score<G>(sh_part);
+  if (wv == 0 && blk < used) scores[(size_t)unit * nblk + blk] = joined_score<G, SCORE_SHARES>(sh_part);
 }
 
 // The choice of a unit from the order_keys of its blocks below `open` (key(i)), by a workgroup of NT threads.
@@ -222,12 +226,12 @@ __global__ __launch_bounds__(CHOOSE_WG) void corm_block_choose_kernel(const char
     __syncthreads();
     if (grp * 64 < open) {   // (uniform over the wave)
       double sum[G];
-      quarter_score<DT, D, G>(bounds + ((size_t)unit * nblk + min(blk, open - 1)) * 2 * ROWB, quarter, sh_q, sum);
+      share_score<DT, D, G, WAVES>(bounds + ((size_t)unit * nblk + min(blk, open - 1)) * 2 * ROWB, quarter, sh_q, sum);
 #pragma unroll
       for (int g = 0; g < G; ++g) sh_part[grp][quarter][g][lane] = sum[g];
     }
     __syncthreads();
-    if (quarter == 0 && blk < open) sh_key[blk] = order_key(joined_score<G>(sh_part[grp]));
+    if (quarter == 0 && blk < open) sh_key[blk] = order_key(joined_score<G, WAVES>(sh_part[grp]));
     __syncthreads();
   }
   pick_blocks<CHOOSE_WG>(used, nsel, nlast, blocks + (size_t)unit * nsel, [&](int i) { return sh_key[i]; }, sh, sh_cnt);

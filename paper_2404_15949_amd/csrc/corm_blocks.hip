@@ -234,7 +234,7 @@ int corm_block_select(const corm_desc* desc, const void* q, const void* bounds, 
         hipLaunchKernelGGL((corm_block_choose_kernel<T, D, G>), dim3(units), dim3(CHOOSE_WG), 0, s, qc, bc, lens, blocks, desc->Lcap, nblk,
                            nsel, nlast);
       else
-        hipLaunchKernelGGL((corm_block_score_kernel<T, D, G>), dim3((nblk + 63) / 64, units), dim3(WG), 0, s, qc, bc, lens, scores,
+        hipLaunchKernelGGL((corm_block_score_kernel<T, D, G>), dim3((nblk + 63) / 64, units), dim3(64 * SCORE_SHARES), 0, s, qc, bc, lens, scores,
                            desc->Lcap, nblk);
       return launch_status();
     });
