@@ -403,6 +403,23 @@ def test_evict_mask_weight(units, cap, r, budget):
         assert keep[u, 0].tolist() == ref.kept(w[u, 0], L, r, budget) + [9] * (cap - L), (u, L)
 
 
+def test_evict_mask_weight_of_many_long_units():
+    """So many units of more slots than a workgroup holds that each is decided by one workgroup, from memory: eight of them, over and over."""
+    kinds, units, cap, r, budget = 8, 704, 20001, 9, 6000
+    g = _gen(17)
+    w = torch.exp(3 * torch.randn(kinds, 1, cap, generator=g)) * (torch.rand(kinds, 1, cap, generator=g) > 0.2)
+    w[1] = 0.25
+    w[2] = (w[2] * 4).round() / 4
+    lens = torch.tensor([cap, cap, cap - 1, 12345, budget, budget + 1, 0, r], dtype=torch.int32)
+    desc = corm.make_desc(units, 1, 1, 64, cap, cap, 1, r, "f32")
+    keep = torch.full((units, 1, cap), 9, dtype=torch.uint8, device=DEV)
+    corm.corm_evict_mask_weight(desc, w.repeat(units // kinds, 1, 1).to(DEV), lens.repeat(units // kinds).to(DEV), budget, keep, _ws(desc))
+    for u in range(kinds):
+        L = int(lens[u])
+        want = torch.tensor(ref.kept(w[u, 0], L, r, budget) + [9] * (cap - L), dtype=torch.uint8)
+        assert (keep[u::kinds, 0].cpu() == want).all(), (u, L)
+
+
 # ---------------------------------------------------------------- together, as they would be used
 
 def _layer(B, Hq, Hkv, d, cap, dtype, P, g, r=8):
