@@ -31,7 +31,9 @@ int blocks_of(const corm_desc* d) { return (d->Lcap + QBLK - 1) / QBLK; }
 int max_parts(const corm_desc* d) { return std::max((blocks_of(d) + 3) / 4, 128) + 1; }
 int max_listed(const corm_desc* d) { return std::max(blocks_of(d), 512); }
 
-// Splits of a unit in the eviction decision of few long units, 0 where a workgroup takes a unit alone.
+// Splits of a unit in the eviction decision of long units, 0 where a workgroup takes a unit alone: where it can hold the unit's keys.  Us, one workgroup | splits:
+// 8, 128 and 512 units x 9000 slots 9.7 | 14.1, 10.1 | 16.4 and 15.9 | 31.5, x 16000 14.4 | 13.8, 15.8 | 17.3 and 23.1 | 33.0; keys from memory
+// in every round | splits: 8, 512 and 2000 x 20000 22 | 14, 40 | 42 and 169 | 157, 256 x 40000 69 | 42, 256 x 100000 185 | 101, 8 x 500000 530 | 29.
 struct EvictSplits {
   int splits, slots;
   size_t listed_off, counts_off, digit_off, total;
@@ -42,7 +44,6 @@ EvictSplits evict_splits(const corm_desc* d) {
   if (d->Lcap <= EVW_KEYS) return e;
   e.slots = std::max(EVW_SPLIT, ((d->Lcap + 63) / 64 + EVW_WG - 1) / EVW_WG * EVW_WG);
   e.splits = (d->Lcap + e.slots - 1) / e.slots;
-  if (units * e.splits > EVW_MOST_SPLITS) return EvictSplits{};
   e.listed_off = align_up(units * e.splits * EVW_COUNTS * sizeof(uint32_t), 256);
   e.counts_off = e.listed_off + align_up(units * d->Lcap * sizeof(uint32_t), 256);
   e.digit_off = e.counts_off + align_up(units * e.splits * sizeof(uint32_t), 256);
@@ -302,9 +303,8 @@ int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int
   hipStream_t s = (hipStream_t)stream;
   const EvictSplits e = evict_splits(desc);
   if (e.splits == 0) {
-    const bool held = desc->Lcap <= EVW_KEYS;
-    hipLaunchKernelGGL(corm_evict_weight_kernel, dim3(units), dim3(EVW_WG), held ? (size_t)desc->Lcap * sizeof(uint32_t) : 0, s, weight, lens,
-                       keep, desc->Lcap, desc->r, budget, (int)held);
+    hipLaunchKernelGGL(corm_evict_weight_kernel, dim3(units), dim3(EVW_WG), (size_t)desc->Lcap * sizeof(uint32_t), s, weight, lens, keep,
+                       desc->Lcap, desc->r, budget);
     return launch_status();
   }
   char* ws = reinterpret_cast<char*>(workspace);

@@ -27,8 +27,8 @@ __device__ __forceinline__ void for_keys(const float* w, int first, int end, con
 // Grid (units).  Bound by the chain of latencies: keys, two rounds of digits (about 2.5 us each: clear, count, find), the listed ones, the decision; 512 units
 // x 4352 slots 9 us (10 MB).
 __global__ __launch_bounds__(EVW_WG) void corm_evict_weight_kernel(const float* weight, const int32_t* lens, uint8_t* keep, int Lcap,
-                                                                   int r, int budget, int held) {
-  extern __shared__ uint32_t sh_key[];   // held: the unit's keys
+                                                                   int r, int budget) {
+  extern __shared__ uint32_t sh_key[];   // the unit's keys
   __shared__ CutLds<EVW_WG, EVW_BITS> sh;
   const int unit = blockIdx.x, tid = threadIdx.x;
   const int L = min(max(lens[unit], 0), Lcap);
@@ -41,12 +41,12 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_weight_kernel(const float* 
   const int open = L - r, k = budget - r;   // (0 <= k < open)
   Cut cut = {0xffffffffu, 0u};
   auto item = [&](int i, uint32_t& x, uint32_t& slot) {
-    x = held ? sh_key[i] : order_key(w[i]);
+    x = sh_key[i];
     slot = (uint32_t)i;
     return true;
   };
   if (k > 0) {
-    if (held) for_keys(w, 0, open, [&](int i, uint32_t x) { sh_key[i] = x; });   // (a thread asks for its own)
+    for_keys(w, 0, open, [&](int i, uint32_t x) { sh_key[i] = x; });   // (a thread asks for its own)
     cut = find_cut<EVW_WG, EVW_BITS, 32>(open, (uint32_t)k, item, sh);
   }
   for (int i = tid; i < L; i += EVW_WG) {
@@ -56,7 +56,7 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_weight_kernel(const float* 
   }
 }
 
-// Few long units: three launches, of which the first two share a unit among workgroups ("splits" of split_slots slots).
+// Long units: three launches, of which the first two share a unit among workgroups ("splits" of split_slots slots).
 //   count    the top 11 bits of a split's keys, and the top 6 of those (so that the next launch reads a few kilobytes of a unit's counts and not
 //            8 for every split: the dies' caches do not see each other's, and 16 units of 131072 slots took 12 us there)
 //   part     which of these digits the cut lies in; slots with a larger or a smaller one are decided, the others (as a rule a few percent)
@@ -75,7 +75,7 @@ struct EvictLongArgs {
 };
 constexpr int SETTLE_KEYS = 8192;
 constexpr int EVW_COARSE = 64, EVW_FINE = (1 << EVW_BITS) / EVW_COARSE, EVW_COUNTS = EVW_COARSE + (1 << EVW_BITS);   // counts of a split
-constexpr int EVW_SPLIT = 8192, EVW_MOST_SPLITS = 2048;   // slots of a split, at least (64 splits at most); splits of all units
+constexpr int EVW_SPLIT = 8192;   // slots of a split, at least (64 splits at most)
 
 __global__ __launch_bounds__(EVW_WG) void corm_evict_count_kernel(const EvictLongArgs a) {
   __shared__ uint32_t sh_hist[1 << EVW_BITS];

@@ -404,7 +404,7 @@ def test_evict_mask_weight(units, cap, r, budget):
 
 
 def test_evict_mask_weight_of_many_long_units():
-    """So many units of more slots than a workgroup holds that each is decided by one workgroup, from memory: eight of them, over and over."""
+    """Many units of more slots than a workgroup holds: eight of them, over and over."""
     kinds, units, cap, r, budget = 8, 704, 20001, 9, 6000
     g = _gen(17)
     w = torch.exp(3 * torch.randn(kinds, 1, cap, generator=g)) * (torch.rand(kinds, 1, cap, generator=g) > 0.2)
