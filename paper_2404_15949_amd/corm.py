@@ -510,13 +510,15 @@ class LayerState:
             self.blocks_workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
 
     def preload(self, K0: torch.Tensor, V0: torch.Tensor) -> None:
-        """Copy n prompt keys/values [B,Hkv,n,d] into slots 0..n-1 (positions 0..n-1, never important yet)."""
+        """Copy n prompt keys/values [B,Hkv,n,d] into slots 0..n-1 (positions 0..n-1, never important yet, accounts empty)."""
         n = K0.shape[2]
         self.K[:, :, :n].copy_(K0)
         self.V[:, :, :n].copy_(V0)
         self.pos[:, :, :n] = torch.arange(n, dtype=torch.int32, device=self.pos.device)
         self.last_hit[:, :, :n] = 0
         self.lens.fill_(n)
+        if self.weight is not None:
+            self.weight.zero_()
 
     def step_attend(self, q, k_new, v_new, t, t_first, stream=None, workspace=None, opts=None) -> None:
         corm_step_attend(self.desc, q, k_new, v_new, self.K, self.V, self.lens, self.pos, self.last_hit, t, t_first,

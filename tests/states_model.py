@@ -1,0 +1,213 @@
+"""A plain model of what a LayerState holds and does (rows, positions, accounts, bounds, 64-bit arithmetic), which follows its steps and
+checks them; and plain forms of the library's calls on host tensors, so that the state's own bookkeeping is tested without a device."""
+import math
+
+import torch
+
+from paper_2404_15949_amd import corm
+from tests import operators_ref as ref
+
+
+def rows(g, dtype, *shape, scale=1.0):
+    return (torch.randn(*shape, generator=g) * scale).to({"f32": torch.float32, "bf16": torch.bfloat16}[dtype])
+
+
+def plain_library(monkeypatch):
+    """The calls a state makes, as plain forms on host tensors, with the layouts and rules corm.h documents.  Returns the names of the calls made."""
+    made = []
+
+    def units(desc):
+        return [(b, h) for b in range(desc.B) for h in range(desc.Hkv)]
+
+    def append(desc, K, V, lens, pos, last_hit, k_new, v_new, t, status=None, stream=None, check=True):
+        made.append("append")
+        for b, h in units(desc):
+            i = int(lens[b, h])
+            if i >= desc.Lcap:
+                status |= corm.CORM_DEV_UNIT_FULL
+                continue
+            K[b, h, i], V[b, h, i], pos[b, h, i], last_hit[b, h, i] = k_new[b, h], v_new[b, h], int(t[b]) - 1, 0
+            lens[b, h] = i + 1
+
+    def block_bounds(desc, K, lens, bounds, newest=0, stream=None, check=True):
+        made.append(("bounds", newest))
+        for b, h in units(desc):
+            n = int(lens[b, h])
+            first = max(n - newest, 0) // ref.BLK if newest else 0
+            x = ref.bounds_of(K[b, h, :n])
+            bounds[b, h, first:x.shape[0]] = x[first:]
+
+    def block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace, workspace_bytes=None, stream=None, check=True):
+        made.append("select")
+        G = desc.Hq // desc.Hkv
+        for b, h in units(desc):
+            got = ref.choose(q[b, h * G:(h + 1) * G], bounds[b, h, :(int(lens[b, h]) + 63) // 64], nsel, nlast)
+            blocks[b, h] = torch.tensor(got + [-1] * (nsel - len(got)), dtype=torch.int32)
+
+    def attend(desc, q, K, V, b, h, slots, out):
+        G = desc.Hq // desc.Hkv
+        o, p = ref.attention(q[b, h * G:(h + 1) * G].double(), K[b, h, slots].double(), V[b, h, slots].double(), 1.0 / math.sqrt(desc.d))
+        out[b, h * G:(h + 1) * G] = o.float()
+        return p
+
+    def block_attend(desc, q, K, V, lens, blocks, nsel, out, workspace, workspace_bytes=None, status=None, stream=None, check=True):
+        made.append("block_attend")
+        for b, h in units(desc):
+            slots = [s for i in blocks[b, h].tolist() if i >= 0 for s in range(64 * i, min(64 * i + 64, int(lens[b, h])))]
+            attend(desc, q, K, V, b, h, slots, out)
+
+    def weigh(desc, q, K, V, lens, weight_in, weight, out, workspace, workspace_bytes=None, status=None, stream=None, check=True, opts=None):
+        made.append("weigh")
+        for b, h in units(desc):
+            n = int(lens[b, h])
+            p = attend(desc, q, K, V, b, h, list(range(n)), out)
+            weight[b, h, :n] = (weight_in[b, h, :n].double() + p.sum(0)).float()
+
+    def evict_mask(desc, weight, lens, budget, keep, workspace, workspace_bytes=None, stream=None, check=True):
+        made.append("mask")
+        for b, h in units(desc):
+            n = int(lens[b, h])
+            keep[b, h, :n] = torch.tensor(ref.kept(weight[b, h], n, desc.r, budget), dtype=torch.uint8)
+
+    def gather(desc, arrays, lens, keep):
+        for b, h in units(desc):
+            idx = keep[b, h, :int(lens[b, h])].nonzero().flatten()
+            for x in arrays:
+                x[b, h, :len(idx)] = x[b, h, idx].clone()
+            lens[b, h] = len(idx)
+
+    def compact(desc, K, V, pos, last_hit, lens, keep, kept_idx=None, workspace=None, workspace_bytes=None, stream=None, check=True):
+        made.append("compact")
+        gather(desc, (K, V, pos, last_hit), lens, keep)
+
+    def evict_first(desc, K, V, lens, pos, last_hit):      # a cut that is no rule's: the lowest slot goes
+        keep = torch.ones(desc.B, desc.Hkv, desc.Lcap, dtype=torch.uint8)
+        keep[:, :, 0] = 0
+        gather(desc, (K, V, pos, last_hit), lens, keep)
+
+    def decode_step(desc, q, k_new, v_new, K, V, lens, pos, last_hit, t, t_first, *rest, status=None, stream=None, opts=None):
+        made.append("step")
+        append(desc, K, V, lens, pos, last_hit, k_new, v_new, t, status)
+        evict_first(desc, K, V, lens, pos, last_hit)
+
+    def prefill_seed(desc, q_tail, m, K, V, lens, pos, last_hit, *rest, status=None, stream=None):
+        made.append("seed")
+        evict_first(desc, K, V, lens, pos, last_hit)
+
+    def decode_step_lazy(desc, q, k_new, v_new, K, V, lens, live, pos, last_hit, t, t_first, *rest, status=None, stream=None, opts=None):
+        made.append("lazy")
+        append(desc, K, V, lens, pos, last_hit, k_new, v_new, t, status)
+        live[:, :, 0] &= -2                                # slot 0 dies
+
+    for name, f in (("corm_append", append), ("corm_block_bounds", block_bounds), ("corm_block_select", block_select),
+                    ("corm_block_attend", block_attend), ("corm_decode_attend_weigh", weigh), ("corm_evict_mask_weight", evict_mask),
+                    ("corm_compact", compact), ("corm_decode_step", decode_step), ("corm_prefill_seed", prefill_seed),
+                    ("corm_decode_step_lazy", decode_step_lazy)):
+        monkeypatch.setattr(corm, name, f)
+    monkeypatch.setattr(corm, "_device", lambda: -1)
+    return made
+
+
+class Follower:
+    """A LayerState and, beside it, what its documented steps make of the same rows; a step is made in both and compared."""
+
+    def __init__(self, g, B, Hq, Hkv, d, cap, dtype, r=8, device="cpu", tcap=None, w=4, **wants):
+        self.g, self.B, self.Hq, self.Hkv, self.d, self.dtype, self.r, self.device = g, B, Hq, Hkv, d, dtype, r, device
+        extra = {"workspace": torch.empty(256, dtype=torch.uint8)} if device == "cpu" else {}
+        self.st = corm.LayerState(B, Hq, Hkv, d, cap, tcap or cap, w, r, dtype, device=device, want_ring=False, **wants, **extra)
+        self.at = [(b, h) for b in range(B) for h in range(Hkv)]
+        self.t = 0
+
+    def preload(self, P):
+        K, V = rows(self.g, self.dtype, self.B, self.Hkv, P, self.d), rows(self.g, self.dtype, self.B, self.Hkv, P, self.d)
+        self.st.preload(K.to(self.device), V.to(self.device))
+        self.K = {(b, h): list(K[b, h]) for b, h in self.at}
+        self.V = {(b, h): list(V[b, h]) for b, h in self.at}
+        self.pos = {u: list(range(P)) for u in self.at}
+        self.weight = {u: torch.zeros(P, dtype=torch.float64) for u in self.at}
+        self.t = P
+
+    def token(self):
+        """A step's query, row and step number, and the row in the model."""
+        q, k, v = (rows(self.g, self.dtype, self.B, n, self.d, scale=s) for n, s in ((self.Hq, 2.0), (self.Hkv, 1.0), (self.Hkv, 1.0)))
+        self.t += 1
+        for b, h in self.at:
+            self.K[b, h].append(k[b, h])
+            self.V[b, h].append(v[b, h])
+            self.pos[b, h].append(self.t - 1)
+            self.weight[b, h] = torch.cat([self.weight[b, h], torch.zeros(1, dtype=torch.float64)])
+        return q, [x.to(self.device) for x in (q, k, v)] + [torch.full((self.B,), self.t, dtype=torch.int32, device=self.device)]
+
+    def heads(self, u):
+        G = self.Hq // self.Hkv
+        return slice(u[1] * G, (u[1] + 1) * G)
+
+    def check_out(self, q, u, slots):
+        sm, x = 1.0 / math.sqrt(self.d), q[u[0], self.heads(u)].double()
+        K, V = (torch.stack([m[u][i] for i in slots]).double() for m in (self.K, self.V))
+        want, p = ref.attention(x, K, V, sm)
+        err = float((self.st.out[u[0], self.heads(u)].cpu().double() - want).abs().max())
+        assert err <= ref.out_error(x, K, V, sm), (u, err)
+        return p, ref.weight_error(x, K, sm) + (len(slots) + 8) * ref.EPS
+
+    def check_rows(self):
+        """Rows, positions and, where the state has them, bounds, as the model has them."""
+        st = self.st
+        K, V, pos, lens = (x.cpu() for x in (st.K, st.V, st.pos, st.lens))
+        for u in self.at:
+            n = len(self.K[u])
+            assert int(lens[u]) == n and pos[u][:n].tolist() == self.pos[u], u
+            Kr = torch.stack(self.K[u])
+            assert torch.equal(K[u][:n], Kr) and torch.equal(V[u][:n], torch.stack(self.V[u])), u
+            if st.bounds is not None:
+                want = ref.bounds_of(Kr)
+                assert torch.equal(st.bounds[u][:want.shape[0]].cpu(), want), u
+        assert int(st.status) == 0
+
+    def check_weight(self, u, p, e):
+        """The accounts are within fp32 of the model's, which then takes them over (they decide)."""
+        n = len(self.K[u])
+        got = self.st.weight[u][:n].cpu().double()
+        assert bool(((got - self.weight[u]).abs() <= p * e + (self.Hq + 1) * ref.EPS * self.weight[u]).all()), u
+        self.weight[u] = got
+
+    def weigh(self, budget=None):
+        q, args = self.token()
+        self.st.step_weigh(*args, budget)
+        for u in self.at:
+            n = len(self.K[u])
+            p, e = self.check_out(q, u, range(n))
+            p = p.sum(0)
+            self.weight[u] = self.weight[u] + p
+            if budget is not None and n > budget:
+                idx = self.st.weight_keep[u][:n].cpu().nonzero().flatten().tolist()
+                assert len(idx) == budget and set(range(n - self.r, n)) <= set(idx)
+                old, gone = self.weight[u][:n - self.r], [i for i in range(n - self.r) if i not in set(idx)]
+                assert float(old[gone].max()) <= float(old[[i for i in idx if i < n - self.r]].min()) * (1 + 4 * e)
+                for m in (self.K, self.V, self.pos):
+                    m[u] = [m[u][i] for i in idx]
+                self.weight[u], p = self.weight[u][idx], p[idx]
+            self.check_weight(u, p, e)
+        self.check_rows()
+
+    def blocks(self, nsel, nlast):
+        q, args = self.token()
+        self.st.step_blocks(*args, nsel, nlast)
+        for u in self.at:
+            n = len(self.K[u])
+            want = ref.choose(q[u[0], self.heads(u)], ref.bounds_of(torch.stack(self.K[u])), nsel, nlast)
+            assert self.st.blocks[u].tolist() == want + [-1] * (nsel - len(want)), u
+            self.check_out(q, u, [i for w in want for i in range(64 * w, min(64 * w + 64, n))])
+            if self.st.weight is not None:
+                assert torch.equal(self.st.weight[u][:n].cpu().double(), self.weight[u]), u
+        self.check_rows()
+
+    def adopt(self):
+        """After a step whose rule is another test's: the rows that stayed, by their positions."""
+        st = self.st
+        K, V, pos, lens = (x.cpu() for x in (st.K, st.V, st.pos, st.lens))
+        for u in self.at:
+            n = int(lens[u])
+            self.pos[u] = pos[u][:n].tolist()
+            self.K[u], self.V[u] = list(K[u][:n]), list(V[u][:n])
+            self.weight[u] = torch.zeros(n, dtype=torch.float64)
