@@ -510,13 +510,14 @@ class LayerState:
             self.blocks_workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
 
     def preload(self, K0: torch.Tensor, V0: torch.Tensor) -> None:
-        """Copy n prompt keys/values [B,Hkv,n,d] into slots 0..n-1 (positions 0..n-1, never important yet, accounts empty)."""
+        """Copy n prompt keys/values [B,Hkv,n,d] into slots 0..n-1 (positions 0..n-1, never important yet, none dead, accounts empty)."""
         n = K0.shape[2]
         self.K[:, :, :n].copy_(K0)
         self.V[:, :, :n].copy_(V0)
         self.pos[:, :, :n] = torch.arange(n, dtype=torch.int32, device=self.pos.device)
         self.last_hit[:, :, :n] = 0
         self.lens.fill_(n)
+        self.live.fill_(-1)
         if self.weight is not None:
             self.weight.zero_()
 

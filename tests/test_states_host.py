@@ -24,3 +24,14 @@ def test_a_second_prompt_starts_with_empty_accounts(monkeypatch):
     f.preload(20)
     assert not f.st.weight.any()
     f.weigh()
+
+
+def test_a_second_prompt_has_no_dead_slots(monkeypatch):
+    plain_library(monkeypatch)
+    f = _follower(2)
+    f.preload(40)
+    q, args = f.token()
+    f.st.step_lazy(*args, None)
+    assert (f.st.live != -1).any()
+    f.preload(50)
+    assert (f.st.live == -1).all()
