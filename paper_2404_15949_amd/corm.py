@@ -7,6 +7,7 @@ torch is used for device memory and streams: tensors are passed as their
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from typing import Optional
@@ -127,6 +128,13 @@ def _stream(stream) -> Optional[int]:
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
+
+
+def _as_current(stream):
+    """For torch's own operations beside a call that is given `stream`."""
+    if stream is None:
+        return contextlib.nullcontext()
+    return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
 
 
 # Launch options of the attend / step wrappers below when a call passes none: a setting of this BINDING (the
@@ -505,6 +513,7 @@ class LayerState:
         self._blocks = {}
         self.weight = torch.zeros(B, Hkv, Lcap, dtype=torch.float32, device=device) if want_weight else None
         self.weight_keep = torch.zeros(B, Hkv, Lcap, dtype=torch.uint8, device=device) if want_weight else None
+        self._rule = None   # what a state with accounts has evicted by since its prompt: "hits" or "weight"
         self.blocks_workspace = None
         if want_bounds or want_weight:
             self.blocks_workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
@@ -520,33 +529,52 @@ class LayerState:
         self.live.fill_(-1)
         if self.weight is not None:
             self.weight.zero_()
+        self._rule = None
+
+    def _check_rule(self, rule: str) -> None:
+        """CORM's steps move rows without their accounts, step_weigh without last_hit, so a state with accounts evicts by one of them from a prompt
+        to the next preload.  (A graph counts where it is captured: one of the other kind is not to be replayed behind a preload.)"""
+        if self.weight is not None and self._rule not in (None, rule):
+            raise RuntimeError("a state with accounts evicts by hits (step, step_lazy, step_attend, step_evict) or by weight (step_weigh), "
+                               "not by both: preload it, or make another one")
 
     def step_attend(self, q, k_new, v_new, t, t_first, stream=None, workspace=None, opts=None) -> None:
+        self._check_rule("hits")
         corm_step_attend(self.desc, q, k_new, v_new, self.K, self.V, self.lens, self.pos, self.last_hit, t, t_first,
                          self.ring, self.out, self.keep, self.workspace if workspace is None else workspace,
                          status=self.status, stream=stream, opts=opts)
+        self._rule = "hits"
 
     def step_evict(self, stream=None, workspace=None) -> None:
+        self._check_rule("hits")
         corm_step_evict(self.desc, self.K, self.V, self.lens, self.pos, self.last_hit, self.kept_idx,
                         self.workspace if workspace is None else workspace, stream=stream)
+        self._rule = "hits"
 
     def step(self, q, k_new, v_new, t, t_first, stream=None, opts=None) -> None:
+        self._check_rule("hits")
         corm_decode_step(self.desc, q, k_new, v_new, self.K, self.V, self.lens, self.pos, self.last_hit, t, t_first,
                          self.ring, self.out, self.keep, self.kept_idx, self.workspace, status=self.status,
                          stream=stream, opts=opts)
+        self._rule = "hits"
 
     def step_lazy(self, q, k_new, v_new, t, t_first, dead_num=1, dead_den=4, stream=None, workspace=None,
                   opts=None) -> None:
+        self._check_rule("hits")
         corm_decode_step_lazy(self.desc, q, k_new, v_new, self.K, self.V, self.lens, self.live, self.pos,
                               self.last_hit, t, t_first, self.ring, self.out, self.keep, self.nlive, dead_num,
                               dead_den, self.workspace if workspace is None else workspace, status=self.status,
                               stream=stream, opts=opts)
+        self._rule = "hits"
 
     def prefill_seed(self, q_tail, t, t_first, stream=None, workspace=None) -> None:
-        """q_tail [B,Hq,m,d]; the cache must already hold the whole prompt (preload)."""
+        """q_tail [B,Hq,m,d]; the cache must already hold the whole prompt (preload).  Accounts are empty behind it."""
         corm_prefill_seed(self.desc, q_tail, q_tail.shape[2], self.K, self.V, self.lens, self.pos, self.last_hit, t,
                           t_first, self.ring, self.keep, self.kept_idx,
                           self.workspace if workspace is None else workspace, status=self.status, stream=stream)
+        if self.weight is not None:
+            with _as_current(stream):
+                self.weight.zero_()
 
     def renew_bounds(self, newest=0, stream=None) -> None:
         """Bounds of the blocks' keys (all of them, or those of the newest slots): after a prompt, and after rows have moved."""
@@ -568,9 +596,11 @@ class LayerState:
 
     def step_weigh(self, q, k_new, v_new, t, budget=None, stream=None) -> None:
         """One decode step of eviction by accumulated attention weight: append, attend and account (self.weight), and with a budget cut every
-        longer unit to it (the r newest slots and the heaviest others; self.weight_keep: the slots that stayed)."""
+        longer unit to it (the r newest slots and the heaviest others; self.weight_keep: the slots that stayed).  last_hit is left behind."""
         if self.weight is None:
             raise RuntimeError("made without want_weight")
+        self._check_rule("weight")
+        self._rule = "weight"
         account = self.weight   # 4-byte entries: append and the gather carry them in the place of last_hit
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, account, k_new, v_new, t, self.status, stream=stream)
         corm_decode_attend_weigh(self.desc, q, self.K, self.V, self.lens, account, account, self.out, self.workspace,

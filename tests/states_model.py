@@ -167,7 +167,7 @@ class Follower:
     def check_weight(self, u, p, e):
         """The accounts are within fp32 of the model's, which then takes them over (they decide)."""
         n = len(self.K[u])
-        got = self.st.weight[u][:n].cpu().double()
+        got = self.st.weight[u][:n].cpu().double()         # (a copy: another type)
         assert bool(((got - self.weight[u]).abs() <= p * e + (self.Hq + 1) * ref.EPS * self.weight[u]).all()), u
         self.weight[u] = got
 
@@ -205,7 +205,7 @@ class Follower:
     def adopt(self):
         """After a step whose rule is another test's: the rows that stayed, by their positions."""
         st = self.st
-        K, V, pos, lens = (x.cpu() for x in (st.K, st.V, st.pos, st.lens))
+        K, V, pos, lens = (x.cpu().clone() for x in (st.K, st.V, st.pos, st.lens))
         for u in self.at:
             n = int(lens[u])
             self.pos[u] = pos[u][:n].tolist()

@@ -35,3 +35,57 @@ def test_a_second_prompt_has_no_dead_slots(monkeypatch):
     assert (f.st.live != -1).any()
     f.preload(50)
     assert (f.st.live == -1).all()
+
+
+def test_a_state_with_accounts_evicts_by_one_rule(monkeypatch):
+    """CORM's steps move rows without their accounts, steps by weight without last_hit: the second kind is refused, before anything is done."""
+    made = plain_library(monkeypatch)
+    f = _follower(3, want_weight=True)
+    f.preload(40)
+    q, args = f.token()
+
+    def corms():
+        st = f.st
+        return (lambda: st.step(*args, None), lambda: st.step_lazy(*args, None), lambda: st.step_attend(*args, None), lambda: st.step_evict())
+
+    for rule in ("weight", "hits"):
+        for first in (lambda: f.st.step_weigh(*args),) if rule == "weight" else corms()[:2]:
+            f.preload(40)
+            first()
+            made.clear()
+            for second in corms() if rule == "weight" else (lambda: f.st.step_weigh(*args), lambda: f.st.step_weigh(*args, 20)):
+                with pytest.raises(RuntimeError, match="accounts"):
+                    second()
+            assert made == []
+    f = _follower(3)                    # without accounts there is nothing to lose
+    f.preload(40)
+    f.st.step(*args, None)
+    f.st.step_lazy(*args, None)
+
+
+def test_a_refused_step_takes_no_rule(monkeypatch):
+    plain_library(monkeypatch)
+
+    def refuse(*a, **k):
+        raise corm.CormError(corm.CORM_EINVAL, "no")
+
+    monkeypatch.setattr(corm, "corm_decode_step", refuse)
+    f = _follower(4, want_weight=True)
+    f.preload(40)
+    q, args = f.token()
+    with pytest.raises(corm.CormError):
+        f.st.step(*args, None)
+    f.preload(40)
+    f.weigh()
+
+
+def test_accounts_are_empty_behind_a_seeded_prompt(monkeypatch):
+    """Seeding evicts by hits and cannot move accounts: what was in them is another prompt's."""
+    plain_library(monkeypatch)
+    f = _follower(5, want_weight=True)
+    f.preload(40)
+    f.st.weight.fill_(3.0)
+    f.st.prefill_seed(rows(f.g, "f32", 2, 4, 4, 64), None, None)
+    f.adopt()
+    f.weigh()
+    f.weigh(budget=30)
