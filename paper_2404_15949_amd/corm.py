@@ -530,6 +530,14 @@ class LayerState:
         if self.weight is not None:
             self.weight.zero_()
         self._rule = None
+        if self.bounds is not None:
+            with torch.cuda.device_of(self.K):
+                self._rows_moved()
+
+    def _rows_moved(self, stream=None) -> None:
+        """Behind a call that moves rows, or may (which only the device knows): the bounds of what lies there now."""
+        if self.bounds is not None:
+            corm_block_bounds(self.desc, self.K, self.lens, self.bounds, 0, stream=stream)
 
     def _check_rule(self, rule: str) -> None:
         """CORM's steps move rows without their accounts, step_weigh without last_hit, so a state with accounts evicts by one of them from a prompt
@@ -550,6 +558,7 @@ class LayerState:
         corm_step_evict(self.desc, self.K, self.V, self.lens, self.pos, self.last_hit, self.kept_idx,
                         self.workspace if workspace is None else workspace, stream=stream)
         self._rule = "hits"
+        self._rows_moved(stream)
 
     def step(self, q, k_new, v_new, t, t_first, stream=None, opts=None) -> None:
         self._check_rule("hits")
@@ -557,6 +566,7 @@ class LayerState:
                          self.ring, self.out, self.keep, self.kept_idx, self.workspace, status=self.status,
                          stream=stream, opts=opts)
         self._rule = "hits"
+        self._rows_moved(stream)
 
     def step_lazy(self, q, k_new, v_new, t, t_first, dead_num=1, dead_den=4, stream=None, workspace=None,
                   opts=None) -> None:
@@ -575,16 +585,18 @@ class LayerState:
         if self.weight is not None:
             with _as_current(stream):
                 self.weight.zero_()
+        self._rows_moved(stream)
 
     def renew_bounds(self, newest=0, stream=None) -> None:
-        """Bounds of the blocks' keys (all of them, or those of the newest slots): after a prompt, and after rows have moved."""
+        """Bounds of the blocks' keys (all of them, or those of the newest slots): after rows were written by other means than the state's own
+        preload and steps, which keep them up."""
         if self.bounds is None:
             raise RuntimeError("made without want_bounds")
         corm_block_bounds(self.desc, self.K, self.lens, self.bounds, newest, stream=stream)
 
     def step_blocks(self, q, k_new, v_new, t, nsel, nlast=1, stream=None) -> None:
         """One decode step that attends to nsel blocks of 64 slots (the nlast newest and those with the highest score bounds): append,
-        the newest block's bounds, choice (self.blocks), attention.  Nothing is recorded or evicted.  renew_bounds() first, after the prompt."""
+        the newest block's bounds, choice (self.blocks), attention.  Nothing is recorded or evicted."""
         if self.bounds is None:
             raise RuntimeError("made without want_bounds")
         self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.K.device)
@@ -605,10 +617,14 @@ class LayerState:
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, account, k_new, v_new, t, self.status, stream=stream)
         corm_decode_attend_weigh(self.desc, q, self.K, self.V, self.lens, account, account, self.out, self.workspace,
                                  status=self.status, stream=stream)
-        if budget is not None:
+        if budget is None:
+            if self.bounds is not None:
+                self.renew_bounds(1, stream=stream)
+        else:
             corm_evict_mask_weight(self.desc, account, self.lens, budget, self.weight_keep, self.blocks_workspace, stream=stream)
             corm_compact(self.desc, self.K, self.V, self.pos, account, self.lens, self.weight_keep, self.kept_idx, self.workspace,
                          stream=stream)
+            self._rows_moved(stream)
 
 
 def _block_list(lists, B, Hkv, nsel, device) -> torch.Tensor:

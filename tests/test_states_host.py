@@ -89,3 +89,33 @@ def test_accounts_are_empty_behind_a_seeded_prompt(monkeypatch):
     f.adopt()
     f.weigh()
     f.weigh(budget=30)
+
+
+def test_bounds_follow_every_step(monkeypatch):
+    """The bounds of every block after a prompt, steps of other kinds that complete blocks, cuts and a second prompt: those of the rows that are there."""
+    plain_library(monkeypatch)
+    f = _follower(9, want_weight=True, want_bounds=True)
+    f.preload(60)
+    f.check_rows()
+    f.blocks(2, 1)
+    for _ in range(10):                  # over a block's end, without block steps between
+        f.weigh()
+    f.blocks(2, 1)
+    f.weigh(budget=66)                   # rows move
+    f.preload(130)
+    f.check_rows()
+    f.blocks(2, 1)
+
+
+def test_bounds_follow_corms_steps(monkeypatch):
+    plain_library(monkeypatch)
+    f = _follower(10, want_bounds=True)
+    f.preload(150)
+    f.st.prefill_seed(rows(f.g, "f32", 2, 4, 4, 64), None, None)
+    f.adopt()
+    f.check_rows()
+    for _ in range(3):
+        f.st.step(*f.token()[1], None)
+        f.adopt()
+        f.check_rows()
+    f.blocks(2, 1)
