@@ -513,6 +513,7 @@ class LayerState:
         self._blocks = {}
         self.weight = torch.zeros(B, Hkv, Lcap, dtype=torch.float32, device=device) if want_weight else None
         self.weight_keep = torch.zeros(B, Hkv, Lcap, dtype=torch.uint8, device=device) if want_weight else None
+        self._dead = False  # there may be dead slots (step_lazy)
         self._rule = None   # what a state with accounts has evicted by since its prompt: "hits" or "weight"
         self.blocks_workspace = None
         if want_bounds or want_weight:
@@ -529,7 +530,7 @@ class LayerState:
         self.live.fill_(-1)
         if self.weight is not None:
             self.weight.zero_()
-        self._rule = None
+        self._rule, self._dead = None, False
         if self.bounds is not None:
             with torch.cuda.device_of(self.K):
                 self._rows_moved()
@@ -575,7 +576,7 @@ class LayerState:
                               self.last_hit, t, t_first, self.ring, self.out, self.keep, self.nlive, dead_num,
                               dead_den, self.workspace if workspace is None else workspace, status=self.status,
                               stream=stream, opts=opts)
-        self._rule = "hits"
+        self._rule, self._dead = "hits", True
 
     def prefill_seed(self, q_tail, t, t_first, stream=None, workspace=None) -> None:
         """q_tail [B,Hq,m,d]; the cache must already hold the whole prompt (preload).  Accounts are empty behind it."""
@@ -599,6 +600,8 @@ class LayerState:
         the newest block's bounds, choice (self.blocks), attention.  Nothing is recorded or evicted."""
         if self.bounds is None:
             raise RuntimeError("made without want_bounds")
+        if self._dead:
+            raise RuntimeError("behind step_lazy a state may hold dead slots, which step_blocks would attend to: preload it, or use step")
         self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.K.device)
         ws = self.blocks_workspace
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, self.last_hit, k_new, v_new, t, self.status, stream=stream)

@@ -119,3 +119,18 @@ def test_bounds_follow_corms_steps(monkeypatch):
         f.adopt()
         f.check_rows()
     f.blocks(2, 1)
+
+
+def test_steps_that_know_no_dead_slots_are_refused_behind_deferred_compaction(monkeypatch):
+    """Attention over chosen blocks would read evicted keys, and the row it appends would be taken for dead."""
+    made = plain_library(monkeypatch)
+    f = _follower(11, want_bounds=True)
+    f.preload(100)
+    f.blocks(2, 1)
+    f.st.step_lazy(*f.token()[1], None)
+    made.clear()
+    with pytest.raises(RuntimeError, match="dead"):
+        f.st.step_blocks(*f.token()[1], 2)
+    assert made == []
+    f.preload(100)
+    f.blocks(2, 1)
