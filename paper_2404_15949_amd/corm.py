@@ -130,6 +130,10 @@ def _stream(stream) -> Optional[int]:
     return int(stream)
 
 
+def _capturing() -> bool:
+    return torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()
+
+
 def _as_current(stream):
     """For torch's own operations beside a call that is given `stream`."""
     if stream is None:
@@ -604,7 +608,12 @@ class LayerState:
             raise RuntimeError("behind step_lazy a state may hold dead slots, which step_blocks would attend to: preload it, or use step")
         self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.K.device)
         ws = self.blocks_workspace
-        corm_append(self.desc, self.K, self.V, self.lens, self.pos, self.last_hit, k_new, v_new, t, self.status, stream=stream)
+        # The new row's entry of what the state evicts by.  While it has evicted by neither, all accounts behind the rows are empty, so last_hit
+        # is the one to set; a graph may be replayed behind a cut by weight, so one that is captured sets the account and goes by that rule.
+        if self.weight is not None and self._rule is None and _capturing():
+            self._rule = "weight"
+        entry = self.weight if self._rule == "weight" else self.last_hit
+        corm_append(self.desc, self.K, self.V, self.lens, self.pos, entry, k_new, v_new, t, self.status, stream=stream)
         self.renew_bounds(1, stream=stream)
         corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, ws, stream=stream)
         corm_block_attend(self.desc, q, self.K, self.V, self.lens, self.blocks, nsel, self.out, ws, status=self.status, stream=stream)

@@ -134,3 +134,45 @@ def test_steps_that_know_no_dead_slots_are_refused_behind_deferred_compaction(mo
     assert made == []
     f.preload(100)
     f.blocks(2, 1)
+
+
+def test_a_row_of_a_block_step_starts_with_an_empty_account(monkeypatch):
+    """Behind a cut the slots from the new length on hold accounts of keys that moved or went."""
+    plain_library(monkeypatch)
+    f = _follower(6, want_weight=True, want_bounds=True)
+    f.preload(100)
+    f.weigh()
+    f.weigh(budget=70)
+    f.st.renew_bounds()
+    for _ in range(3):
+        f.blocks(2, 1)
+    f.weigh()
+    f.weigh(budget=66)
+
+
+def test_a_row_of_a_block_step_has_never_been_hit(monkeypatch):
+    """... of a state that evicts by hits: the slot's last_hit."""
+    plain_library(monkeypatch)
+    for wants in (dict(want_bounds=True), dict(want_bounds=True, want_weight=True)):
+        f = _follower(7, **wants)
+        f.preload(100)
+        q, args = f.token()
+        f.st.step(*args, None)
+        f.adopt()
+        f.st.last_hit.fill_(50)
+        f.st.renew_bounds()
+        f.blocks(2, 1)
+        assert (f.st.last_hit[:, :, 100] == 0).all() and (f.st.last_hit[:, :, 101] == 50).all()
+
+
+def test_a_captured_block_step_may_be_replayed_behind_a_cut(monkeypatch):
+    """What a graph holds cannot know of steps that come later: a block step captured on a state with accounts sets the new row's account."""
+    plain_library(monkeypatch)
+    monkeypatch.setattr(corm, "_capturing", lambda: True)
+    f = _follower(8, want_weight=True, want_bounds=True)
+    f.preload(100)
+    f.st.renew_bounds()
+    f.st.weight[:, :, 100:] = 5.0       # as a cut between capture and replay leaves it
+    f.blocks(2, 1)
+    with pytest.raises(RuntimeError, match="accounts"):
+        f.st.step(*f.token()[1], None)
