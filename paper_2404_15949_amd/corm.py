@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes
+import operator
 import os
 from typing import Optional
 
@@ -606,14 +607,16 @@ class LayerState:
             raise RuntimeError("made without want_bounds")
         if self._dead:
             raise RuntimeError("behind step_lazy a state may hold dead slots, which step_blocks would attend to: preload it, or use step")
+        _check_choice(self.desc, nsel, nlast)
+        _check_query(self.desc, q)
         self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.K.device)
         ws = self.blocks_workspace
         # The new row's entry of what the state evicts by.  While it has evicted by neither, all accounts behind the rows are empty, so last_hit
         # is the one to set; a graph may be replayed behind a cut by weight, so one that is captured sets the account and goes by that rule.
-        if self.weight is not None and self._rule is None and _capturing():
-            self._rule = "weight"
-        entry = self.weight if self._rule == "weight" else self.last_hit
+        rule = "weight" if self.weight is not None and self._rule is None and _capturing() else self._rule
+        entry = self.weight if rule == "weight" else self.last_hit
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, entry, k_new, v_new, t, self.status, stream=stream)
+        self._rule = rule
         self.renew_bounds(1, stream=stream)
         corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, ws, stream=stream)
         corm_block_attend(self.desc, q, self.K, self.V, self.lens, self.blocks, nsel, self.out, ws, status=self.status, stream=stream)
@@ -624,9 +627,12 @@ class LayerState:
         if self.weight is None:
             raise RuntimeError("made without want_weight")
         self._check_rule("weight")
-        self._rule = "weight"
+        _check_query(self.desc, q)
+        if budget is not None and not self.r <= operator.index(budget) < 1 << 31:
+            raise CormError(CORM_EINVAL, f"budget {budget} with r {self.r}")
         account = self.weight   # 4-byte entries: append and the gather carry them in the place of last_hit
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, account, k_new, v_new, t, self.status, stream=stream)
+        self._rule = "weight"
         corm_decode_attend_weigh(self.desc, q, self.K, self.V, self.lens, account, account, self.out, self.workspace,
                                  status=self.status, stream=stream)
         if budget is None:
@@ -637,6 +643,20 @@ class LayerState:
             corm_compact(self.desc, self.K, self.V, self.pos, account, self.lens, self.weight_keep, self.kept_idx, self.workspace,
                          stream=stream)
             self._rows_moved(stream)
+
+
+# A step of several calls looks at what the later ones would refuse before the first one has put a row in.
+
+def _check_choice(desc, nsel, nlast) -> None:
+    if not 1 <= operator.index(nlast) <= operator.index(nsel) <= max((desc.Lcap + BLOCK - 1) // BLOCK, 512):
+        raise CormError(CORM_EINVAL, f"nsel {nsel}, nlast {nlast}")
+
+
+def _check_query(desc, q) -> None:
+    _, heads, _, kv = _sizes(desc)
+    p = _dev(q, heads * desc.d, kv, "q", _device())
+    if not p or p % 16:
+        raise CormError(CORM_EINVAL, "q")
 
 
 def _block_list(lists, B, Hkv, nsel, device) -> torch.Tensor:
@@ -677,11 +697,15 @@ class Q8State:
         corm_q8_append(self.desc, self.code, k, v, n, n_new, self.K_codes, self.V_codes, self.k_scale, self.v_scale, self.K_tail,
                        self.V_tail, self.lens, self.lens, self.bounds, self.status, stream=stream)
 
+    def _check_choice(self, nsel, nlast) -> None:
+        if self.bounds is None:
+            raise RuntimeError("made without want_bounds")
+        _check_choice(self.desc, nsel, nlast)
+
     def attend(self, q, nsel=0, nlast=1, stream=None) -> None:
         """q [B,Hq,d] -> out.  nsel > 0: over the nlast newest blocks and those with the highest score bounds, nsel in all."""
         if nsel:
-            if self.bounds is None:
-                raise RuntimeError("made without want_bounds")
+            self._check_choice(nsel, nlast)
             self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.lens.device)
             corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, self.workspace, stream=stream)
         corm_q8_attend(self.desc, self.code, q, self.K_codes, self.V_codes, self.k_scale, self.v_scale, self.K_tail, self.V_tail,
@@ -690,5 +714,8 @@ class Q8State:
 
     def step(self, q, k_new, v_new, nsel=0, nlast=1, stream=None) -> None:
         """One decode step: the new row goes in, the query attends to all keys (or the chosen blocks), itself among them."""
+        if nsel:
+            self._check_choice(nsel, nlast)
+        _check_query(self.desc, q)
         self.append(k_new, v_new, stream=stream)
         self.attend(q, nsel, nlast, stream=stream)

@@ -176,3 +176,61 @@ def test_a_captured_block_step_may_be_replayed_behind_a_cut(monkeypatch):
     f.blocks(2, 1)
     with pytest.raises(RuntimeError, match="accounts"):
         f.st.step(*f.token()[1], None)
+
+
+REFUSED_Q = (("shape", lambda q: q[:, :2]), ("type", lambda q: q.bfloat16()), ("strides", lambda q: q.transpose(0, 1)), ("none", lambda q: None),
+             ("address", lambda q: torch.zeros(q.numel() + 1)[1:].view_as(q)))
+
+
+def test_a_refused_step_leaves_the_state_as_it_was(monkeypatch):
+    """Choice, budget and query are looked at before the row goes in: a caller that mends its call and repeats it has the token once."""
+    made = plain_library(monkeypatch)
+    f = _follower(12, want_weight=True, want_bounds=True)
+    f.preload(100)
+    q, args = f.token()
+    rest, st = args[1:], f.st
+    before = [x.clone() for x in (st.K, st.V, st.lens, st.pos, st.last_hit, st.weight, st.bounds)]
+    made.clear()
+
+    def refused(step, *a):
+        with pytest.raises((ValueError, TypeError, corm.CormError)):
+            step(*a)
+        assert made == [] and all(torch.equal(x, y) for x, y in zip(before, (st.K, st.V, st.lens, st.pos, st.last_hit, st.weight, st.bounds))), a[3:]
+
+    for nsel, nlast in ((0, 1), (-1, 1), (2, 0), (2, 3), (513, 1), (1 << 32, 1), (2, -(1 << 32) + 1), (2.0, 1), (None, 1), (2, None)):
+        refused(st.step_blocks, *args, nsel, nlast)
+    for budget in (0, f.r - 1, -1, 1 << 31, (1 << 32) + 50, 50.0):
+        refused(st.step_weigh, *args, budget)
+    for _, bad in REFUSED_Q:
+        refused(st.step_blocks, bad(args[0]), *rest, 2, 1)
+        refused(st.step_weigh, bad(args[0]), *rest)
+    monkeypatch.setattr(corm, "corm_append", lambda *a, **k: corm._check(corm.CORM_EINVAL, "no"))
+    refused(st.step_weigh, *args)
+    monkeypatch.undo()
+    made = plain_library(monkeypatch)
+    assert st._rule is None
+    st.step_blocks(*args, 512, 512)
+    st.step_weigh(*f.token()[1], f.r)
+
+
+def test_a_refused_step_leaves_the_8_bit_cache_as_it_was(monkeypatch):
+    made = []
+    for name in ("corm_q8_append", "corm_q8_attend", "corm_block_select"):
+        monkeypatch.setattr(corm, name, lambda *a, name=name, **k: made.append(name))
+    monkeypatch.setattr(corm, "_device", lambda: -1)
+    states = [corm.Q8State(2, 4, 2, 64, 640, "f32", device="cpu", want_bounds=w, workspace=torch.empty(256, dtype=torch.uint8)) for w in (True, False)]
+    q, k = torch.zeros(2, 4, 64), torch.zeros(2, 2, 64)
+    for nsel, nlast in ((-1, 1), (2, 0), (2, 3), (513, 1), (2.0, 1), (2, None)):
+        for call in (lambda: states[0].step(q, k, k, nsel, nlast), lambda: states[0].attend(q, nsel, nlast)):
+            with pytest.raises((TypeError, corm.CormError)):
+                call()
+    for call in (lambda: states[1].step(q, k, k, 2), lambda: states[1].attend(q, 2)):
+        with pytest.raises(RuntimeError, match="want_bounds"):
+            call()
+    for _, bad in REFUSED_Q:
+        with pytest.raises((ValueError, corm.CormError)):
+            states[0].step(bad(q), k, k)
+    assert made == []
+    states[0].step(q, k, k, 512, 512)
+    states[1].step(q, k, k)
+    assert made == ["corm_q8_append", "corm_block_select", "corm_q8_attend", "corm_q8_append", "corm_q8_attend"]
