@@ -515,7 +515,7 @@ class LayerState:
         # want_bounds: bounds of the blocks' keys, for step_blocks; want_weight: the keys' accounts, for step_weigh
         nblk = (Lcap + BLOCK - 1) // BLOCK
         self.bounds = torch.zeros(B, Hkv, nblk, 2, d, dtype=tdt, device=device) if want_bounds else None
-        self._blocks = {}
+        self._lists = _block_lists(self.desc, device) if want_bounds else None
         self.weight = torch.zeros(B, Hkv, Lcap, dtype=torch.float32, device=device) if want_weight else None
         self.weight_keep = torch.zeros(B, Hkv, Lcap, dtype=torch.uint8, device=device) if want_weight else None
         self._dead = False  # there may be dead slots (step_lazy)
@@ -602,14 +602,14 @@ class LayerState:
 
     def step_blocks(self, q, k_new, v_new, t, nsel, nlast=1, stream=None) -> None:
         """One decode step that attends to nsel blocks of 64 slots (the nlast newest and those with the highest score bounds): append,
-        the newest block's bounds, choice (self.blocks), attention.  Nothing is recorded or evicted."""
+        the newest block's bounds, choice (self.blocks, until the next step), attention.  Nothing is recorded or evicted."""
         if self.bounds is None:
             raise RuntimeError("made without want_bounds")
         if self._dead:
             raise RuntimeError("behind step_lazy a state may hold dead slots, which step_blocks would attend to: preload it, or use step")
         _check_choice(self.desc, nsel, nlast)
         _check_query(self.desc, q)
-        self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.K.device)
+        self.blocks = _lists_of(self._lists, self.desc, nsel)
         ws = self.blocks_workspace
         # The new row's entry of what the state evicts by.  While it has evicted by neither, all accounts behind the rows are empty, so last_hit
         # is the one to set; a graph may be replayed behind a cut by weight, so one that is captured sets the account and goes by that rule.
@@ -647,8 +647,12 @@ class LayerState:
 
 # A step of several calls looks at what the later ones would refuse before the first one has put a row in.
 
+def _most_listed(desc) -> int:
+    return max((desc.Lcap + BLOCK - 1) // BLOCK, 512)
+
+
 def _check_choice(desc, nsel, nlast) -> None:
-    if not 1 <= operator.index(nlast) <= operator.index(nsel) <= max((desc.Lcap + BLOCK - 1) // BLOCK, 512):
+    if not 1 <= operator.index(nlast) <= operator.index(nsel) <= _most_listed(desc):
         raise CormError(CORM_EINVAL, f"nsel {nsel}, nlast {nlast}")
 
 
@@ -659,11 +663,14 @@ def _check_query(desc, q) -> None:
         raise CormError(CORM_EINVAL, "q")
 
 
-def _block_list(lists, B, Hkv, nsel, device) -> torch.Tensor:
-    """The array for nsel chosen blocks; none is given back while a step on some stream may still read it."""
-    if nsel not in lists:
-        lists[nsel] = torch.empty(B, Hkv, nsel, dtype=torch.int32, device=device)
-    return lists[nsel]
+def _block_lists(desc, device) -> torch.Tensor:
+    """Room for the longest lists of chosen blocks."""
+    return torch.empty(desc.B * desc.Hkv * _most_listed(desc), dtype=torch.int32, device=device)
+
+
+def _lists_of(room, desc, nsel) -> torch.Tensor:
+    """Lists of nsel blocks in it: a step allocates nothing, since it may be given another stream than the current one."""
+    return room[:desc.B * desc.Hkv * nsel].view(desc.B, desc.Hkv, nsel)
 
 
 class Q8State:
@@ -686,7 +693,7 @@ class Q8State:
         self.out = torch.zeros(B, Hq, d, dtype=torch.float32, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)
         self.bounds = torch.zeros(B, Hkv, n, 2, d, dtype=tdt, device=device) if want_bounds else None
-        self._blocks = {}
+        self._lists = _block_lists(self.desc, device) if want_bounds else None
         if workspace is None:
             workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
         self.workspace = workspace
@@ -706,7 +713,7 @@ class Q8State:
         """q [B,Hq,d] -> out.  nsel > 0: over the nlast newest blocks and those with the highest score bounds, nsel in all."""
         if nsel:
             self._check_choice(nsel, nlast)
-            self.blocks = _block_list(self._blocks, self.B, self.Hkv, nsel, self.lens.device)
+            self.blocks = _lists_of(self._lists, self.desc, nsel)
             corm_block_select(self.desc, q, self.bounds, self.lens, nsel, nlast, self.blocks, self.workspace, stream=stream)
         corm_q8_attend(self.desc, self.code, q, self.K_codes, self.V_codes, self.k_scale, self.v_scale, self.K_tail, self.V_tail,
                        self.lens, self.out, self.workspace, blocks=self.blocks if nsel else None, nsel=nsel, status=self.status,

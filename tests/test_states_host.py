@@ -234,3 +234,27 @@ def test_a_refused_step_leaves_the_8_bit_cache_as_it_was(monkeypatch):
     states[0].step(q, k, k, 512, 512)
     states[1].step(q, k, k)
     assert made == ["corm_q8_append", "corm_block_select", "corm_q8_attend", "corm_q8_append", "corm_q8_attend"]
+
+
+def test_steps_allocate_nothing(monkeypatch):
+    """Memory taken within a step would belong to the current stream, whose earlier work may still be using it, and be written on the step's."""
+    plain_library(monkeypatch)
+    monkeypatch.setattr(corm, "corm_q8_append", lambda *a, **k: None)
+    monkeypatch.setattr(corm, "corm_q8_attend", lambda *a, **k: None)
+    f = _follower(13, want_weight=True, want_bounds=True)
+    f.preload(100)
+    q8 = corm.Q8State(2, 4, 2, 64, 256, "f32", device="cpu", want_bounds=True, workspace=torch.empty(256, dtype=torch.uint8))
+    tokens = [f.token()[1] for _ in range(5)]
+
+    def none(*a, **k):
+        raise AssertionError("an allocation")
+
+    with monkeypatch.context() as m:
+        for name in ("empty", "zeros", "empty_like", "zeros_like"):
+            m.setattr(torch, name, none)
+        for args, (nsel, nlast) in zip(tokens, ((1, 1), (3, 2), (512, 7), (2, 2))):
+            f.st.step_blocks(*args, nsel, nlast)
+            assert f.st.blocks.shape == (2, 2, nsel) and f.st.blocks.is_contiguous()
+            q8.step(*args[:3], nsel, nlast)
+            assert q8.blocks.shape == (2, 2, nsel) and q8.blocks.is_contiguous()
+        f.st.step_weigh(*tokens[4], 60)
