@@ -290,7 +290,8 @@ int corm_blocks_workspace_bytes(const corm_desc* desc, size_t* bytes);
  * kv_dtype (the tail).  A block is quantised once, when it gets full, from the rows themselves:
  *   amax = largest magnitude of the block's 64 x d elements (K and V apart);  Q = 127 (CORM_I8) or 448 (CORM_E4M3)
  *   scale = fp32(amax / Q);  code = x * fp32(Q / amax) in fp32, rounded to the nearest (even) integer / e4m3 (OCP) value
- * (a block with amax < 2^-100 is held as zeros with scale 0).  The key of a slot is then scale * code.
+ * (a block with amax < 2^-100 is held as zeros with scale 0).  The key of a slot is then scale * code.  In a block with an element that is infinite
+ * or not a number the scale is not a number, and with it every output over the block.
  *   K_codes  [B, Hkv, nblk, d/64, 64, 64]  1 byte    [.., block, channel / 64, slot % 64, channel % 64]
  *   V_codes  [B, Hkv, nblk, d, 64]         1 byte    [.., block, channel, slot % 64]
  *   k_scale, v_scale  [B, Hkv, nblk]       float32

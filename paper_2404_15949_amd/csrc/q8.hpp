@@ -561,7 +561,7 @@ __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a
   constexpr int ESZ = DT::ESZ, EPL = DT::EPL, ROWB = D * ESZ, SL = ROWB / 16;   // 16-byte slices of a row
   constexpr int QUADS = 16 * SL, QPT = (QUADS + WG - 1) / WG;
   __shared__ uint32_t sh_v[D][17];     // four keys a word
-  __shared__ float sh_top[2][WAVES];
+  __shared__ uint32_t sh_top[2][WAVES];
   __shared__ float sh_lo[16][D], sh_hi[16][D];
   const int unit = blockIdx.y, blk = blockIdx.x, tid = threadIdx.x;
   const Arrival r = arrival(a, unit);
@@ -576,7 +576,7 @@ __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a
 
   if (whole) {
     uint4 k[QPT][4], v[QPT][4];
-    float ktop = 0.f, vtop = 0.f;
+    uint32_t kbits = 0u, vbits = 0u;   // largest magnitudes, as bits: what is not a number lies above all numbers (fmaxf would drop it)
 #pragma unroll
     for (int p = 0; p < QPT; ++p) {
       const int quad = tid + p * WG, rg = quad / SL, sl = quad % SL;
@@ -591,19 +591,19 @@ __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a
         }
 #pragma unroll
         for (int e = 0; e < EPL; ++e) {
-          ktop = fmaxf(ktop, fabsf(element<DT>(k[p][j], e)));
-          vtop = fmaxf(vtop, fabsf(element<DT>(v[p][j], e)));
+          kbits = max(kbits, __float_as_uint(fabsf(element<DT>(k[p][j], e))));
+          vbits = max(vbits, __float_as_uint(fabsf(element<DT>(v[p][j], e))));
         }
       }
     }
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) {
-      ktop = fmaxf(ktop, __shfl_xor(ktop, o));
-      vtop = fmaxf(vtop, __shfl_xor(vtop, o));
+      kbits = max(kbits, (uint32_t)__shfl_xor((int)kbits, o));
+      vbits = max(vbits, (uint32_t)__shfl_xor((int)vbits, o));
     }
     if ((tid & 63) == 0) {
-      sh_top[0][tid >> 6] = ktop;
-      sh_top[1][tid >> 6] = vtop;
+      sh_top[0][tid >> 6] = kbits;
+      sh_top[1][tid >> 6] = vbits;
     }
     if (a.bounds) {
 #pragma unroll
@@ -625,14 +625,18 @@ __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a
       }
     }
     __syncthreads();
-    ktop = fmaxf(fmaxf(sh_top[0][0], sh_top[0][1]), fmaxf(sh_top[0][2], sh_top[0][3]));
-    vtop = fmaxf(fmaxf(sh_top[1][0], sh_top[1][1]), fmaxf(sh_top[1][2], sh_top[1][3]));
-    // (a block whose largest magnitude is below 2^-100 is held as zeros: 1 / it is near the end of fp32's range)
-    const bool ksome = ktop >= 0x1p-100f, vsome = vtop >= 0x1p-100f;
-    const float kinv = ksome ? __fdiv_rn(C::QMAX, ktop) : 0.f, vinv = vsome ? __fdiv_rn(C::QMAX, vtop) : 0.f;
+    // (a block whose largest magnitude is below 2^-100 is held as zeros: 1 / it is near the end of fp32's range.  The scale of a block with an element that is
+    // infinite or not a number is not a number: int8 has no code for these)
+    auto top = [](const uint32_t(&w)[WAVES]) {
+      const uint32_t bits = max(max(w[0], w[1]), max(w[2], w[3]));
+      return bits < 0x7f800000u ? __uint_as_float(bits) : __builtin_nanf("");
+    };
+    const float ktop = top(sh_top[0]), vtop = top(sh_top[1]);
+    const bool knone = ktop < 0x1p-100f, vnone = vtop < 0x1p-100f;
+    const float kinv = knone ? 0.f : __fdiv_rn(C::QMAX, ktop), vinv = vnone ? 0.f : __fdiv_rn(C::QMAX, vtop);
     if (tid == 0) {
-      a.ks[dst] = ksome ? __fdiv_rn(ktop, C::QMAX) : 0.f;
-      a.vs[dst] = vsome ? __fdiv_rn(vtop, C::QMAX) : 0.f;
+      a.ks[dst] = knone ? 0.f : __fdiv_rn(ktop, C::QMAX);
+      a.vs[dst] = vnone ? 0.f : __fdiv_rn(vtop, C::QMAX);
     }
     unsigned char* kc = a.Kc + dst * (QBLK * D);
     unsigned char* vc = a.Vc + dst * (QBLK * D);

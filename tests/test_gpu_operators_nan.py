@@ -1,0 +1,45 @@
+"""What is not a number in rows and queries: it stays none where it belongs, and spoils nothing else."""
+import pytest
+import torch
+
+from paper_2404_15949_amd import corm
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+
+
+@pytest.mark.parametrize("what", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64), ("f32", 128)])
+def test_a_block_with_what_is_not_a_number_is_none(dtype, d, code, what):
+    """One element of a block, of a key and then of a value: outputs over the block are not numbers (int8 has no code for it, its scale says so); the other
+    blocks have the codes and scales they have without it, and so have outputs over them alone."""
+    g = torch.Generator().manual_seed(1)
+    P, bad = 64 * 5 + 9, 2
+    k, v = ((torch.randn(2, 1, P, d, generator=g)).to(DT[dtype]) for _ in range(2))
+    q = torch.randn(2, 2, d, generator=g).to(DT[dtype]).to(DEV)
+    clean = corm.Q8State(2, 2, 1, d, 64 * 6, dtype, code, device=DEV)
+    clean.append(k.to(DEV), v.to(DEV))
+    for side in (0, 1):
+        rows = [k.clone(), v.clone()]
+        rows[side][0, 0, 64 * bad + 17, 5] = what
+        st = corm.Q8State(2, 2, 1, d, 64 * 6, dtype, code, device=DEV)
+        st.append(rows[0].to(DEV), rows[1].to(DEV))
+        scales, want = ((st.k_scale, st.v_scale), (clean.k_scale, clean.v_scale))
+        assert not bool(scales[side][0, 0, bad].isfinite())
+        for s, w, c, e in zip(scales, want, (st.K_codes, st.V_codes), (clean.K_codes, clean.V_codes)):
+            same = torch.ones(2, 1, 6, dtype=torch.bool, device=DEV)
+            if s is scales[side]:
+                same[0, 0, bad] = False
+            assert torch.equal(s[same], w[same]) and torch.equal(c.view(torch.int8)[same], e.view(torch.int8)[same])
+        st.attend(q)
+        clean.attend(q)
+        assert bool(st.out[0].isnan().all()) and torch.equal(st.out[1], clean.out[1])
+        listed = torch.tensor([[[0, 1, 3, 4, 5]]] * 2, dtype=torch.int32, device=DEV)
+        outs = []
+        for x in (st, clean):
+            corm.corm_q8_attend(x.desc, code, q, x.K_codes, x.V_codes, x.k_scale, x.v_scale, x.K_tail, x.V_tail, x.lens, x.out, x.workspace,
+                                blocks=listed, nsel=5)
+            outs.append(x.out.clone())
+        assert torch.equal(*outs) and bool(outs[0].isfinite().all())
