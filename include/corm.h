@@ -323,8 +323,9 @@ int corm_block_bounds(const corm_desc* desc, const void* K, const int32_t* lens,
 
 /* The blocks a decode step attends to: the nlast newest blocks of the unit and, of the others, those with the highest upper
  * bound of a logit of the group, max over its heads of sum_c max(q_c lo_c, q_c hi_c), formed in 64 bits and rounded once to
- * fp32 (equal ones: the lower block first; not a number: last).  blocks [B, Hkv, nsel] int32: ascending, -1 behind the last where the unit has
- * fewer than nsel.  1 <= nlast <= nsel <= max(nblk, 512). */
+ * fp32 (equal ones: the lower block first; a head for which it is not a number does not count, a block without any is last).
+ * blocks [B, Hkv, nsel] int32: ascending, -1 behind the last where the unit has fewer than nsel.
+ * 1 <= nlast <= nsel <= max(nblk, 512). */
 int corm_block_select(const corm_desc* desc, const void* q, const void* bounds, const int32_t* lens, int32_t nsel, int32_t nlast,
                       int32_t* blocks, void* workspace, size_t workspace_bytes, void* stream);
 

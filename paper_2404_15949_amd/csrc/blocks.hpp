@@ -71,13 +71,13 @@ __global__ __launch_bounds__(WG) void corm_block_bounds_kernel(const char* K, co
 // Upper bound of a block's logits: sum over channels of the larger of q*lo and q*hi, which is q+ * hi + q- * lo; the largest over the
 // heads of the group.  In 64 bits, rounded once to fp32, so that the choice does not hang on the order of a sum (two blocks
 // next to each other at the border of the choice differ by 1e-5 of their scores now and then, never by 1e-15).
-// q- (taken with the smaller elements) and q+ (with the larger) of the group's heads.  Ends without a barrier.
+// q- (taken with the smaller elements) and q+ (with the larger) of the group's heads; what is not a number is so in both.  Ends without a barrier.
 template <typename DT, int D, int G, int NT>
 __device__ __forceinline__ void stage_signed_q(const char* qu, double2 (&sh_q)[G][D]) {
   for (int i = threadIdx.x; i < G * D; i += NT) {
     const float x = DT::ESZ == 2 ? __uint_as_float((uint32_t)reinterpret_cast<const uint16_t*>(qu)[i] << 16)
                                  : reinterpret_cast<const float*>(qu)[i];
-    sh_q[i / D][i % D] = make_double2((double)fminf(x, 0.f), (double)fmaxf(x, 0.f));
+    sh_q[i / D][i % D] = make_double2((double)(x > 0.f ? 0.f : x), (double)(x < 0.f ? 0.f : x));
   }
 }
 
@@ -112,7 +112,7 @@ __device__ __forceinline__ void share_score(const char* at, int share, const dou
   }
 }
 
-// The shares' sums of the lane's block -> its score.
+// The shares' sums of the lane's block -> its score, from the heads for which it is a number.
 template <int G, int SHARES>
 __device__ __forceinline__ float joined_score(const double (&part)[SHARES][G][64]) {
   const int lane = threadIdx.x & 63;

@@ -3,6 +3,7 @@ import pytest
 import torch
 
 from paper_2404_15949_amd import corm
+from tests import operators_ref as ref
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -43,3 +44,22 @@ def test_a_block_with_what_is_not_a_number_is_none(dtype, d, code, what):
                                 blocks=listed, nsel=5)
             outs.append(x.out.clone())
         assert torch.equal(*outs) and bool(outs[0].isfinite().all())
+
+
+@pytest.mark.parametrize("nblk", [40, 300])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_head_whose_query_is_not_a_number_does_not_choose(dtype, nblk):
+    """The others of its group do; where none does, the lower blocks are chosen."""
+    g, d, G = torch.Generator().manual_seed(nblk), 64, 4
+    desc = corm.make_desc(3, G, 1, d, nblk * 64, nblk * 64, 1, 1, dtype)
+    lo = torch.randn(3, 1, nblk, d, generator=g)
+    bounds = torch.stack([lo, lo + torch.rand(3, 1, nblk, d, generator=g)], 3).to(DT[dtype])
+    lens = torch.full((3, 1), nblk * 64, dtype=torch.int32, device=DEV)
+    q = torch.randn(3, G, d, generator=g).to(DT[dtype])
+    q[0, 0, 3], q[1, 2, 7], q[2, :, 1] = float("nan"), float("nan"), float("nan")
+    blocks = torch.full((3, 1, 9), -77, dtype=torch.int32, device=DEV)
+    ws = torch.full((corm.corm_blocks_workspace_bytes(desc),), 0xA5, dtype=torch.uint8, device=DEV)
+    corm.corm_block_select(desc, q.to(DEV), bounds.to(DEV), lens, 9, 2, blocks, ws)
+    for b, heads in ((0, [1, 2, 3]), (1, [0, 1, 3])):
+        assert blocks[b, 0].tolist() == ref.choose(q[b, heads], bounds[b, 0], 9, 2), b
+    assert blocks[2, 0].tolist() == list(range(7)) + [nblk - 2, nblk - 1]
