@@ -148,7 +148,7 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_part_kernel(const EvictLong
 }
 
 __global__ __launch_bounds__(EVW_WG) void corm_evict_settle_kernel(const EvictLongArgs a) {
-  __shared__ uint32_t sh_slot[SETTLE_KEYS], sh_key[SETTLE_KEYS];
+  __shared__ uint32_t sh_slot[SETTLE_KEYS], sh_key[SETTLE_KEYS], sh_count[64];
   __shared__ CutLds<EVW_WG, EVW_BITS> sh;
   constexpr uint32_t LOW = (1u << (32 - EVW_BITS)) - 1u;
   const int unit = blockIdx.x, tid = threadIdx.x;
@@ -164,6 +164,7 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_settle_kernel(const EvictLo
   const uint32_t mine = lane < a.splits ? counts[lane] : 0u, upto = wave_prefix_sum(mine);
   const int total = __builtin_amdgcn_readlane((int)upto, 63);
   const bool held = total <= SETTLE_KEYS;
+  if (wv == 0) sh_count[lane] = mine;
   if (held) {
     for (int s = wv; s < a.splits; s += EVW_WG / 64) {
       const int c = __builtin_amdgcn_readlane((int)mine, s), at = __builtin_amdgcn_readlane((int)upto, s) - c;
@@ -173,25 +174,45 @@ __global__ __launch_bounds__(EVW_WG) void corm_evict_settle_kernel(const EvictLo
         sh_key[at + j] = order_key(w[slot]) & LOW;
       }
     }
-    __syncthreads();
   }
-  // (very many with one digit, as where all weights are equal: every slot is looked at in every round)
-  const int n = held ? total : L - a.r;
-  auto item = [&](int i, uint32_t& x, uint32_t& slot) {
-    if (held) {
+  __syncthreads();
+  // More than that have the digit (accounts within a factor of two or three, or very many slots): they are walked from memory in every round, by their
+  // lists, side by side in rows of 2^shift places; but where over a quarter of the slots is listed, slot by slot, which is one load less in a chain.
+  // Whole calls, us, slots | lists: lognormal accounts of sigma 2, a sixteenth kept, 8 units x 1048576 1026 | 60; of 0.5, half kept (a seventh listed),
+  // 16 x 131072 102 | 58, 8 x 1048576 1065 | 460, 256 x 100000 203 | 147; of 0.18 (two fifths) 94 | 101, 1170 | 1333, 213 | 203; all equal 404 | 477,
+  // 3248 | 4388, 478 | 585.
+  uint32_t most = mine;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) most = max(most, (uint32_t)__shfl_xor((int)most, o));
+  const int shift = 32 - __clz((int)max(most, 2u) - 1);
+  auto settle = [&](int n, const auto& item) {
+    const Cut cut = find_cut<EVW_WG, EVW_BITS, 32 - EVW_BITS>(n, digit.y, item, sh);
+    for (int i = tid; i < n; i += EVW_WG) {
+      uint32_t x, slot;
+      if (item(i, x, slot)) to[slot] = x > cut.key || (x == cut.key && slot <= cut.last);
+    }
+  };
+  if (held) {
+    settle(total, [&](int i, uint32_t& x, uint32_t& slot) {
       x = sh_key[i];
       slot = sh_slot[i];
       return true;
-    }
-    const uint32_t full = order_key(w[i]);
-    x = full & LOW;
-    slot = (uint32_t)i;
-    return full >> (32 - EVW_BITS) == digit.x;
-  };
-  const Cut cut = find_cut<EVW_WG, EVW_BITS, 32 - EVW_BITS>(n, digit.y, item, sh);
-  for (int i = tid; i < n; i += EVW_WG) {
-    uint32_t x, slot;
-    if (item(i, x, slot)) to[slot] = x > cut.key || (x == cut.key && slot <= cut.last);
+    });
+  } else if (total <= (L - a.r) / 4) {
+    settle(a.splits << shift, [&](int i, uint32_t& x, uint32_t& slot) {
+      const uint32_t s = (uint32_t)i >> shift, j = (uint32_t)i & ((1u << shift) - 1u);
+      if (j >= sh_count[s]) return false;
+      slot = listed[(size_t)s * a.split_slots + j];
+      x = order_key(w[slot]) & LOW;
+      return true;
+    });
+  } else {
+    settle(L - a.r, [&](int i, uint32_t& x, uint32_t& slot) {
+      const uint32_t full = order_key(w[i]);
+      x = full & LOW;
+      slot = (uint32_t)i;
+      return full >> (32 - EVW_BITS) == digit.x;
+    });
   }
 }
 

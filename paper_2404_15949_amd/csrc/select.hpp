@@ -139,7 +139,7 @@ __device__ __forceinline__ Cut find_cut(int n, uint32_t k, const Item& item, Cut
     __syncthreads();
     return cut;
   }
-  // more equal keys than threads: the need-th lowest of their slots, by digits of the slots
+  // more equal keys than the list holds: the need-th lowest of their slots, by digits of the slots
   Cut cut = {prefix, SLOT_TOP};
   if (need == have) return cut;
   auto slots = [&](int i, uint32_t& x, uint32_t& slot) {

@@ -177,3 +177,28 @@ def test_block_attend_of_many_units(units, G, d, dtype, nsel):
         L = int(lens[u])
         slots = [s for i in blocks[u].tolist() if i >= 0 for s in range(64 * i, min(64 * i + 64, L))]
         _check(out[u].cpu().double(), q[u].cpu().double(), K[u, slots].cpu().double(), V[u, slots].cpu().double(), 1.0 / math.sqrt(d), u)
+
+
+@pytest.mark.parametrize("units,cap", [(3, 1 << 20), (20, 131072), (300, 60000)])
+@pytest.mark.parametrize("sigma", [2.0, 0.5, 0.25, 0.1])
+def test_evict_mask_weight_of_close_accounts(units, cap, sigma):
+    """Long units with more accounts in the digit of the cut than a workgroup holds, few and many of all there are; a part of them equal."""
+    g = torch.Generator(device=DEV).manual_seed(cap)
+    w = torch.exp(sigma * torch.randn(units, cap, generator=g, device=DEV)) / 1024
+    w[1] = (w[1] * 2 ** 14).round() / 2 ** 14
+    lens = torch.full((units, 1), cap, dtype=torch.int32)
+    lens[1::3] = cap - 17
+    r = 33
+    desc = corm.make_desc(units, 1, 1, 64, cap, cap, 1, r, "f32")
+    ws = torch.full((corm.corm_blocks_workspace_bytes(desc),), 0xA5, dtype=torch.uint8, device=DEV)
+    for budget in (cap // 16, cap // 2):
+        keep = torch.full((units, cap), 9, dtype=torch.uint8, device=DEV)
+        corm.corm_evict_mask_weight(desc, w, lens.to(DEV), budget, keep, ws)
+        at = torch.arange(cap, device=DEV)
+        for u in sorted({0, 1, 2, units - 1, units // 2}):
+            L = int(lens[u])
+            order = torch.sort(w[u, :L - r], descending=True, stable=True)[1][:budget - r]      # (equal ones: the lower slot first)
+            want = (at >= L - r).to(torch.uint8)
+            want[order] = 1
+            want[L:] = 9
+            assert torch.equal(keep[u], want), (u, L, budget)
