@@ -433,7 +433,7 @@ def corm_block_bounds(desc, K, lens, bounds, newest=0, stream=None, check=True) 
     return _check(rc, "corm_block_bounds") if check else rc
 
 
-def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace=None, workspace_bytes=None, stream=None, check=True) -> int:
+def corm_block_select(desc, q, bounds, lens, nsel, nlast, blocks, workspace, workspace_bytes=None, stream=None, check=True) -> int:
     units, heads, nblk, kv = _sizes(desc)
     at = _device()
     rc = lib().corm_block_select(ctypes.byref(desc), _dev(q, heads * desc.d, kv, "q", at), _dev(bounds, units * nblk * 2 * desc.d, kv, "bounds", at),

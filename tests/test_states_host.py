@@ -258,3 +258,9 @@ def test_steps_allocate_nothing(monkeypatch):
             q8.step(*args[:3], nsel, nlast)
             assert q8.blocks.shape == (2, 2, nsel) and q8.blocks.is_contiguous()
         f.st.step_weigh(*tokens[4], 60)
+
+
+def test_the_choice_asks_for_its_workspace():
+    """It has never done without one."""
+    with pytest.raises(TypeError):
+        corm.corm_block_select(_follower(14).st.desc, 4096, 4096, 4096, 8, 2, 4096)
