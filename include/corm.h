@@ -282,8 +282,9 @@ int corm_prefill_seed(const corm_desc* desc, const void* q_tail, int32_t m, void
  * where it says so, r; the other fields have to be valid and do nothing.
  *
  * corm_blocks_workspace_bytes: the workspace of corm_q8_attend, corm_block_select, corm_block_attend and
- * corm_evict_mask_weight (256-byte aligned).  Nothing in it has to be prepared or survives a call, so calls on one stream, and
- * captured graphs that are replayed one after the other, may share it. */
+ * corm_evict_mask_weight (256-byte aligned): one size for all of them, partials of 129 parts a head at least (d 128: 67 KB a
+ * head), so layers that run one after the other had better share it.  Nothing in it has to be prepared or survives a call, so
+ * calls on one stream, and captured graphs that are replayed one after the other, may do so. */
 int corm_blocks_workspace_bytes(const corm_desc* desc, size_t* bytes);
 
 /* 8-bit cache.  Full blocks are held in codes with a scale each; the lens % 64 newest rows, which fill no block yet, stay in
@@ -346,10 +347,12 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
  * budget - r with the greatest weight (equal ones: the lower slot first; not a number: least); all of them where lens <= budget.
  * budget >= r.  Entries >= lens are left as they were.
  *
- * The accounts of a prompt: corm_decode_attend_weigh for each of its last queries (as many as are to count), with lens as it was at the query's step.
+ * The accounts of a prompt: corm_decode_attend_weigh for each of its last queries (as many as are to count), with lens as it was
+ * at the query's step; each of these calls reads the whole cache.
  * corm_append and corm_compact carry the accounts where they are given in the place of last_hit, whose 4-byte entries they set
- * to 0 (0.0f) for a new key and move with a survivor.  A whole step is corm_append, corm_decode_attend_weigh and, where
- * the cache is to be cut, corm_evict_mask_weight and corm_compact. */
+ * to 0 (0.0f) for a new key and move with a survivor; last_hit itself then stays behind, so a cache goes by one of the two rules.
+ * A whole step is corm_append, corm_decode_attend_weigh and, where the cache is to be cut, corm_evict_mask_weight and
+ * corm_compact. */
 int corm_decode_attend_weigh(const corm_desc* desc, const void* q, const void* K, const void* V, const int32_t* lens,
                              const float* weight_in, float* weight, float* out, void* workspace, size_t workspace_bytes,
                              int32_t* status, const corm_launch_opts* opts, void* stream);

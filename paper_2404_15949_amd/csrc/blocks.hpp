@@ -81,11 +81,13 @@ __device__ __forceinline__ void stage_signed_q(const char* qu, double2 (&sh_q)[G
   }
 }
 
-// A share of the channels of the lane's block (bounds at `at`): its sums for every head.  (From the bounds' sum and distance one number of a query per channel
-// would do, a little faster, but one bound of 1e30 would take all digits of the other.)
+// A share of the channels of the lane's block (bounds at `at`): its sums for every head.  The definition takes the larger product whichever of the two bounds it
+// is of, and so does this.  (From the bounds' sum and distance one number of a query per channel would do, a little faster, but one bound of 1e30 would take
+// all digits of the other.)
 template <typename DT, int D, int G, int SHARES>
 __device__ __forceinline__ void share_score(const char* at, int share, const double2 (&sh_q)[G][D], double (&sum)[G]) {
-  constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / SHARES, CH = D / SHARES, STEP = PIECES < 2 ? PIECES : 2;   // pieces of 16 bytes; of them in flight, from both rows
+  // pieces of 16 bytes, STEP of them in flight from both rows
+  constexpr int EPL = DT::EPL, ROWB = D * DT::ESZ, PIECES = ROWB / 16 / SHARES, CH = D / SHARES, STEP = PIECES < 2 ? PIECES : 2;
   at += (size_t)share * (PIECES * 16);
 #pragma unroll
   for (int g = 0; g < G; ++g) sum[g] = 0.;
@@ -127,8 +129,8 @@ __device__ __forceinline__ float joined_score(const double (&part)[SHARES][G][64
   return (float)best;
 }
 
-// Grid (groups of 64 blocks, units).  Lane = block, wave = an eighth of the channels: what bounds it are the chains of 64-bit products behind the queries' LDS
-// reads, and more waves have shorter ones (whole steps of 128 units x 440 blocks by 2 | 4 | 8 | 16 waves, us: 73.7 | 71.4 | 68.9 | 70.7).
+// Grid (groups of 64 blocks, units).  Lane = block, wave = an eighth of the channels: what bounds it are the chains of 64-bit products behind the queries'
+// LDS reads, and more waves have shorter ones (whole steps of 128 units x 440 blocks by 2 | 4 | 8 | 16 waves, us: 73.7 | 71.4 | 68.9 | 70.7).
 constexpr int SCORE_SHARES = 8;
 template <typename DT, int D, int G>
 __global__ __launch_bounds__(64 * SCORE_SHARES) void corm_block_score_kernel(const char* q, const char* bounds, const int32_t* lens, float* scores,

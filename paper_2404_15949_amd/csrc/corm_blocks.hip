@@ -31,9 +31,10 @@ int blocks_of(const corm_desc* d) { return (d->Lcap + QBLK - 1) / QBLK; }
 int max_parts(const corm_desc* d) { return std::max((blocks_of(d) + 3) / 4, 128) + 1; }
 int max_listed(const corm_desc* d) { return std::max(blocks_of(d), 512); }
 
-// Splits of a unit in the eviction decision of long units, 0 where a workgroup takes a unit alone: where it can hold the unit's keys.  Us, one workgroup | splits:
-// 8, 128 and 512 units x 9000 slots 9.7 | 14.1, 10.1 | 16.4 and 15.9 | 31.5, x 16000 14.4 | 13.8, 15.8 | 17.3 and 23.1 | 33.0; keys from memory
-// in every round | splits: 8, 512 and 2000 x 20000 22 | 14, 40 | 42 and 169 | 157, 256 x 40000 69 | 42, 256 x 100000 185 | 101, 8 x 500000 530 | 29.
+// Splits of a unit in the eviction decision of long units, 0 where a workgroup takes a unit alone: where it can hold the unit's keys.  Us, one
+// workgroup | splits: 8, 128 and 512 units x 9000 slots 9.7 | 14.1, 10.1 | 16.4 and 15.9 | 31.5, x 16000 14.4 | 13.8, 15.8 | 17.3 and 23.1 | 33.0;
+// keys from memory in every round | splits: 8, 512 and 2000 x 20000 22 | 14, 40 | 42 and 169 | 157, 256 x 40000 69 | 42, 256 x 100000 185 | 101,
+// 8 x 500000 530 | 29.
 struct EvictSplits {
   int splits, slots;
   size_t listed_off, counts_off, digit_off, total;
@@ -259,15 +260,17 @@ int corm_block_attend(const corm_desc* desc, const void* q, const void* K, const
   a.lens = lens; a.blocks = blocks; a.partials = reinterpret_cast<float*>(workspace); a.out = out; a.status = status;
   a.Lcap = desc->Lcap; a.nsel = nsel; a.scale_log2 = scale_log2(desc);
   const long units = (long)desc->B * desc->Hkv;
-  // The longest parts of up to 8 blocks that leave two workgroups for each compute unit, four where rows are 512 bytes (a list holds at most the
-  // unit's blocks in earnest).  Whole steps, us, two | four | eight workgroups: bf16 128 units x 64 blocks 69.8 | 69.7 | 71.7, 64 x 64 of eight heads
-  // 47.6 | 50.8 | 57.2, 288 units of up to 4 blocks in a list of 65 27.7 | 37.6 | 53.5; fp32 64 x 32 42.7 | 39.1 | 39.2.
+  // The shortest parts (1, 2, 4 or 8 blocks) with which the launch has at most two workgroups for each compute unit, four where rows are 512 bytes; parts
+  // of 8 where it has more all the same (a list holds at most the unit's blocks in earnest).  Whole steps, us, at most two | four | eight:
+  // bf16 64 units x 64 blocks of eight heads 47.6 | 50.8 | 57.2, 288 units of up to 4 blocks in a list of 65 27.7 | 37.6 | 53.5; fp32 64 x 32
+  // 42.7 | 39.1 | 39.2; bf16 128 x 64 parts of 8 (1024 workgroups, with two and with four) 69.7, of 4 (with eight) 71.7.
   const int room = max_parts(desc), real = std::min(nsel, blocks_of(desc));
   const long wgs = (row_bytes(desc) > 256 ? 4L : 2L) * device_cus();
   auto parts_of = [&](int n) { return (n + a.part_blocks - 1) / a.part_blocks; };
   a.part_blocks = 1;
-  // (few blocks: one part, which writes out itself.  Whole steps, us, parts and merge | one part: bf16, 8 to 128 units, 2 blocks 15.6 | 13.5 and 17.3 | 14.5, 4 blocks
-  // 15.5 | 14.9 and 20.4 | 16.4, 8 blocks 15.5 | 17.6 and 23.0 | 20.1; fp32 2 blocks 15.0 | 13.8 and 17.6 | 16.0, of eight heads 21.3 | 22.2 and 25.3 | 24.5, 4 blocks 15.3 | 18.3)
+  // (few blocks: one part, which writes out itself.  Whole steps, us, parts and merge | one part: bf16, 8 to 128 units, 2 blocks 15.6 | 13.5 and
+  // 17.3 | 14.5, 4 blocks 15.5 | 14.9 and 20.4 | 16.4, 8 blocks 15.5 | 17.6 and 23.0 | 20.1; fp32 2 blocks 15.0 | 13.8 and 17.6 | 16.0, of eight heads
+  // 21.3 | 22.2 and 25.3 | 24.5, 4 blocks 15.3 | 18.3)
   const bool few = nsel <= (desc->kv_dtype == CORM_F32 ? 2 : 4);
   while (a.part_blocks < LIST_PART && (few || units * parts_of(real) > wgs || parts_of(nsel) > room)) a.part_blocks *= 2;
   const int parts = parts_of(nsel);

@@ -26,8 +26,8 @@ __device__ __forceinline__ float element(const uint4& x, int i) {
   return DT::ESZ == 2 ? ((i & 1) ? bf16_hi(w) : bf16_lo(w)) : __uint_as_float(w);
 }
 
-// 16 bytes that are not needed again soon: rows on their way into codes or bounds are gigabytes of which nobody finds anything in a cache (with the codes stored so
-// too, 16 prompts of up to 4096 rows, 32 heads: 245 -> 218 us; loads alone 249; bounds of as many keys 80 -> 73).
+// 16 bytes that are not needed again soon: rows on their way into codes or bounds are gigabytes of which nobody finds anything in a cache (with the
+// codes stored so too, 16 prompts of up to 4096 rows, 32 heads: 245 -> 218 us; loads alone 249; bounds of as many keys 80 -> 73).
 __device__ __forceinline__ uint4 load_once(const char* at) {
   const u32x4_t v = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(at));
   return make_uint4(v.x, v.y, v.z, v.w);
@@ -213,8 +213,8 @@ struct QueryOperand {
   }
 };
 
-// A workgroup is a part of a unit, a wave takes every fourth block of it; the tail is the last part, or a workgroup has the whole unit.  Workgroups go to the 8 dies in
-// turn: each die gets whole units, one after the other, so that no die has all first or all last parts, nor all units of a head.
+// A workgroup is a part of a unit, a wave takes every fourth block of it; the tail is the last part, or a workgroup has the whole unit.  Workgroups go to
+// the 8 dies in turn: each die gets whole units, one after the other, so that no die has all first or all last parts, nor all units of a head.
 //
 // S^T = K q^T: four tiles of 16 keys, A = 16 keys x 32 channels of codes, B = the heads of the unit in columns 0 .. G-1.  Row m of
 // tile t is key 16*(m/4) + 4*t + m%4, so that lane (n, lg) gets the scores of head n for keys 16*lg .. +16 in the order of its 16 registers --
@@ -554,8 +554,9 @@ __device__ __forceinline__ void put_element(char* at, float v) {   // (v is an e
 
 // Grid (blocks a call can touch, units).  A workgroup takes a block that gets full: a thread has four consecutive rows of a
 // 16-byte column slice, so that it packs four channels of a key and four keys of a channel into words; the value words take a turn
-// through LDS to lie by channel.  Bound by HBM (16 prompts of up to 4096 rows, 32 heads: 6.0 TB/s read and written).  The first workgroup of a unit also writes the rows that stay unfinished (behind its own
-// loads: the block it has may be made of the old tail) and, unless others still have to read the old one, the new length.
+// through LDS to lie by channel.  Bound by HBM (16 prompts of up to 4096 rows, 32 heads: 6.1 TB/s read and written; fp32, 16 heads 5.9; with bounds kept up 2
+// to 4 % more time).  The first workgroup of a unit also writes the rows that stay unfinished (behind its own loads: the block it has may be made of the
+// old tail) and, unless others still have to read the old one, the new length.
 template <typename C, typename DT, int D>
 __global__ __launch_bounds__(WG) void corm_q8_append_kernel(const Q8AppendArgs a) {
   constexpr int ESZ = DT::ESZ, EPL = DT::EPL, ROWB = D * ESZ, SL = ROWB / 16;   // 16-byte slices of a row

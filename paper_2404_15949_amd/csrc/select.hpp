@@ -67,7 +67,8 @@ __device__ __forceinline__ void find_digit(const uint32_t* sh_hist, uint32_t* sh
   __syncthreads();
 }
 
-constexpr int CUT_LISTED = 128;   // keys that are counted against each other (512 units x 4352 weights, us: 64 8.9, 128 8.9, 256 9.0; 512 x 1500 10.5, 7.7, 7.1)
+// Keys that are counted against each other (512 units x 4352 weights, us: 64 8.9, 128 8.9, 256 9.0; 512 x 1500 10.5, 7.7, 7.1).
+constexpr int CUT_LISTED = 128;
 
 // Memory of find_cut.
 template <int NT, int BITS>
