@@ -482,7 +482,7 @@ class LayerState:
 
     def __init__(self, B, Hq, Hkv, d, Lcap, Tcap, w, r, dtype, thr_scale=1.0, device="cuda",
                  workspace: Optional[torch.Tensor] = None, want_masks=False, want_ring=True, score_dtype=None, want_bounds=False,
-                 want_weight=False):
+                 want_weight=False, blocks_workspace: Optional[torch.Tensor] = None):
         tdt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
         self.desc = make_desc(B, Hq, Hkv, d, Lcap, Tcap, w, r, dtype, score_dtype=score_dtype, thr_scale=thr_scale)
         self.ring_bits = self.desc.score_dtype == CORM_BIT
@@ -520,8 +520,9 @@ class LayerState:
         self.weight_keep = torch.zeros(B, Hkv, Lcap, dtype=torch.uint8, device=device) if want_weight else None
         self._dead = False  # there may be dead slots (step_lazy)
         self._rule = None   # what a state with accounts has evicted by since its prompt: "hits" or "weight"
-        self.blocks_workspace = None
-        if want_bounds or want_weight:
+        # (tens of megabytes for hundreds of heads: layers whose steps follow one another may share it, as they may `workspace`)
+        self.blocks_workspace = blocks_workspace
+        if blocks_workspace is None and (want_bounds or want_weight):
             self.blocks_workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
 
     def preload(self, K0: torch.Tensor, V0: torch.Tensor) -> None:

@@ -264,3 +264,12 @@ def test_the_choice_asks_for_its_workspace():
     """It has never done without one."""
     with pytest.raises(TypeError):
         corm.corm_block_select(_follower(14).st.desc, 4096, 4096, 4096, 8, 2, 4096)
+
+
+def test_layers_may_share_their_workspaces(monkeypatch):
+    """The second one is not made, however large: 2048 heads would take 137 MB a layer."""
+    plain_library(monkeypatch)
+    first = _follower(15, want_bounds=True).st
+    monkeypatch.setattr(corm, "corm_blocks_workspace_bytes", lambda desc: pytest.fail("made anew"))
+    second = _follower(16, want_bounds=True, want_weight=True, blocks_workspace=first.blocks_workspace).st
+    assert second.blocks_workspace is first.blocks_workspace
