@@ -603,7 +603,8 @@ class LayerState:
 
     def step_blocks(self, q, k_new, v_new, t, nsel, nlast=1, stream=None) -> None:
         """One decode step that attends to nsel blocks of 64 slots (the nlast newest and those with the highest score bounds): append,
-        the newest block's bounds, choice (self.blocks, until the next step), attention.  Nothing is recorded or evicted."""
+        the newest block's bounds, choice (self.blocks, until the next step), attention.  Nothing is evicted, and nothing recorded: a
+        ring's row of this step keeps what an older step left in it, so the literal corm_evict_mask is not for windows with such a step."""
         if self.bounds is None:
             raise RuntimeError("made without want_bounds")
         if self._dead:
