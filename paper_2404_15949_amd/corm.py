@@ -131,15 +131,18 @@ def _stream(stream) -> Optional[int]:
     return int(stream)
 
 
-def _capturing() -> bool:
-    return torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing()
-
-
 def _as_current(stream):
     """For torch's own operations beside a call that is given `stream`."""
     if stream is None:
         return contextlib.nullcontext()
     return torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(int(stream)))
+
+
+def _capturing(stream) -> bool:
+    if not torch.cuda.is_initialized():
+        return False
+    with _as_current(stream):
+        return torch.cuda.is_current_stream_capturing()
 
 
 # Launch options of the attend / step wrappers below when a call passes none: a setting of this BINDING (the
@@ -615,7 +618,7 @@ class LayerState:
         ws = self.blocks_workspace
         # The new row's entry of what the state evicts by.  While it has evicted by neither, all accounts behind the rows are empty, so last_hit
         # is the one to set; a graph may be replayed behind a cut by weight, so one that is captured sets the account and goes by that rule.
-        rule = "weight" if self.weight is not None and self._rule is None and _capturing() else self._rule
+        rule = "weight" if self.weight is not None and self._rule is None and _capturing(stream) else self._rule
         entry = self.weight if rule == "weight" else self.last_hit
         corm_append(self.desc, self.K, self.V, self.lens, self.pos, entry, k_new, v_new, t, self.status, stream=stream)
         self._rule = rule

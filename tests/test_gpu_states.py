@@ -113,6 +113,37 @@ class _OnStream:
         self._run(self._st.step_weigh, *args)
 
 
+def test_a_block_step_captured_on_a_given_stream_goes_by_accounts():
+    """The stream a step is given is the one that tells whether it is captured, not the current one."""
+    f = _follower(8, "f32", want_weight=True, want_bounds=True)
+    f.preload(60)
+    f.blocks(2, 1)
+    inputs, s, main = _tokens(f), torch.cuda.Stream(), torch.cuda.current_stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        with torch.cuda.stream(main):
+            f.st.step_blocks(*inputs, 2, 1, stream=s)
+    f.weigh(budget=30)
+    f.st = _Once(f.st, graph, inputs)
+    f.blocks(2, 1)
+
+
+class _Once:
+    """The state, with a block step that is a graph's."""
+
+    def __init__(self, st, graph, inputs):
+        self._st, self._graph, self._in = st, graph, inputs
+
+    def __getattr__(self, name):
+        return getattr(self._st, name)
+
+    def step_blocks(self, *args):
+        for x, y in zip(self._in, args[:4]):
+            x.copy_(y)
+        self._graph.replay()
+        torch.cuda.synchronize()
+
+
 def test_mixed_steps_on_another_stream():
     f = _follower(4, "bf16", want_weight=True, want_bounds=True)
     f.preload(60)

@@ -168,7 +168,7 @@ def test_a_row_of_a_block_step_has_never_been_hit(monkeypatch):
 def test_a_captured_block_step_may_be_replayed_behind_a_cut(monkeypatch):
     """What a graph holds cannot know of steps that come later: a block step captured on a state with accounts sets the new row's account."""
     plain_library(monkeypatch)
-    monkeypatch.setattr(corm, "_capturing", lambda: True)
+    monkeypatch.setattr(corm, "_capturing", lambda stream: True)
     f = _follower(8, want_weight=True, want_bounds=True)
     f.preload(100)
     f.st.renew_bounds()
