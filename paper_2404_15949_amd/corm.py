@@ -514,6 +514,8 @@ class LayerState:
         if workspace is None:
             workspace = torch.empty(corm_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
             corm_workspace_init(self.desc, workspace)
+        elif want_weight:
+            _check_room(workspace, corm_workspace_bytes(self.desc), "workspace")
         self.workspace = workspace
         # want_bounds: bounds of the blocks' keys, for step_blocks; want_weight: the keys' accounts, for step_weigh
         nblk = (Lcap + BLOCK - 1) // BLOCK
@@ -527,6 +529,8 @@ class LayerState:
         self.blocks_workspace = blocks_workspace
         if blocks_workspace is None and (want_bounds or want_weight):
             self.blocks_workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
+        elif blocks_workspace is not None:
+            _check_room(blocks_workspace, corm_blocks_workspace_bytes(self.desc), "blocks_workspace")
 
     def preload(self, K0: torch.Tensor, V0: torch.Tensor) -> None:
         """Copy n prompt keys/values [B,Hkv,n,d] into slots 0..n-1 (positions 0..n-1, never important yet, none dead, accounts empty)."""
@@ -611,7 +615,7 @@ class LayerState:
         if self.bounds is None:
             raise RuntimeError("made without want_bounds")
         if self._dead:
-            raise RuntimeError("behind step_lazy a state may hold dead slots, which step_blocks would attend to: preload it, or use step")
+            raise RuntimeError("behind step_lazy a state may hold dead slots, which step_blocks would attend to: preload it, or go on with step_lazy")
         _check_choice(self.desc, nsel, nlast)
         _check_query(self.desc, q)
         self.blocks = _lists_of(self._lists, self.desc, nsel)
@@ -668,6 +672,13 @@ def _check_query(desc, q) -> None:
         raise CormError(CORM_EINVAL, "q")
 
 
+def _check_room(x, nbytes, name) -> None:
+    if not x.is_contiguous():
+        raise ValueError(f"{name}: expected contiguous memory")
+    if x.numel() * x.element_size() < nbytes or x.data_ptr() % 256:
+        raise CormError(CORM_ECAPACITY, f"{name}: {nbytes} bytes, 256-byte aligned")
+
+
 def _block_lists(desc, device) -> torch.Tensor:
     """Room for the longest lists of chosen blocks."""
     return torch.empty(desc.B * desc.Hkv * _most_listed(desc), dtype=torch.int32, device=device)
@@ -701,6 +712,8 @@ class Q8State:
         self._lists = _block_lists(self.desc, device) if want_bounds else None
         if workspace is None:
             workspace = torch.empty(corm_blocks_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
+        else:
+            _check_room(workspace, corm_blocks_workspace_bytes(self.desc), "workspace")
         self.workspace = workspace
 
     def append(self, k, v, n_new=None, stream=None) -> None:

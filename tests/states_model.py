@@ -104,6 +104,7 @@ def plain_library(monkeypatch):
                     ("corm_compact", compact), ("corm_decode_step", decode_step), ("corm_prefill_seed", prefill_seed),
                     ("corm_decode_step_lazy", decode_step_lazy)):
         monkeypatch.setattr(corm, name, f)
+    monkeypatch.setattr(corm, "corm_workspace_init", lambda *a, **k: None)
     monkeypatch.setattr(corm, "_device", lambda: -1)
     return made
 
@@ -113,8 +114,7 @@ class Follower:
 
     def __init__(self, g, B, Hq, Hkv, d, cap, dtype, r=8, device="cpu", tcap=None, w=4, **wants):
         self.g, self.B, self.Hq, self.Hkv, self.d, self.dtype, self.r, self.device = g, B, Hq, Hkv, d, dtype, r, device
-        extra = {"workspace": torch.empty(256, dtype=torch.uint8)} if device == "cpu" else {}
-        self.st = corm.LayerState(B, Hq, Hkv, d, cap, tcap or cap, w, r, dtype, device=device, want_ring=False, **wants, **extra)
+        self.st = corm.LayerState(B, Hq, Hkv, d, cap, tcap or cap, w, r, dtype, device=device, want_ring=False, **wants)
         self.at = [(b, h) for b in range(B) for h in range(Hkv)]
         self.t = 0
 

@@ -218,7 +218,7 @@ def test_a_refused_step_leaves_the_8_bit_cache_as_it_was(monkeypatch):
     for name in ("corm_q8_append", "corm_q8_attend", "corm_block_select"):
         monkeypatch.setattr(corm, name, lambda *a, name=name, **k: made.append(name))
     monkeypatch.setattr(corm, "_device", lambda: -1)
-    states = [corm.Q8State(2, 4, 2, 64, 640, "f32", device="cpu", want_bounds=w, workspace=torch.empty(256, dtype=torch.uint8)) for w in (True, False)]
+    states = [corm.Q8State(2, 4, 2, 64, 640, "f32", device="cpu", want_bounds=w) for w in (True, False)]
     q, k = torch.zeros(2, 4, 64), torch.zeros(2, 2, 64)
     for nsel, nlast in ((-1, 1), (2, 0), (2, 3), (513, 1), (2.0, 1), (2, None)):
         for call in (lambda: states[0].step(q, k, k, nsel, nlast), lambda: states[0].attend(q, nsel, nlast)):
@@ -243,7 +243,7 @@ def test_steps_allocate_nothing(monkeypatch):
     monkeypatch.setattr(corm, "corm_q8_attend", lambda *a, **k: None)
     f = _follower(13, want_weight=True, want_bounds=True)
     f.preload(100)
-    q8 = corm.Q8State(2, 4, 2, 64, 256, "f32", device="cpu", want_bounds=True, workspace=torch.empty(256, dtype=torch.uint8))
+    q8 = corm.Q8State(2, 4, 2, 64, 256, "f32", device="cpu", want_bounds=True)
     tokens = [f.token()[1] for _ in range(5)]
 
     def none(*a, **k):
@@ -263,13 +263,38 @@ def test_steps_allocate_nothing(monkeypatch):
 def test_the_choice_asks_for_its_workspace():
     """It has never done without one."""
     with pytest.raises(TypeError):
-        corm.corm_block_select(_follower(14).st.desc, 4096, 4096, 4096, 8, 2, 4096)
+        corm.corm_block_select(corm.make_desc(2, 4, 2, 64, 256, 256, 4, 4, "f32"), 4096, 4096, 4096, 8, 2, 4096)
 
 
 def test_layers_may_share_their_workspaces(monkeypatch):
-    """The second one is not made, however large: 2048 heads would take 137 MB a layer."""
     plain_library(monkeypatch)
-    first = _follower(15, want_bounds=True).st
-    monkeypatch.setattr(corm, "corm_blocks_workspace_bytes", lambda desc: pytest.fail("made anew"))
-    second = _follower(16, want_bounds=True, want_weight=True, blocks_workspace=first.blocks_workspace).st
-    assert second.blocks_workspace is first.blocks_workspace
+    room = _room(corm.corm_blocks_workspace_bytes(corm.make_desc(2, 4, 2, 64, 256, 256, 4, 4, "f32")))
+    layers = [_follower(15, want_bounds=True, want_weight=w, blocks_workspace=room) for w in (True, False)]
+    for f in layers:
+        assert f.st.blocks_workspace is room
+        f.preload(100)
+        f.blocks(2, 1)
+
+
+def _room(nbytes):
+    x = torch.empty(nbytes + 256, dtype=torch.uint8)
+    x = x[-x.data_ptr() % 256:]
+    return x[:nbytes]
+
+
+def test_a_workspace_that_does_not_do_is_refused_where_it_is_given():
+    """Not by the second call of a step, behind the row that the first one has put in."""
+    args, small = (2, 4, 2, 64, 256), torch.empty(256, dtype=torch.uint8)
+    desc = corm.make_desc(*args, 256, 4, 4, "f32")
+    room = [_room(n(desc) + 256) for n in (corm.corm_workspace_bytes, corm.corm_blocks_workspace_bytes)]
+    layer = dict(device="cpu", want_ring=False, want_bounds=True, want_weight=True)
+    for bad in (small, room[1][16:], room[1][::2]):
+        for make in (lambda: corm.LayerState(*args, 256, 4, 4, "f32", workspace=room[0], blocks_workspace=bad, **layer),
+                     lambda: corm.Q8State(*args, "f32", device="cpu", workspace=bad)):
+            with pytest.raises((ValueError, corm.CormError)):
+                make()
+    for bad in (small, room[0][16:], room[0][::2]):
+        with pytest.raises((ValueError, corm.CormError)):
+            corm.LayerState(*args, 256, 4, 4, "f32", workspace=bad, blocks_workspace=room[1], **layer)
+    corm.LayerState(*args, 256, 4, 4, "f32", workspace=room[0], blocks_workspace=room[1], **layer)
+    corm.Q8State(*args, "f32", device="cpu", workspace=room[1])
