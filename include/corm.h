@@ -92,7 +92,8 @@ enum corm_dev_status {
   CORM_DEV_UNIT_FULL = 1, /* append skipped: lens == Lcap                                        */
   CORM_DEV_BAD_STEP = 2,  /* t < 1 or t > Tcap or a position outside [0,Tcap): record skipped   */
   CORM_DEV_BAD_LENS = 4,  /* lens outside [0,Lcap]: clamped                                      */
-  CORM_DEV_BAD_BLOCK = 8  /* a listed block beyond the unit's slots (or below -1): skipped       */
+  CORM_DEV_BAD_BLOCK = 8, /* a listed block beyond the unit's slots (or below -1): skipped       */
+  CORM_DEV_BAD_PAGE = 16  /* a slot whose table entry is no page of the pool: neither written nor read */
 };
 
 typedef struct corm_desc {
@@ -358,6 +359,85 @@ int corm_decode_attend_weigh(const corm_desc* desc, const void* q, const void* K
                              int32_t* status, const corm_launch_opts* opts, void* stream);
 int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int32_t* lens, int32_t budget, uint8_t* keep, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------------------------------------------
+ * A cache of pages, and the rows on their way into it.  Conventions as above; of the descriptor these calls read B, Hq, Hkv, d,
+ * Lcap, kv_dtype and, for attention, sm_scale; the other fields have to be valid and do nothing.
+ *
+ * corm_rows: where a call finds its rows of queries, keys and values (kv_dtype), e.g. in the packed output of a projection
+ * [B, n, (Hq + 2 Hkv) d].  Row of sequence b, token i, head h: base + b stride[0] + i stride[1] + h stride[2], in elements; the d
+ * elements of a row lie together.  Bases 16-byte aligned, strides >= 0 and whole multiples of 16 bytes.
+ *
+ * corm_rotation: what queries and keys go through, all in fp32 and rounded once where they are stored:
+ *   norm      y = x * weight / sqrt(mean of x^2 over the d channels + eps), per head, where q_norm (k_norm) [d], kv_dtype, is given
+ *   rotation  of the first rot channels, rot / 2 pairs: pair i is turned by the angle positions[axis(i)][b][token] * inv_freq[i], formed in
+ *             64 bits:  (u, v) -> gain * (u cos - v sin, v cos + u sin).  CORM_HALVES: pair i is channels i and i + rot / 2;
+ *             CORM_NEIGHBOURS: 2i and 2i + 1.  Channels at and above rot are normed only, values go as they are.
+ *   axes      1: every pair goes by the one position.  2..4 (time, height, width ..): axis x turns section[x] pairs (their sum is rot / 2):
+ *             in_turn = 0 the first section[0] pairs, the next section[1] and so on; in_turn = 1 axis x > 0 the pairs x, x + axes, ..
+ *             (section[x] of them), axis 0 all others.
+ * rot: 0 (norm alone) .. d, a multiple of 16.  inv_freq [rot / 2] float32 and positions [axes, B, n] int32 on the device. */
+typedef struct corm_rows {
+  const void *q, *k, *v;
+  int64_t q_stride[3], k_stride[3], v_stride[3];   /* of the sequence, the token, the head */
+} corm_rows;
+
+enum corm_pairing { CORM_HALVES = 0, CORM_NEIGHBOURS = 1 };
+
+typedef struct corm_rotation {
+  int32_t rot, pairing, axes, in_turn;
+  int32_t section[4];
+  float eps, gain;             /* gain: 1 unless the model scales what it rotates */
+  const float* inv_freq;       /* may be NULL with rot = 0 */
+  const void *q_norm, *k_norm; /* may be NULL: no norm */
+} corm_rotation;
+
+/* Rows of queries and keys normed and rotated, and the values beside them, laid out head by head as the other calls take them:
+ * q_out [B, Hq, n, d], k_out and v_out [B, Hkv, n, d] (for n = 1 the q, k_new and v_new of a decode step).  The first n_new[b] tokens of a sequence
+ * (device int32 [B], held to [0, n]; NULL = n); the others are neither read nor written.  q_out may be NULL: no queries, rows->q is not
+ * read then.  Outputs must not overlap the inputs. */
+int corm_rotate(const corm_desc* desc, const corm_rows* rows, const corm_rotation* rotation, const int32_t* positions, int32_t n,
+                const int32_t* n_new, void* q_out, void* k_out, void* v_out, void* stream);
+
+/* A pool of pages that hold `page` slots each, and the tables that say which of them a unit's slots lie in: slot i of a unit is row
+ * i % page of page table[..][i / page].
+ *   table_heads = 1     the KV heads of a sequence share a table and a length: table [B, 1, max_pages], lens [B, 1],
+ *                       K, V [npages, Hkv, page, d]
+ *   table_heads = Hkv   every KV head has its own, as eviction per head leaves them: table [B, Hkv, max_pages], lens [B, Hkv],
+ *                       K, V [npages, page, d]
+ *   dtype   kv_dtype: rows as they are.  CORM_I8, CORM_E4M3: codes with a scale per row, k_scale and v_scale (16-byte aligned) float32,
+ *           laid out as K and V without d; with amax the largest magnitude of the row's elements (fp32, before any rounding) and Q = 127 or 448
+ *             scale = fp32(amax / Q);  code = x * fp32(Q / amax) in fp32, rounded to the nearest (even) integer / e4m3 (OCP) value
+ *           (amax < 2^-100: zeros with scale 0; an element that is infinite or not a number: codes 0 and a scale that is none).
+ * page 16, 32, 64, 128 or 256; Lcap (the descriptor's) <= max_pages * page bounds every length.  Entries of the table behind a unit's last
+ * page are never used and may hold anything.  An entry below 0 or >= npages is no page: its slots are neither written nor read
+ * (CORM_DEV_BAD_PAGE).  A page that several tables hold is read by all of them; two units that write to it race. */
+typedef struct corm_pages {
+  int32_t dtype, page, npages, max_pages, table_heads;
+  int32_t reserved;            /* 0 */
+  void *K, *V;
+  float *k_scale, *v_scale;    /* NULL unless dtype is one of codes */
+  const int32_t* table;
+} corm_pages;
+
+/* Rows to slots lens .. of their units: the first n_new[b] tokens of a sequence (as in corm_rotate).  lens_out receives the new lengths and
+ * may be lens.  A unit that has no room for all its rows (Lcap) gets none and keeps its length (CORM_DEV_UNIT_FULL), one whose length is
+ * outside [0, Lcap] too (CORM_DEV_BAD_LENS).  rotation (may be NULL: rows come ready): keys are normed and rotated on the way, and queries, where
+ * q_out [B, Hq, n, d] is given (else it is NULL and rows->q is not read).  Codes are formed from the fp32 values, rounded once.  1 <= n <= Lcap. */
+int corm_paged_append(const corm_desc* desc, const corm_pages* pages, const corm_rows* rows, const corm_rotation* rotation,
+                      const int32_t* positions, int32_t n, const int32_t* n_new, void* q_out, const int32_t* lens, int32_t* lens_out,
+                      int32_t* status, void* stream);
+
+/* Slots 0 .. min(lens, n) - 1 of every unit into K_out, V_out [B, Hkv, n, d], kv_dtype (codes: fp32(code * scale), rounded to it).  Rows at and
+ * above that, and of slots without a page, are left as they were. */
+int corm_paged_read(const corm_desc* desc, const corm_pages* pages, const int32_t* lens, int32_t n, void* K_out, void* V_out,
+                    int32_t* status, void* stream);
+
+/* Decode attention (Eq. 1) over the slots < lens: q [B, Hq, d] kv_dtype, out [B, Hq, d] float32, 0 where a unit has no slot that can be read.
+ * Workspace (256-byte aligned, of corm_paged_workspace_bytes): partials alone; nothing in it has to be prepared or survives a call. */
+int corm_paged_workspace_bytes(const corm_desc* desc, size_t* bytes);
+int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void* q, const int32_t* lens, float* out, void* workspace,
+                      size_t workspace_bytes, int32_t* status, void* stream);
 
 /* HIP graph capture.  The step, seeding and standalone calls enqueue kernels only (no allocation, no memset,
  * no host synchronization), so a caller may capture them in a HIP graph on `stream` and replay it with the

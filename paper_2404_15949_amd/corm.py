@@ -20,7 +20,8 @@ LIB_PATH = os.path.join(_HERE, "libcorm.so")
 
 CORM_F32, CORM_BF16, CORM_BIT, CORM_I8, CORM_E4M3 = 0, 1, 2, 3, 4
 CORM_OK, CORM_EINVAL, CORM_EUNSUPPORTED, CORM_ECAPACITY, CORM_EHIP = 0, -1, -2, -3, -4
-CORM_DEV_UNIT_FULL, CORM_DEV_BAD_STEP, CORM_DEV_BAD_LENS, CORM_DEV_BAD_BLOCK = 1, 2, 4, 8
+CORM_DEV_UNIT_FULL, CORM_DEV_BAD_STEP, CORM_DEV_BAD_LENS, CORM_DEV_BAD_BLOCK, CORM_DEV_BAD_PAGE = 1, 2, 4, 8, 16
+CORM_HALVES, CORM_NEIGHBOURS = 0, 1
 BLOCK = 64   # slots per block of the 8-bit cache and of the calls that choose blocks
 CORM_STATIC_SCRATCH_BYTES = 40 << 20
 
@@ -28,7 +29,8 @@ EXPORTS = ("corm_version", "corm_strerror", "corm_workspace_bytes", "corm_worksp
            "corm_decode_attend", "corm_decode_attend_static", "corm_evict_mask", "corm_evict_mask_summary", "corm_row_density", "corm_compact",
            "corm_decode_step", "corm_step_attend", "corm_step_evict", "corm_decode_step_lazy", "corm_prefill_seed",
            "corm_selected_path", "corm_threshold", "corm_blocks_workspace_bytes", "corm_q8_append", "corm_q8_attend",
-           "corm_block_bounds", "corm_block_select", "corm_block_attend", "corm_decode_attend_weigh", "corm_evict_mask_weight")
+           "corm_block_bounds", "corm_block_select", "corm_block_attend", "corm_decode_attend_weigh", "corm_evict_mask_weight",
+           "corm_rotate", "corm_paged_append", "corm_paged_read", "corm_paged_workspace_bytes", "corm_paged_attend")
 
 
 class corm_desc(ctypes.Structure):
@@ -41,6 +43,23 @@ class corm_desc(ctypes.Structure):
 class corm_launch_opts(ctypes.Structure):
     _fields_ = [("path", ctypes.c_int32), ("reserved", ctypes.c_int32),
                 ("attend_start_event", ctypes.c_void_p), ("attend_stop_event", ctypes.c_void_p)]
+
+
+class corm_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 3),
+                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+
+
+class corm_rotation(ctypes.Structure):
+    _fields_ = [("rot", ctypes.c_int32), ("pairing", ctypes.c_int32), ("axes", ctypes.c_int32), ("in_turn", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 4), ("eps", ctypes.c_float), ("gain", ctypes.c_float), ("inv_freq", ctypes.c_void_p),
+                ("q_norm", ctypes.c_void_p), ("k_norm", ctypes.c_void_p)]
+
+
+class corm_pages(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("page", ctypes.c_int32), ("npages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+                ("table_heads", ctypes.c_int32), ("reserved", ctypes.c_int32), ("K", ctypes.c_void_p), ("V", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p), ("table", ctypes.c_void_p)]
 
 
 class CormError(RuntimeError):
@@ -95,6 +114,12 @@ def lib() -> ctypes.CDLL:
         L.corm_block_attend.argtypes = [dp, vp, vp, vp, i32p, i32p, i32, vp, vp, sz, i32p, vp]
         L.corm_decode_attend_weigh.argtypes = [dp, vp, vp, vp, i32p, vp, vp, vp, vp, sz, i32p, op, vp]
         L.corm_evict_mask_weight.argtypes = [dp, vp, i32p, i32, vp, vp, sz, vp]
+        rp, tp, pp = (ctypes.POINTER(c) for c in (corm_rows, corm_rotation, corm_pages))
+        L.corm_rotate.argtypes = [dp, rp, tp, i32p, i32, i32p, vp, vp, vp, vp]
+        L.corm_paged_append.argtypes = [dp, pp, rp, tp, i32p, i32, i32p, vp, i32p, i32p, i32p, vp]
+        L.corm_paged_read.argtypes = [dp, pp, i32p, i32, vp, vp, i32p, vp]
+        L.corm_paged_workspace_bytes.argtypes = [dp, ctypes.POINTER(ctypes.c_size_t)]
+        L.corm_paged_attend.argtypes = [dp, pp, vp, i32p, vp, vp, sz, i32p, vp]
         L.corm_threshold.argtypes = [ctypes.c_float, i32p, ctypes.c_int32, vp, vp]
         for name in EXPORTS:
             if name not in ("corm_version", "corm_strerror"):
@@ -478,6 +503,147 @@ def corm_evict_mask_weight(desc, weight, lens, budget, keep, workspace, workspac
     return _check(rc, "corm_evict_mask_weight") if check else rc
 
 
+# ---- a cache of pages, and the rows on their way into it
+
+class Rotation:
+    """What a model does to its queries and keys before attention (corm_rotation): norms per head and the position rotation.  Made once.
+
+    inv_freq [rot / 2] float32 (None: norms alone); q_norm, k_norm [d] in the KV type; pairing "halves" or "neighbours"; sections: the pairs of
+    each axis (None: one axis), dealt in blocks or in_turn."""
+
+    def __init__(self, inv_freq, q_norm=None, k_norm=None, eps=1e-6, pairing="halves", sections=None, in_turn=False, gain=1.0):
+        half = 0 if inv_freq is None else inv_freq.numel()
+        sections = [half] if sections is None else [operator.index(x) for x in sections]
+        if not 1 <= len(sections) <= 4:
+            raise ValueError(f"sections: one to four axes, got {len(sections)}")
+        self.inv_freq, self.q_norm, self.k_norm, self.axes, self.rot = inv_freq, q_norm, k_norm, len(sections), 2 * half
+        self.c = corm_rotation(2 * half, {"halves": CORM_HALVES, "neighbours": CORM_NEIGHBOURS}[pairing], len(sections), int(bool(in_turn)),
+                               (ctypes.c_int32 * 4)(*sections), eps, gain)
+
+    def _bind(self, desc, device):
+        _, _, _, kv = _sizes(desc)
+        self.c.inv_freq = _dev(self.inv_freq, self.rot // 2, _F4, "inv_freq", device)
+        self.c.q_norm = _dev(self.q_norm, desc.d, kv, "q_norm", device)
+        self.c.k_norm = _dev(self.k_norm, desc.d, kv, "k_norm", device)
+        return ctypes.byref(self.c)
+
+
+class Pages:
+    """A pool of pages and the tables of the units (corm_pages).  Made once; the tensors' contents may change, the tables' among them.
+
+    K, V [npages, page, d] with table [B, Hkv, max_pages] int32, or [npages, Hkv, page, d] with table [B, 1, max_pages]: in the KV type, or int8 or
+    float8_e4m3fn with k_scale and v_scale, float32, of the same shape without d."""
+
+    def __init__(self, desc, K, V, table, k_scale=None, v_scale=None):
+        if table.dim() != 3 or K.dim() not in (3, 4) or K.shape != V.shape or K.dtype != V.dtype:
+            raise ValueError(f"pages: K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}, table {tuple(table.shape)}")
+        _, _, _, kv = _sizes(desc)
+        code = _code_ids.get(K.dtype)
+        self.desc, self.K, self.V, self.table, self.k_scale, self.v_scale = desc, K, V, table, k_scale, v_scale
+        self.types = kv if code is None else (K.dtype,)
+        shared = K.dim() == 4
+        if tuple(K.shape[1:]) != ((desc.Hkv,) if shared else ()) + (K.shape[-2], desc.d) or tuple(table.shape[:2]) != (desc.B, 1 if shared else desc.Hkv):
+            raise ValueError(f"pages: K {tuple(K.shape)} and table {tuple(table.shape)} are not those of B {desc.B}, Hkv {desc.Hkv}, d {desc.d}")
+        self.tables = desc.B * table.shape[1]
+        self.c = corm_pages(desc.kv_dtype if code is None else code, K.shape[-2], K.shape[0], table.shape[2], table.shape[1], 0)
+
+    def _bind(self, desc, device):
+        if (desc.B, desc.Hkv, desc.d, desc.kv_dtype) != (self.desc.B, self.desc.Hkv, self.desc.d, self.desc.kv_dtype):
+            raise ValueError("pages: made for another descriptor")
+        n, c = self.K.numel(), self.c
+        c.K, c.V = _dev(self.K, n, self.types, "K", device), _dev(self.V, n, self.types, "V", device)
+        c.k_scale = _dev(self.k_scale, n // desc.d, _F4, "k_scale", device)
+        c.v_scale = _dev(self.v_scale, n // desc.d, _F4, "v_scale", device)
+        c.table = _dev(self.table, self.tables * c.max_pages, _I32, "table", device)
+        return ctypes.byref(c)
+
+
+def _strided(x, desc, heads, n, name, device):
+    """Pointer and strides (sequence, token, head) of rows [B, heads, n, d] or, of one token, [B, heads, d]: any view whose rows lie whole."""
+    _, _, _, kv = _sizes(desc)
+    if x.dim() == 3:
+        x = x.unsqueeze(2)
+    if x.dtype not in kv or tuple(x.shape) != (desc.B, heads, n, desc.d) or x.stride(3) != 1 or x.get_device() != device:
+        raise ValueError(f"{name}: expected {(desc.B, heads, n, desc.d)} of {kv} on the current device with its rows whole, got {x.dtype} "
+                         f"{tuple(x.shape)} with strides {x.stride()} on {x.device}")
+    b, h, t, _ = x.stride()
+    return x.data_ptr(), (ctypes.c_int64 * 3)(b if desc.B > 1 else 0, t if n > 1 else 0, h if heads > 1 else 0)
+
+
+def _rows_of(desc, q, k, v, device):
+    n = 1 if k.dim() == 3 else k.shape[2]
+    r = corm_rows()
+    if q is not None:
+        r.q, r.q_stride = _strided(q, desc, desc.Hq, n, "q", device)
+    r.k, r.k_stride = _strided(k, desc, desc.Hkv, n, "k", device)
+    r.v, r.v_stride = _strided(v, desc, desc.Hkv, n, "v", device)
+    return r, n
+
+
+def _turning(desc, rotation, positions, n, device):
+    if rotation is None:
+        return None, None
+    return rotation._bind(desc, device), _dev(positions, rotation.axes * desc.B * n, _I32, "positions", device)
+
+
+def corm_rotate(desc, q, k, v, rotation, positions, q_out, k_out, v_out, n_new=None, stream=None, check=True) -> int:
+    """q [B,Hq,n,d] (with q_out None: not read), k, v [B,Hkv,n,d], any strides (a projection's output token by token: its view, transposed);
+    positions [axes,B,n] int32."""
+    at = _device()
+    rows, n = _rows_of(desc, None if q_out is None else q, k, v, at)
+    units, heads, _, kv = _sizes(desc)
+    turn, pos = _turning(desc, rotation, positions, n, at)
+    rc = lib().corm_rotate(ctypes.byref(desc), ctypes.byref(rows), turn, pos, n, _dev(n_new, desc.B, _I32, "n_new", at),
+                           _dev(q_out, heads * n * desc.d, kv, "q_out", at), _dev(k_out, units * n * desc.d, kv, "k_out", at),
+                           _dev(v_out, units * n * desc.d, kv, "v_out", at), _on(stream, at))
+    return _check(rc, "corm_rotate") if check else rc
+
+
+def corm_paged_append(desc, pages, k, v, lens, lens_out, n_new=None, q=None, q_out=None, rotation=None, positions=None, status=None,
+                      stream=None, check=True) -> int:
+    """k, v (and q, where q_out is given) as in corm_rotate; lens, lens_out [B, tables per sequence]."""
+    at = _device()
+    rows, n = _rows_of(desc, None if q_out is None else q, k, v, at)
+    turn, pos = _turning(desc, rotation, positions, n, at)
+    rc = lib().corm_paged_append(ctypes.byref(desc), pages._bind(desc, at), ctypes.byref(rows), turn, pos, n,
+                                 _dev(n_new, desc.B, _I32, "n_new", at), _dev(q_out, desc.B * desc.Hq * n * desc.d, _sizes(desc)[3], "q_out", at),
+                                 _dev(lens, pages.tables, _I32, "lens", at), _dev(lens_out, pages.tables, _I32, "lens_out", at),
+                                 _dev(status, None, _I32, "status", at), _on(stream, at))
+    return _check(rc, "corm_paged_append") if check else rc
+
+
+def corm_paged_read(desc, pages, lens, K_out, V_out, status=None, stream=None, check=True) -> int:
+    """K_out, V_out [B,Hkv,n,d]"""
+    at = _device()
+    units, _, _, kv = _sizes(desc)
+    if K_out.dim() != 4 or K_out.shape != V_out.shape:
+        raise ValueError(f"K_out {tuple(K_out.shape)}, V_out {tuple(V_out.shape)}: expected [B, Hkv, n, d]")
+    n = K_out.shape[2]
+    rc = lib().corm_paged_read(ctypes.byref(desc), pages._bind(desc, at), _dev(lens, pages.tables, _I32, "lens", at), n,
+                               _dev(K_out, units * n * desc.d, kv, "K_out", at), _dev(V_out, units * n * desc.d, kv, "V_out", at),
+                               _dev(status, None, _I32, "status", at), _on(stream, at))
+    return _check(rc, "corm_paged_read") if check else rc
+
+
+def corm_paged_workspace_bytes(desc: corm_desc, check=True) -> int:
+    n = ctypes.c_size_t(0)
+    rc = lib().corm_paged_workspace_bytes(ctypes.byref(desc), ctypes.byref(n))
+    if check:
+        _check(rc, "corm_paged_workspace_bytes")
+        return n.value
+    return rc
+
+
+def corm_paged_attend(desc, pages, q, lens, out, workspace, workspace_bytes=None, status=None, stream=None, check=True) -> int:
+    """q [B,Hq,d] -> out [B,Hq,d] float32"""
+    at = _device()
+    heads, kv = desc.B * desc.Hq, _sizes(desc)[3]
+    rc = lib().corm_paged_attend(ctypes.byref(desc), pages._bind(desc, at), _dev(q, heads * desc.d, kv, "q", at),
+                                 _dev(lens, pages.tables, _I32, "lens", at), _dev(out, heads * desc.d, _F4, "out", at), _scratch(workspace, at),
+                                 _nbytes(workspace, workspace_bytes), _dev(status, None, _I32, "status", at), _on(stream, at))
+    return _check(rc, "corm_paged_attend") if check else rc
+
+
 # ---- device-memory plumbing for one layer (allocation only; no arithmetic of the method)
 
 class LayerState:
@@ -744,3 +910,64 @@ class Q8State:
         _check_query(self.desc, q)
         self.append(k_new, v_new, stream=stream)
         self.attend(q, nsel, nlast, stream=stream)
+
+
+class PagedState:
+    """The device arrays of one layer's cache of pages, in the layouts corm.h documents.  The caller deals the pages: table [B, 1, max_pages], or
+    [B, Hkv, max_pages] with per_head, holds -1 (no page) until it is written (deal() gives every unit max_pages of its own)."""
+
+    def __init__(self, B, Hq, Hkv, d, npages, max_pages, dtype, page=16, code=None, per_head=False, device="cuda",
+                 workspace: Optional[torch.Tensor] = None):
+        tdt = {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+        cdt = {None: tdt, "i8": torch.int8, "e4m3": torch.float8_e4m3fn}[code]
+        cap = max_pages * page
+        self.desc = make_desc(B, Hq, Hkv, d, cap, cap, 1, 1, dtype)
+        self.B, self.Hq, self.Hkv, self.d, self.page, self.dtype, self.code = B, Hq, Hkv, d, page, tdt, code
+        shape = (npages,) + (() if per_head else (Hkv,)) + (page, d)
+        tables = Hkv if per_head else 1
+        self.K = torch.zeros(shape, dtype=torch.int8 if code else tdt, device=device).view(cdt)
+        self.V = torch.zeros(shape, dtype=torch.int8 if code else tdt, device=device).view(cdt)
+        self.k_scale = torch.zeros(shape[:-1], dtype=torch.float32, device=device) if code else None
+        self.v_scale = torch.zeros(shape[:-1], dtype=torch.float32, device=device) if code else None
+        self.table = torch.full((B, tables, max_pages), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(B, tables, dtype=torch.int32, device=device)
+        self.pages = Pages(self.desc, self.K, self.V, self.table, self.k_scale, self.v_scale)
+        self.q = torch.zeros(B, Hq, d, dtype=tdt, device=device)   # a step's queries, rotated
+        self.out = torch.zeros(B, Hq, d, dtype=torch.float32, device=device)
+        self.status = torch.zeros(1, dtype=torch.int32, device=device)
+        if workspace is None:
+            workspace = torch.empty(corm_paged_workspace_bytes(self.desc), dtype=torch.uint8, device=device)
+        else:
+            _check_room(workspace, corm_paged_workspace_bytes(self.desc), "workspace")
+        self.workspace = workspace
+
+    def deal(self) -> None:
+        """Every unit's pages, one unit behind the other."""
+        if self.K.shape[0] < self.table.numel():
+            raise CormError(CORM_ECAPACITY, f"{self.K.shape[0]} pages for tables of {self.table.numel()}")
+        self.table.copy_(torch.arange(self.table.numel(), dtype=torch.int32, device=self.table.device).view_as(self.table))
+
+    def append(self, k, v, n_new=None, q=None, q_out=None, rotation=None, positions=None, stream=None) -> None:
+        """k, v [B,Hkv,n,d] (or [B,Hkv,d]: one row), any strides; n_new [B]: the rows of a sequence that count.  With a rotation keys are normed and
+        rotated on the way, and queries q [B,Hq,n,d] into q_out."""
+        corm_paged_append(self.desc, self.pages, k, v, self.lens, self.lens, n_new=n_new, q=q, q_out=q_out, rotation=rotation, positions=positions,
+                          status=self.status, stream=stream)
+
+    def read(self, K_out, V_out, stream=None) -> None:
+        """The rows of every unit's slots into K_out, V_out [B,Hkv,n,d]."""
+        corm_paged_read(self.desc, self.pages, self.lens, K_out, V_out, status=self.status, stream=stream)
+
+    def attend(self, q, stream=None) -> None:
+        """q [B,Hq,d] -> out"""
+        corm_paged_attend(self.desc, self.pages, q, self.lens, self.out, self.workspace, status=self.status, stream=stream)
+
+    def step(self, q, k_new, v_new, rotation=None, positions=None, stream=None) -> None:
+        """One decode step: the new row goes in, the query attends to all keys, itself among them.  With a rotation queries and keys come as the
+        projection leaves them (positions [axes,B,1])."""
+        if rotation is None:
+            _check_query(self.desc, q)
+            self.append(k_new, v_new, stream=stream)
+            self.attend(q, stream=stream)
+        else:
+            self.append(k_new, v_new, q=q, q_out=self.q, rotation=rotation, positions=positions, stream=stream)
+            self.attend(self.q, stream=stream)

@@ -1,6 +1,7 @@
 // HIP kernels (gfx950 / CDNA4, wave64) and C ABI of what bounds a decode step's reads beside CORM's own rule: a cache held in 8
 // bits, attention over chosen blocks of it or of the plain cache, and the eviction decision by accumulated attention weight.
 // One translation unit:
+//   codes.hpp          8-bit codes
 //   q8.hpp             rows quantised into blocks of 64, and attention over them (q.K^T and p.V on the matrix cores)
 //   select.hpp         the k-th largest of many numbers
 //   blocks.hpp         bounds of the blocks' keys, the choice, attention over the chosen ones
@@ -17,6 +18,7 @@
 
 #include "common.hpp"
 #include "attend.hpp"
+#include "codes.hpp"
 #include "q8.hpp"
 #include "select.hpp"
 #include "blocks.hpp"
