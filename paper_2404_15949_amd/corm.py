@@ -518,13 +518,19 @@ class Rotation:
             raise ValueError(f"sections: one to four axes, got {len(sections)}")
         self.inv_freq, self.q_norm, self.k_norm, self.axes, self.rot = inv_freq, q_norm, k_norm, len(sections), 2 * half
         self.c = corm_rotation(2 * half, {"halves": CORM_HALVES, "neighbours": CORM_NEIGHBOURS}[pairing], len(sections), int(bool(in_turn)),
-                               (ctypes.c_int32 * 4)(*sections), eps, gain)
+                               tuple(sections), eps, gain)
+        self._seen = None
 
     def _bind(self, desc, device):
-        _, _, _, kv = _sizes(desc)
-        self.c.inv_freq = _dev(self.inv_freq, self.rot // 2, _F4, "inv_freq", device)
-        self.c.q_norm = _dev(self.q_norm, desc.d, kv, "q_norm", device)
-        self.c.k_norm = _dev(self.k_norm, desc.d, kv, "k_norm", device)
+        # the tensors are looked at again only where one has got other memory (a module moved its weights), or another call wants another type of them
+        seen = (device, desc.kv_dtype, desc.d, *[None if x is None else x.data_ptr() for x in (self.inv_freq, self.q_norm, self.k_norm)])
+        if seen != self._seen:
+            _, _, _, kv = _sizes(desc)
+            self._seen = None
+            self.c.inv_freq = _dev(self.inv_freq, self.rot // 2, _F4, "inv_freq", device)
+            self.c.q_norm = _dev(self.q_norm, desc.d, kv, "q_norm", device)
+            self.c.k_norm = _dev(self.k_norm, desc.d, kv, "k_norm", device)
+            self._seen = seen
         return ctypes.byref(self.c)
 
 
@@ -539,74 +545,78 @@ class Pages:
             raise ValueError(f"pages: K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}, table {tuple(table.shape)}")
         _, _, _, kv = _sizes(desc)
         code = _code_ids.get(K.dtype)
-        self.desc, self.K, self.V, self.table, self.k_scale, self.v_scale = desc, K, V, table, k_scale, v_scale
+        self.K, self.V, self.table, self.k_scale, self.v_scale = K, V, table, k_scale, v_scale
         self.types = kv if code is None else (K.dtype,)
         shared = K.dim() == 4
         if tuple(K.shape[1:]) != ((desc.Hkv,) if shared else ()) + (K.shape[-2], desc.d) or tuple(table.shape[:2]) != (desc.B, 1 if shared else desc.Hkv):
             raise ValueError(f"pages: K {tuple(K.shape)} and table {tuple(table.shape)} are not those of B {desc.B}, Hkv {desc.Hkv}, d {desc.d}")
+        self._of = (desc.B, desc.Hkv, desc.d, desc.kv_dtype)
         self.tables = desc.B * table.shape[1]
         self.c = corm_pages(desc.kv_dtype if code is None else code, K.shape[-2], K.shape[0], table.shape[2], table.shape[1], 0)
+        self._seen = None
 
     def _bind(self, desc, device):
-        if (desc.B, desc.Hkv, desc.d, desc.kv_dtype) != (self.desc.B, self.desc.Hkv, self.desc.d, self.desc.kv_dtype):
+        if (desc.B, desc.Hkv, desc.d, desc.kv_dtype) != self._of:
             raise ValueError("pages: made for another descriptor")
-        n, c = self.K.numel(), self.c
-        c.K, c.V = _dev(self.K, n, self.types, "K", device), _dev(self.V, n, self.types, "V", device)
-        c.k_scale = _dev(self.k_scale, n // desc.d, _F4, "k_scale", device)
-        c.v_scale = _dev(self.v_scale, n // desc.d, _F4, "v_scale", device)
-        c.table = _dev(self.table, self.tables * c.max_pages, _I32, "table", device)
-        return ctypes.byref(c)
+        seen = (device, self.K.data_ptr(), self.V.data_ptr(), self.table.data_ptr(), 0 if self.k_scale is None else self.k_scale.data_ptr(),
+                0 if self.v_scale is None else self.v_scale.data_ptr())
+        if seen != self._seen:      # (as in Rotation)
+            n, c = self.K.numel(), self.c
+            self._seen = None
+            c.K, c.V = _dev(self.K, n, self.types, "K", device), _dev(self.V, n, self.types, "V", device)
+            c.k_scale = _dev(self.k_scale, n // desc.d, _F4, "k_scale", device)
+            c.v_scale = _dev(self.v_scale, n // desc.d, _F4, "v_scale", device)
+            c.table = _dev(self.table, self.tables * c.max_pages, _I32, "table", device)
+            self._seen = seen
+        return ctypes.byref(self.c)
 
 
-def _strided(x, desc, heads, n, name, device):
+def _strided(x, shape, kv, name, device):
     """Pointer and strides (sequence, token, head) of rows [B, heads, n, d] or, of one token, [B, heads, d]: any view whose rows lie whole."""
-    _, _, _, kv = _sizes(desc)
-    if x.dim() == 3:
-        x = x.unsqueeze(2)
-    if x.dtype not in kv or tuple(x.shape) != (desc.B, heads, n, desc.d) or x.stride(3) != 1 or x.get_device() != device:
-        raise ValueError(f"{name}: expected {(desc.B, heads, n, desc.d)} of {kv} on the current device with its rows whole, got {x.dtype} "
-                         f"{tuple(x.shape)} with strides {x.stride()} on {x.device}")
-    b, h, t, _ = x.stride()
-    return x.data_ptr(), (ctypes.c_int64 * 3)(b if desc.B > 1 else 0, t if n > 1 else 0, h if heads > 1 else 0)
+    at = x.stride()
+    if x.dtype is not kv or x.shape != (shape if len(at) == 4 else shape[:2] + shape[3:]) or at[-1] != 1 or x.get_device() != device:
+        raise ValueError(f"{name}: expected {shape} of {kv} on the current device with its rows whole, got {x.dtype} {tuple(x.shape)} with strides "
+                         f"{at} on {x.device}")
+    B, heads, n, _ = shape
+    return x.data_ptr(), (at[0] if B > 1 else 0, at[2] if n > 1 else 0, at[1] if heads > 1 else 0)
 
 
-def _rows_of(desc, q, k, v, device):
-    n = 1 if k.dim() == 3 else k.shape[2]
-    r = corm_rows()
-    if q is not None:
-        r.q, r.q_stride = _strided(q, desc, desc.Hq, n, "q", device)
-    r.k, r.k_stride = _strided(k, desc, desc.Hkv, n, "k", device)
-    r.v, r.v_stride = _strided(v, desc, desc.Hkv, n, "v", device)
-    return r, n
+def _rows_of(desc, q, k, v, n, device):
+    B, Hkv, d, kv = desc.B, desc.Hkv, desc.d, _FLOATS.get(desc.kv_dtype)
+    qp, qs = (None, (0, 0, 0)) if q is None else _strided(q, (B, desc.Hq, n, d), kv, "q", device)
+    kp, ks = _strided(k, (B, Hkv, n, d), kv, "k", device)
+    vp, vs = _strided(v, (B, Hkv, n, d), kv, "v", device)
+    return corm_rows(qp, kp, vp, qs, ks, vs)
 
 
-def _turning(desc, rotation, positions, n, device):
-    if rotation is None:
-        return None, None
-    return rotation._bind(desc, device), _dev(positions, rotation.axes * desc.B * n, _I32, "positions", device)
+def _tokens(k) -> int:
+    return 1 if k.dim() == 3 else k.shape[2]
 
 
 def corm_rotate(desc, q, k, v, rotation, positions, q_out, k_out, v_out, n_new=None, stream=None, check=True) -> int:
     """q [B,Hq,n,d] (with q_out None: not read), k, v [B,Hkv,n,d], any strides (a projection's output token by token: its view, transposed);
     positions [axes,B,n] int32."""
-    at = _device()
-    rows, n = _rows_of(desc, None if q_out is None else q, k, v, at)
-    units, heads, _, kv = _sizes(desc)
-    turn, pos = _turning(desc, rotation, positions, n, at)
-    rc = lib().corm_rotate(ctypes.byref(desc), ctypes.byref(rows), turn, pos, n, _dev(n_new, desc.B, _I32, "n_new", at),
-                           _dev(q_out, heads * n * desc.d, kv, "q_out", at), _dev(k_out, units * n * desc.d, kv, "k_out", at),
-                           _dev(v_out, units * n * desc.d, kv, "v_out", at), _on(stream, at))
+    at, n = _device(), _tokens(k)
+    rows = _rows_of(desc, None if q_out is None else q, k, v, n, at)
+    kv, each = (_FLOATS.get(desc.kv_dtype),), desc.B * n * desc.d
+    rc = lib().corm_rotate(ctypes.byref(desc), ctypes.byref(rows), rotation._bind(desc, at),
+                           _dev(positions, rotation.axes * desc.B * n, _I32, "positions", at), n, _dev(n_new, desc.B, _I32, "n_new", at),
+                           _dev(q_out, desc.Hq * each, kv, "q_out", at), _dev(k_out, desc.Hkv * each, kv, "k_out", at),
+                           _dev(v_out, desc.Hkv * each, kv, "v_out", at), _on(stream, at))
     return _check(rc, "corm_rotate") if check else rc
 
 
 def corm_paged_append(desc, pages, k, v, lens, lens_out, n_new=None, q=None, q_out=None, rotation=None, positions=None, status=None,
                       stream=None, check=True) -> int:
     """k, v (and q, where q_out is given) as in corm_rotate; lens, lens_out [B, tables per sequence]."""
-    at = _device()
-    rows, n = _rows_of(desc, None if q_out is None else q, k, v, at)
-    turn, pos = _turning(desc, rotation, positions, n, at)
+    at, n = _device(), _tokens(k)
+    rows = _rows_of(desc, None if q_out is None else q, k, v, n, at)
+    turn = pos = None
+    if rotation is not None:
+        turn, pos = rotation._bind(desc, at), _dev(positions, rotation.axes * desc.B * n, _I32, "positions", at)
     rc = lib().corm_paged_append(ctypes.byref(desc), pages._bind(desc, at), ctypes.byref(rows), turn, pos, n,
-                                 _dev(n_new, desc.B, _I32, "n_new", at), _dev(q_out, desc.B * desc.Hq * n * desc.d, _sizes(desc)[3], "q_out", at),
+                                 _dev(n_new, desc.B, _I32, "n_new", at),
+                                 _dev(q_out, desc.B * desc.Hq * n * desc.d, (_FLOATS.get(desc.kv_dtype),), "q_out", at),
                                  _dev(lens, pages.tables, _I32, "lens", at), _dev(lens_out, pages.tables, _I32, "lens_out", at),
                                  _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_paged_append") if check else rc

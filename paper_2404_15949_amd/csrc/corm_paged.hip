@@ -88,31 +88,43 @@ void bind_rows(const corm_desc* d, const corm_rows* r, const corm_rotation* rot,
   if (rot) {
     a.inv_freq = rot->inv_freq; a.positions = positions;
     a.q_norm = reinterpret_cast<const char*>(rot->q_norm); a.k_norm = reinterpret_cast<const char*>(rot->k_norm);
-    a.rot = rot->rot; a.neighbours = rot->pairing == CORM_NEIGHBOURS; a.axes = rot->axes; a.in_turn = rot->in_turn != 0;
+    a.rot = rot->rot; a.axes = rot->axes; a.in_turn = rot->in_turn != 0;
     for (int i = 0; i < 4; ++i) a.section[i] = i < rot->axes ? rot->section[i] : 0;
     a.eps = rot->eps; a.gain = rot->gain;
   }
+  a.joined = a.rot == 0 || rot->pairing == CORM_NEIGHBOURS;
+}
+
+template <typename C, typename DT, int D>
+int launch_rows_d(RowsArgs& a, hipStream_t s) {
+  constexpr int RPW = 512 / D;   // rows of a wave
+  const long cus = device_cus();
+  const int heads = a.Hq + 2 * a.Hkv;
+  if (a.n >= RPW && (long)a.n * a.B >= 4 * cus) {
+    const long groups = (a.n + RPW - 1) / RPW;
+    a.head_waves = 1;
+    while (a.head_waves < 4 && groups * a.B * a.head_waves < 16 * cus) a.head_waves *= 2;
+    const dim3 grid((unsigned)((groups * a.head_waves + 3) / 4), a.B);
+    a.lens_here = a.lens_out && (grid.x == 1 || a.lens_out != a.lens);
+    if (a.joined) hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, true, true>), grid, dim3(256), 0, s, a);
+    else hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, true, false>), grid, dim3(256), 0, s, a);
+  } else {
+    a.head_waves = std::min(16, (heads + RPW - 1) / RPW);
+    a.lens_here = a.lens_out && (a.n == 1 || a.lens_out != a.lens);
+    const dim3 grid(a.n, a.B), wg(64 * a.head_waves);
+    if (a.joined) hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, false, true>), grid, wg, 0, s, a);
+    else hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, false, false>), grid, wg, 0, s, a);
+  }
+  const int rc = launch_status();
+  if (rc || !a.lens_out || a.lens_here) return rc;
+  hipLaunchKernelGGL(corm_rows_lens_kernel, dim3(a.B), dim3(WG), 0, s, a);
+  return launch_status();
 }
 
 template <typename C>
 int launch_rows(const corm_desc* d, RowsArgs& a, hipStream_t s) {
-  const long cus = device_cus();
-  a.tok_shift = 3;
-  while (a.tok_shift > 0 && (((long)a.n + (1 << a.tok_shift) - 1) >> a.tok_shift) * a.B < 2 * cus) --a.tok_shift;
-  const dim3 grid((a.n + (1 << a.tok_shift) - 1) >> a.tok_shift, a.B);
-  a.lens_here = a.lens_out && (grid.x == 1 || a.lens_out != a.lens);
-  const long lanes = ((long)(a.Hq + 2 * a.Hkv) << a.tok_shift) * (row_bytes(d) / 16);
-  const int threads = (int)std::min<long>(a.tok_shift == 3 ? WG : 1024, (lanes + 63) / 64 * 64);
-  auto go = [&](auto dt, auto dd) {
-    hipLaunchKernelGGL((corm_rows_kernel<C, decltype(dt), decltype(dd)::value, 4>), grid, dim3(threads), 0, s, a);
-    return launch_status();
-  };
-  using D64 = std::integral_constant<int, 64>;
-  using D128 = std::integral_constant<int, 128>;
-  const int rc = d->kv_dtype == CORM_F32 ? (d->d == 64 ? go(F32(), D64()) : go(F32(), D128())) : d->d == 64 ? go(BF16(), D64()) : go(BF16(), D128());
-  if (rc || !a.lens_out || a.lens_here) return rc;
-  hipLaunchKernelGGL(corm_rows_lens_kernel, dim3(a.B), dim3(WG), 0, s, a);
-  return launch_status();
+  if (d->kv_dtype == CORM_F32) return d->d == 64 ? launch_rows_d<C, F32, 64>(a, s) : launch_rows_d<C, F32, 128>(a, s);
+  return d->d == 64 ? launch_rows_d<C, BF16, 64>(a, s) : launch_rows_d<C, BF16, 128>(a, s);
 }
 
 // Parts of a unit, at most: enough for eight workgroups per compute unit of a large device, and not below 64 slots each.

@@ -18,8 +18,6 @@ struct PagedArgs {
   float scale_log2;
 };
 
-typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
-
 // 16, 8 or 4 bytes of a row, which are read once.
 template <int N>
 struct Slice;

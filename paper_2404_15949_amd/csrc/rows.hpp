@@ -5,6 +5,8 @@
 
 namespace {
 
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
+
 // Where the rows of a cache of pages lie.
 struct PageView {
   char* K;
@@ -46,13 +48,13 @@ struct RowsArgs {
   int32_t* lens_out;
   int32_t* status;
   int32_t B, n, Hq, Hkv, Lcap;   // Hq = 0: no queries
-  int32_t rot, neighbours, axes, in_turn, section[4];
+  int32_t rot, axes, in_turn, section[4];
+  int32_t joined;            // pairs of channels are neighbours, or nothing is turned
   float eps, gain;
-  int32_t tok_shift;         // log2 of the tokens of a workgroup
+  int32_t head_waves;        // waves of a workgroup that share the heads of their tokens
   int32_t lens_here;         // this launch writes the new lengths (not where they replace the old ones and a sequence has several workgroups)
 };
 
-constexpr int ROWS_TOKENS = 8;   // of a workgroup, at most
 constexpr double HALF_TURNS = 0.318309886183790671537767526745;   // 1 / pi
 
 // The axis that turns pair i of channels.
@@ -74,16 +76,85 @@ struct AsIs {
   static constexpr int ID = -1;
 };
 
+// Two fp32 as two bf16, rounded to nearest even (what is not a number stays none).
+__device__ __forceinline__ uint32_t two_bf16(float lo, float hi) {
+  const bf16x2_t x = {(__bf16)lo, (__bf16)hi};
+  return __builtin_bit_cast(uint32_t, x);
+}
+
+// Four channels of a row in the KV type: 16 or 8 bytes.
 template <typename DT>
-__device__ __forceinline__ uint4 round_row(const float* y) {
-  uint4 o;
-  uint32_t* w = &o.x;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if (DT::ESZ == 2) w[i] = (uint32_t)f32_to_bf16_rne(y[2 * i]) | (uint32_t)f32_to_bf16_rne(y[2 * i + 1]) << 16;
-    else w[i] = __float_as_uint(y[i]);
+struct Four {
+  uint32_t w[DT::ESZ];
+  __device__ __forceinline__ void load(const char* at) {
+    if constexpr (DT::ESZ == 4) {
+      const u32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(at));
+      w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
+    } else {
+      const u32x2_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(at));
+      w[0] = x.x; w[1] = x.y;
+    }
   }
-  return o;
+  __device__ __forceinline__ void store(char* at) const {
+    if constexpr (DT::ESZ == 4) __builtin_nontemporal_store(u32x4_t{w[0], w[1], w[2], w[3]}, reinterpret_cast<u32x4_t*>(at));
+    else __builtin_nontemporal_store(u32x2_t{w[0], w[1]}, reinterpret_cast<u32x2_t*>(at));
+  }
+  __device__ __forceinline__ void widen(float* y) const {
+    if constexpr (DT::ESZ == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) y[i] = __uint_as_float(w[i]);
+    } else {
+      y[0] = bf16_lo(w[0]); y[1] = bf16_hi(w[0]); y[2] = bf16_lo(w[1]); y[3] = bf16_hi(w[1]);
+    }
+  }
+  __device__ __forceinline__ void round(const float* y) {
+    if constexpr (DT::ESZ == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(y[i]);
+    } else {
+      w[0] = two_bf16(y[0], y[1]);
+      w[1] = two_bf16(y[2], y[3]);
+    }
+  }
+};
+
+// A lane's eight channels, c0 .. +4 and c1 .. +4.  JOINED: c1 = c0 + 4, one access where the type is small enough.
+template <typename DT, bool JOINED>
+__device__ __forceinline__ void load_eight(Four<DT> (&f)[2], const char* row, int c0, int c1) {
+  if constexpr (JOINED && DT::ESZ == 2) {
+    const u32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + c0 * 2));
+    f[0].w[0] = x.x; f[0].w[1] = x.y; f[1].w[0] = x.z; f[1].w[1] = x.w;
+  } else {
+    f[0].load(row + c0 * DT::ESZ);
+    f[1].load(row + c1 * DT::ESZ);
+  }
+}
+template <typename DT, bool JOINED>
+__device__ __forceinline__ void store_eight(char* row, int c0, int c1, const float* y) {
+  Four<DT> f[2];
+  f[0].round(y);
+  f[1].round(y + 4);
+  if constexpr (JOINED && DT::ESZ == 2) {
+    __builtin_nontemporal_store(u32x4_t{f[0].w[0], f[0].w[1], f[1].w[0], f[1].w[1]}, reinterpret_cast<u32x4_t*>(row + c0 * 2));
+  } else {
+    f[0].store(row + c0 * DT::ESZ);
+    f[1].store(row + c1 * DT::ESZ);
+  }
+}
+
+// Four numbers, in steps of the scale and not beyond the largest code, as codes.  int8: 1.5 * 2^23 has a last place of 1, so that the low byte of the
+// sum is the nearest (even) integer.
+template <typename C>
+__device__ __forceinline__ uint32_t four_codes(const float* y, float up) {
+#pragma clang fp contract(off)   // (the product is rounded before the sum is)
+  if constexpr (C::ID == CORM_I8) {
+    uint32_t u[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) u[e] = __float_as_uint(y[e] * up + 12582912.f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(u[3], u[2], 0x0c0c0400u), __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0400u), 0x05040100u);
+  } else {
+    return C::pack(y[0] * up, y[1] * up, y[2] * up, y[3] * up);
+  }
 }
 
 template <int LPR>
@@ -93,30 +164,29 @@ __device__ __forceinline__ uint32_t row_allreduce_max(uint32_t v) {
   v = max(v, other(v, std::integral_constant<int, 0x4E>()));     // quad_perm [2,3,0,1]
   v = max(v, other(v, std::integral_constant<int, 0x141>()));    // row_half_mirror
   if (LPR >= 16) v = max(v, other(v, std::integral_constant<int, 0x140>()));   // row_mirror
-  if (LPR >= 32) v = max(v, (uint32_t)__shfl_xor((int)v, 16));
   return v;
 }
 
-// The lanes of a row put it into a slot of a pool: in the KV type, or in codes with the row's scale.
-template <typename C, typename DT, int D>
-__device__ __forceinline__ void put_row(char* pool, float* scales, size_t row, int cl, const float* y) {
-  constexpr int EPL = DT::EPL, LPR = D / EPL;
+// The lanes of a row put it into row `row` of a pool, each its eight channels: in the KV type, or in codes with the row's scale.
+template <typename C, typename DT, int D, bool JOINED>
+__device__ __forceinline__ void put_row(char* pool, float* scales, size_t row, int cl, int c0, int c1, const float* y) {
   if constexpr (C::ID < 0) {
-    *reinterpret_cast<uint4*>(pool + row * (D * DT::ESZ) + (size_t)cl * 16) = round_row<DT>(y);
+    store_eight<DT, JOINED>(pool + row * (D * DT::ESZ), c0, c1, y);
   } else {
     uint32_t top = 0;   // as bits: what is not a number is above infinity, and that above all others
 #pragma unroll
-    for (int e = 0; e < EPL; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
-    const float amax = __uint_as_float(row_allreduce_max<LPR>(top));
+    for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(y[e]) & 0x7fffffffu);
+    const float amax = __uint_as_float(row_allreduce_max<D / 8>(top));
     const bool some = amax >= 0x1p-100f, none = __float_as_uint(amax) >= 0x7f800000u;
     const float up = some && !none ? __fdiv_rn(C::QMAX, amax) : 0.f;
-    uint32_t w[EPL / 4];
-#pragma unroll
-    for (int i = 0; i < EPL / 4; ++i)
-      w[i] = none ? 0u : C::pack(y[4 * i] * up, y[4 * i + 1] * up, y[4 * i + 2] * up, y[4 * i + 3] * up);
-    char* to = pool + row * D + (size_t)cl * EPL;
-    if constexpr (EPL == 8) *reinterpret_cast<uint2*>(to) = make_uint2(w[0], w[1]);
-    else *reinterpret_cast<uint32_t*>(to) = w[0];
+    const uint32_t w0 = none ? 0u : four_codes<C>(y, up), w1 = none ? 0u : four_codes<C>(y + 4, up);
+    char* to = pool + row * D;
+    if constexpr (JOINED) {
+      *reinterpret_cast<uint2*>(to + c0) = make_uint2(w0, w1);
+    } else {
+      *reinterpret_cast<uint32_t*>(to + c0) = w0;
+      *reinterpret_cast<uint32_t*>(to + c1) = w1;
+    }
     if (cl == 0) scales[row] = none ? __uint_as_float(0x7fc00000u) : some ? __fdiv_rn(amax, C::QMAX) : 0.f;
   }
 }
@@ -141,104 +211,122 @@ __device__ __forceinline__ void write_lens(const RowsArgs& a, int b, int take) {
 // values go as they are.  The angle is formed in 64 bits (an int32 times an fp32 is exact but for two bits) and brought to a turn there: at position
 // 10^6 32 bits would leave an error of 0.06.  Everything else is fp32, rounded once at the end.
 //
-// Few operations a byte: a token's 64 angles are shared by its heads, so the workgroup of a few tokens forms them first (LDS); then a row
-// is the work of D * ESZ / 16 lanes.  A lane reads its own 16 bytes and those of the pairs' other halves (the second time from the L1).
-template <typename C, typename DT, int D, int U>
-__global__ __launch_bounds__(1024) void corm_rows_kernel(const RowsArgs a) {
-  constexpr int EPL = DT::EPL, LPR = D / EPL;
-  __shared__ float2 turn[ROWS_TOKENS][D / 2];
-  const int b = blockIdx.y, t0 = (int)blockIdx.x << a.tok_shift;
-  const int take = rows_taken(a, b), half = a.rot / 2;
-  const int ntok = min(1 << a.tok_shift, take - t0);
-  if (ntok > 0) {
-    for (int i = threadIdx.x; i < ntok * half; i += blockDim.x) {
-      const int tok = i / half, pair = i - tok * half;
-      const int pos = a.positions[((size_t)axis_of(a, pair) * a.B + b) * a.n + t0 + tok];
+// A row is the work of D / 8 lanes; a lane has four channels and the four that are paired with them, so nothing but the sum of squares goes from lane to
+// lane.  A wave works for a group of tokens (TOKENS: as many as it has rows, so that what depends on the head is uniform; else for one token, a
+// head a row) and goes through their heads (its share of them): its angles are formed once, a pair a lane, and handed out through LDS.
+template <typename C, typename DT, int D, bool TOKENS, bool JOINED>
+__global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const RowsArgs a) {
+  constexpr int LPR = D / 8, RPW = 64 / LPR, TW = TOKENS ? RPW : 1, U = 4;   // lanes of a row, rows and tokens of a wave, heads in flight
+  __shared__ float2 turns[TOKENS ? 4 : 16][TW][D / 2 + 2];   // (a token's angles start on other banks than its neighbours')
+  const int b = blockIdx.y, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int share = wv % a.head_waves, group = wv / a.head_waves;
+  const int t0 = ((int)blockIdx.x * ((int)(blockDim.x >> 6) / a.head_waves) + group) * TW;
+  const int take = rows_taken(a, b);
+  if (t0 < take) {
+    const int lane = threadIdx.x & 63, sub = lane / LPR, cl = lane % LPR;
+    const int half = a.rot / 2, tok = t0 + (TOKENS ? sub : 0);
+    const bool in = tok < take;
+    // this lane's channels: JOINED eight that lie together (pairs of neighbours, or nothing is turned); else four of the first halves and their partners
+    const bool turned = JOINED ? 8 * cl < a.rot : 4 * cl < half;
+    const int c0 = JOINED ? 8 * cl : turned ? 4 * cl : a.rot + 8 * (cl - half / 4), c1 = !JOINED && turned ? c0 + half : c0 + 4;
+    const int heads = a.Hq + 2 * a.Hkv, step = TOKENS ? 1 : RPW;
+    const int each = ((heads + step - 1) / step + a.head_waves - 1) / a.head_waves * step;   // heads of a wave
+    const int end = min(heads, (share + 1) * each);
+    // a batch of U heads: their rows, and the lengths of the units that they go to
+    struct Batch {
+      Four<DT> x[U][2];
+      int L0[U];
+    };
+    auto kind_of = [&](int head) { return head < a.Hq ? 0 : head < a.Hq + a.Hkv ? 1 : 2; };
+    auto load = [&](Batch& t, int h0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int head = h0 + u * step + (TOKENS ? 0 : sub);
+        if (head >= end || !in) continue;
+        const int kind = kind_of(head), h = head - (kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + a.Hkv);
+        const char* base = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
+        const int64_t sq = kind == 0 ? a.qs.seq : kind == 1 ? a.ks.seq : a.vs.seq, st = kind == 0 ? a.qs.token : kind == 1 ? a.ks.token : a.vs.token,
+                      sh = kind == 0 ? a.qs.head : kind == 1 ? a.ks.head : a.vs.head;
+        load_eight<DT, JOINED>(t.x[u], base + b * sq + h * sh + tok * st, c0, c1);
+        if (!a.k_out && kind != 0) t.L0[u] = a.lens[(size_t)b * a.pages.TH + (a.pages.TH == 1 ? 0 : h)];
+      }
+    };
+    Batch now;
+    load(now, share * each);
+    // the angles, behind the loads of the first rows
+    for (int i = lane; i < TW * half; i += 64) {
+      const int t = TOKENS ? i / half : 0, pair = i - t * half;
+      const int pos = a.positions[((size_t)axis_of(a, pair) * a.B + b) * a.n + min(t0 + t, a.n - 1)];
       const double x = (double)pos * (double)a.inv_freq[pair] * HALF_TURNS;
       float s, c;
       sincospif((float)(x - 2.0 * rint(0.5 * x)), &s, &c);
-      turn[tok][pair] = make_float2(c * a.gain, s * a.gain);
+      turns[wv][t][pair] = make_float2(c * a.gain, s * a.gain);
     }
-    __syncthreads();
-    const int sub = threadIdx.x / LPR, cl = threadIdx.x % LPR, c0 = cl * EPL;
-    const int rows = blockDim.x / LPR, items = (a.Hq + 2 * a.Hkv) << a.tok_shift;
-    const int mask = (1 << a.tok_shift) - 1;
-    // (of the channels that are turned: does this lane hold the first or the second ones of its pairs, and where are the others)
-    const bool turned = c0 < a.rot, second = !a.neighbours && c0 >= half;
-    const int o0 = a.neighbours || !turned ? c0 : second ? c0 - half : c0 + half;
-    for (int i0 = sub; i0 < items; i0 += rows * U) {
-      uint4 own[U], other[U];
+    __builtin_amdgcn_wave_barrier();   // (LDS operations of a wave are done in order)
+    float2 turn[4];
+    if (turned) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * rows, tok = i & mask, head = i >> a.tok_shift;
-        if (i >= items || tok >= ntok) continue;
-        const bool isq = head < a.Hq, isk = !isq && head < a.Hq + a.Hkv;
-        const RowStrides& st = isq ? a.qs : isk ? a.ks : a.vs;
-        const int h = isq ? head : isk ? head - a.Hq : head - a.Hq - a.Hkv;
-        const char* row = (isq ? a.q : isk ? a.k : a.v) + b * st.seq + (t0 + tok) * st.token + h * st.head;
-        own[u] = *reinterpret_cast<const uint4*>(row + (size_t)c0 * DT::ESZ);
-        if ((isq || isk) && o0 != c0) other[u] = *reinterpret_cast<const uint4*>(row + (size_t)o0 * DT::ESZ);
+      for (int e = 0; e < 4; ++e) turn[e] = turns[wv][TOKENS ? sub : 0][4 * cl + e];
+    }
+    Four<DT> wq[2], wk[2];
+    if (a.q_norm) load_eight<DT, JOINED>(wq, a.q_norm, c0, c1);
+    if (a.k_norm) load_eight<DT, JOINED>(wk, a.k_norm, c0, c1);
+    for (int h0 = share * each; h0 < end; h0 += step * U) {
+      Batch next;
+      load(next, h0 + step * U);
+      int id[U];
+      if (!a.k_out) {   // the pages, behind the loads of the next rows
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int head = h0 + u * step + (TOKENS ? 0 : sub), kind = kind_of(head), h = head - (kind == 1 ? a.Hq : a.Hq + a.Hkv);
+          if (head >= end || !in || kind == 0 || !has_room(now.L0[u], take, a.Lcap)) continue;
+          id[u] = table_of(a.pages, b, h)[(now.L0[u] + tok) >> a.pages.shift];
+        }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const int i = i0 + u * rows, tok = i & mask, head = i >> a.tok_shift;
-        if (i >= items || tok >= ntok) continue;
-        const bool isq = head < a.Hq, isk = !isq && head < a.Hq + a.Hkv;
-        const int h = isq ? head : isk ? head - a.Hq : head - a.Hq - a.Hkv;
-        float y[EPL];
+        const int head = h0 + u * step + (TOKENS ? 0 : sub);
+        if (head >= end || !in) continue;
+        const int kind = kind_of(head), h = head - (kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + a.Hkv);
+        float y[8];
+        now.x[u][0].widen(y);
+        now.x[u][1].widen(y + 4);
+        if (kind != 2) {
+          if (kind == 0 ? a.q_norm : a.k_norm) {
+            float ss = 0.f, w[8];
 #pragma unroll
-        for (int e = 0; e < EPL; ++e) y[e] = element<DT>(own[u], e);
-        if (isq || isk) {
-          float z[EPL];
+            for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
+            const float r = rsqrtf(row_allreduce_sum<LPR>(ss) * (1.0f / D) + a.eps);
+            const Four<DT> f[2] = {kind == 0 ? wq[0] : wk[0], kind == 0 ? wq[1] : wk[1]};
+            f[0].widen(w);
+            f[1].widen(w + 4);
 #pragma unroll
-          for (int e = 0; e < EPL; ++e) z[e] = o0 != c0 ? element<DT>(other[u], e) : y[e];
-          const char* w = isq ? a.q_norm : a.k_norm;
-          if (w) {
-            float ss = 0.f;
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) ss = fmaf(y[e], y[e], ss);
-            const float r = 1.0f / sqrtf(row_allreduce_sum<LPR>(ss) * (1.0f / D) + a.eps);
-            const uint4 wy = *reinterpret_cast<const uint4*>(w + (size_t)c0 * DT::ESZ);
-            const uint4 wz = *reinterpret_cast<const uint4*>(w + (size_t)o0 * DT::ESZ);
-#pragma unroll
-            for (int e = 0; e < EPL; ++e) {
-              y[e] *= r * element<DT>(wy, e);
-              z[e] *= r * element<DT>(wz, e);
-            }
+            for (int e = 0; e < 8; ++e) y[e] *= r * w[e];
           }
           if (turned) {
-            if (a.neighbours) {
 #pragma unroll
-              for (int e = 0; e < EPL; e += 2) {
-                const float2 t = turn[tok][(c0 + e) / 2];
-                y[e] = z[e] * t.x - z[e + 1] * t.y;
-                y[e + 1] = z[e + 1] * t.x + z[e] * t.y;
-              }
-            } else {
-#pragma unroll
-              for (int e = 0; e < EPL; ++e) {
-                const float2 t = turn[tok][(second ? o0 : c0) + e];
-                y[e] = second ? y[e] * t.x + z[e] * t.y : y[e] * t.x - z[e] * t.y;
-              }
+            for (int e = 0; e < 4; ++e) {
+              float &first = y[JOINED ? 2 * e : e], &second = y[JOINED ? 2 * e + 1 : e + 4];
+              const float p = first, q = second;
+              first = p * turn[e].x - q * turn[e].y;
+              second = q * turn[e].x + p * turn[e].y;
             }
           }
         }
-        char* dense = isq ? a.q_out : isk ? a.k_out : a.v_out;
+        char* dense = kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out;
         if (dense) {
-          const size_t row = ((size_t)b * (isq ? a.Hq : a.Hkv) + h) * a.n + t0 + tok;
-          *reinterpret_cast<uint4*>(dense + row * (D * DT::ESZ) + (size_t)cl * 16) = round_row<DT>(y);
-        } else if (!isq) {
-          const int L0 = a.lens[(size_t)b * a.pages.TH + (a.pages.TH == 1 ? 0 : h)];
-          if (has_room(L0, take, a.Lcap)) {   // (the same for all lanes of the row)
-            const int slot = L0 + t0 + tok, id = table_of(a.pages, b, h)[slot >> a.pages.shift];
-            if (is_page(a.pages, id)) {
-              put_row<C, DT, D>(isk ? a.pages.K : a.pages.V, isk ? a.pages.ks : a.pages.vs, pool_row(a.pages, id, h, slot), cl, y);
-            } else if (cl == 0 && a.status) {
-              atomicOr(a.status, CORM_DEV_BAD_PAGE);
-            }
+          const size_t row = ((size_t)b * (kind == 0 ? a.Hq : a.Hkv) + h) * a.n + tok;
+          store_eight<DT, JOINED>(dense + row * (D * DT::ESZ), c0, c1, y);
+        } else if (kind != 0 && has_room(now.L0[u], take, a.Lcap)) {   // (the same for all lanes of the row)
+          if (is_page(a.pages, id[u])) {
+            put_row<C, DT, D, JOINED>(kind == 1 ? a.pages.K : a.pages.V, kind == 1 ? a.pages.ks : a.pages.vs,
+                                      pool_row(a.pages, id[u], h, now.L0[u] + tok), cl, c0, c1, y);
+          } else if (cl == 0 && a.status) {
+            atomicOr(a.status, CORM_DEV_BAD_PAGE);
           }
         }
       }
+      now = next;
     }
   }
   if (a.lens_here && blockIdx.x == 0) {
@@ -262,6 +350,7 @@ struct ReadArgs {
 
 constexpr int READ_ROWS = 4;   // of K and of V in flight per lane
 
+// One lane's 16 bytes of a row of a pool, in the KV type.
 template <typename C, typename DT, int D>
 __device__ __forceinline__ uint4 widen_row(const char* pool, const float* scales, size_t row, int cl) {
   constexpr int EPL = DT::EPL;
@@ -288,7 +377,10 @@ __device__ __forceinline__ uint4 widen_row(const char* pool, const float* scales
       y[4 * i + 2] = (float)hi[0] * scale;
       y[4 * i + 3] = (float)hi[1] * scale;
     }
-    return round_row<DT>(y);
+    uint4 o;
+    if constexpr (DT::ESZ == 4) o = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
+    else o = make_uint4(two_bf16(y[0], y[1]), two_bf16(y[2], y[3]), two_bf16(y[4], y[5]), two_bf16(y[6], y[7]));
+    return o;
   }
 }
 
