@@ -98,23 +98,15 @@ void bind_rows(const corm_desc* d, const corm_rows* r, const corm_rotation* rot,
 template <typename C, typename DT, int D>
 int launch_rows_d(RowsArgs& a, hipStream_t s) {
   constexpr int RPW = 512 / D;   // rows of a wave
-  const long cus = device_cus();
   const int heads = a.Hq + 2 * a.Hkv;
-  if (a.n >= RPW && (long)a.n * a.B >= 4 * cus) {
-    const long groups = (a.n + RPW - 1) / RPW;
-    a.head_waves = 1;
-    while (a.head_waves < 4 && groups * a.B * a.head_waves < 16 * cus) a.head_waves *= 2;
-    const dim3 grid((unsigned)((groups * a.head_waves + 3) / 4), a.B);
-    a.lens_here = a.lens_out && (grid.x == 1 || a.lens_out != a.lens);
-    if (a.joined) hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, true, true>), grid, dim3(256), 0, s, a);
-    else hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, true, false>), grid, dim3(256), 0, s, a);
-  } else {
-    a.head_waves = std::min(16, (heads + RPW - 1) / RPW);
-    a.lens_here = a.lens_out && (a.n == 1 || a.lens_out != a.lens);
-    const dim3 grid(a.n, a.B), wg(64 * a.head_waves);
-    if (a.joined) hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, false, true>), grid, wg, 0, s, a);
-    else hipLaunchKernelGGL((corm_rows_kernel<C, DT, D, false, false>), grid, wg, 0, s, a);
-  }
+  // Groups of tokens once they make two workgroups per compute unit, else a workgroup a token.  Us, a token | a group: bf16, d 128, 48 heads, 512, 1024,
+  // 2048, 4096 and 8192 tokens 6.5 | 12.2, 10.0 | 13.1, 16.9 | 15.9, 31.2 | 22.2 and 67 | 47; fp32, d 64, 10 heads, 2048 and 8192 4.9 | 5.8 and 10.4 | 9.7.
+  const bool tokens = a.n >= RPW && (long)a.n * a.B >= 2L * RPW * device_cus();
+  const dim3 grid((unsigned)(tokens ? (a.n + RPW - 1) / RPW : a.n), a.B), wg(64 * (tokens ? 4 : std::min(16, (heads + RPW - 1) / RPW)));
+  a.lens_here = a.lens_out && (grid.x == 1 || a.lens_out != a.lens);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, 0, s, a); };
+  if (tokens) a.joined ? launch(corm_rows_kernel<C, DT, D, true, true>) : launch(corm_rows_kernel<C, DT, D, true, false>);
+  else a.joined ? launch(corm_rows_kernel<C, DT, D, false, true>) : launch(corm_rows_kernel<C, DT, D, false, false>);
   const int rc = launch_status();
   if (rc || !a.lens_out || a.lens_here) return rc;
   hipLaunchKernelGGL(corm_rows_lens_kernel, dim3(a.B), dim3(WG), 0, s, a);
@@ -205,7 +197,7 @@ int corm_paged_read(const corm_desc* desc, const corm_pages* pages, const int32_
   a.pages = view_of(desc, pages);
   a.lens = lens; a.K_out = reinterpret_cast<char*>(K_out); a.V_out = reinterpret_cast<char*>(V_out); a.status = status;
   a.Hkv = desc->Hkv; a.Lcap = desc->Lcap; a.n = n;
-  const int rows = WG / (row_bytes(desc) / 16) * READ_ROWS;   // of a workgroup
+  const int rows = WG / (row_bytes(desc) / 16);   // of a workgroup
   const dim3 grid((std::min(n, desc->Lcap) + rows - 1) / rows, desc->B * desc->Hkv);
   return by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
     using P = decltype(pool);

@@ -51,7 +51,6 @@ struct RowsArgs {
   int32_t rot, axes, in_turn, section[4];
   int32_t joined;            // pairs of channels are neighbours, or nothing is turned
   float eps, gain;
-  int32_t head_waves;        // waves of a workgroup that share the heads of their tokens
   int32_t lens_here;         // this launch writes the new lengths (not where they replace the old ones and a sequence has several workgroups)
 };
 
@@ -88,10 +87,10 @@ struct Four {
   uint32_t w[DT::ESZ];
   __device__ __forceinline__ void load(const char* at) {
     if constexpr (DT::ESZ == 4) {
-      const u32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(at));
+      const u32x4_t x = *reinterpret_cast<const u32x4_t*>(at);
       w[0] = x.x; w[1] = x.y; w[2] = x.z; w[3] = x.w;
     } else {
-      const u32x2_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(at));
+      const u32x2_t x = *reinterpret_cast<const u32x2_t*>(at);
       w[0] = x.x; w[1] = x.y;
     }
   }
@@ -122,7 +121,7 @@ struct Four {
 template <typename DT, bool JOINED>
 __device__ __forceinline__ void load_eight(Four<DT> (&f)[2], const char* row, int c0, int c1) {
   if constexpr (JOINED && DT::ESZ == 2) {
-    const u32x4_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(row + c0 * 2));
+    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(row + c0 * 2);
     f[0].w[0] = x.x; f[0].w[1] = x.y; f[1].w[0] = x.z; f[1].w[1] = x.w;
   } else {
     f[0].load(row + c0 * DT::ESZ);
@@ -212,15 +211,14 @@ __device__ __forceinline__ void write_lens(const RowsArgs& a, int b, int take) {
 // 10^6 32 bits would leave an error of 0.06.  Everything else is fp32, rounded once at the end.
 //
 // A row is the work of D / 8 lanes; a lane has four channels and the four that are paired with them, so nothing but the sum of squares goes from lane to
-// lane.  A wave works for a group of tokens (TOKENS: as many as it has rows, so that what depends on the head is uniform; else for one token, a
-// head a row) and goes through their heads (its share of them): its angles are formed once, a pair a lane, and handed out through LDS.
+// lane.  A workgroup has a group of tokens (TOKENS: as many as a wave has rows, so that what depends on the head is uniform; else one token, a head a
+// row), its waves share their heads.  A wave's angles are formed once, a pair a lane, and handed out through LDS.
 template <typename C, typename DT, int D, bool TOKENS, bool JOINED>
 __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const RowsArgs a) {
-  constexpr int LPR = D / 8, RPW = 64 / LPR, TW = TOKENS ? RPW : 1, U = 4;   // lanes of a row, rows and tokens of a wave, heads in flight
+  constexpr int LPR = D / 8, RPW = 64 / LPR, TW = TOKENS ? RPW : 1, U = TOKENS ? 4 : 1;   // lanes of a row, rows and tokens of a wave, heads in flight
   __shared__ float2 turns[TOKENS ? 4 : 16][TW][D / 2 + 2];   // (a token's angles start on other banks than its neighbours')
   const int b = blockIdx.y, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int share = wv % a.head_waves, group = wv / a.head_waves;
-  const int t0 = ((int)blockIdx.x * ((int)(blockDim.x >> 6) / a.head_waves) + group) * TW;
+  const int shares = blockDim.x >> 6, t0 = (int)blockIdx.x * TW;
   const int take = rows_taken(a, b);
   if (t0 < take) {
     const int lane = threadIdx.x & 63, sub = lane / LPR, cl = lane % LPR;
@@ -230,8 +228,8 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
     const bool turned = JOINED ? 8 * cl < a.rot : 4 * cl < half;
     const int c0 = JOINED ? 8 * cl : turned ? 4 * cl : a.rot + 8 * (cl - half / 4), c1 = !JOINED && turned ? c0 + half : c0 + 4;
     const int heads = a.Hq + 2 * a.Hkv, step = TOKENS ? 1 : RPW;
-    const int each = ((heads + step - 1) / step + a.head_waves - 1) / a.head_waves * step;   // heads of a wave
-    const int end = min(heads, (share + 1) * each);
+    const int each = ((heads + step - 1) / step + shares - 1) / shares * step;   // heads of a wave
+    const int end = min(heads, (wv + 1) * each);
     // a batch of U heads: their rows, and the lengths of the units that they go to
     struct Batch {
       Four<DT> x[U][2];
@@ -252,7 +250,7 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
       }
     };
     Batch now;
-    load(now, share * each);
+    load(now, wv * each);
     // the angles, behind the loads of the first rows
     for (int i = lane; i < TW * half; i += 64) {
       const int t = TOKENS ? i / half : 0, pair = i - t * half;
@@ -271,7 +269,7 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
     Four<DT> wq[2], wk[2];
     if (a.q_norm) load_eight<DT, JOINED>(wq, a.q_norm, c0, c1);
     if (a.k_norm) load_eight<DT, JOINED>(wk, a.k_norm, c0, c1);
-    for (int h0 = share * each; h0 < end; h0 += step * U) {
+    for (int h0 = wv * each; h0 < end; h0 += step * U) {
       Batch next;
       load(next, h0 + step * U);
       int id[U];
@@ -348,23 +346,21 @@ struct ReadArgs {
   int32_t Hkv, Lcap, n;
 };
 
-constexpr int READ_ROWS = 4;   // of K and of V in flight per lane
-
 // One lane's 16 bytes of a row of a pool, in the KV type.
 template <typename C, typename DT, int D>
-__device__ __forceinline__ uint4 widen_row(const char* pool, const float* scales, size_t row, int cl) {
+__device__ __forceinline__ u32x4_t widen_row(const char* pool, const float* scales, size_t row, int cl) {
   constexpr int EPL = DT::EPL;
   if constexpr (C::ID < 0) {
-    return load_once(pool + row * (D * DT::ESZ) + (size_t)cl * 16);
+    return __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(pool + row * (D * DT::ESZ) + (size_t)cl * 16));
   } else {
     const char* at = pool + row * D + (size_t)cl * EPL;
     uint32_t w[2];
     if constexpr (EPL == 8) {
-      const uint2 x = *reinterpret_cast<const uint2*>(at);
+      const u32x2_t x = __builtin_nontemporal_load(reinterpret_cast<const u32x2_t*>(at));
       w[0] = x.x;
       w[1] = x.y;
     } else {
-      w[0] = *reinterpret_cast<const uint32_t*>(at);
+      w[0] = __builtin_nontemporal_load(reinterpret_cast<const uint32_t*>(at));
     }
     const float scale = scales[row];
     float y[EPL];
@@ -377,49 +373,34 @@ __device__ __forceinline__ uint4 widen_row(const char* pool, const float* scales
       y[4 * i + 2] = (float)hi[0] * scale;
       y[4 * i + 3] = (float)hi[1] * scale;
     }
-    uint4 o;
-    if constexpr (DT::ESZ == 4) o = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3]));
-    else o = make_uint4(two_bf16(y[0], y[1]), two_bf16(y[2], y[3]), two_bf16(y[4], y[5]), two_bf16(y[6], y[7]));
-    return o;
+    if constexpr (DT::ESZ == 4) return u32x4_t{__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]), __float_as_uint(y[3])};
+    else return u32x4_t{two_bf16(y[0], y[1]), two_bf16(y[2], y[3]), two_bf16(y[4], y[5]), two_bf16(y[6], y[7])};
   }
 }
 
-// Rows at and above the unit's length stay as they were, and those of slots without a page.
+// Rows at and above the unit's length stay as they were, and those of slots without a page.  A lane has 16 bytes of a key and of a value: bound by HBM, and
+// many short workgroups, which nothing holds up but one another, keep it busiest (rows of each per lane, 16 x 32 units of up to 4352 int8 slots, d 128: one
+// 230 us (5.8 TB/s), two 238, four 264; with loads and stores that caches are to keep 264).
 template <typename C, typename DT, int D>
 __global__ __launch_bounds__(WG) void corm_paged_read_kernel(const ReadArgs a) {
   constexpr int LPR = D / DT::EPL, ROWS = WG / LPR;
   const int unit = blockIdx.y, b = unit / a.Hkv, h = unit - b * a.Hkv;
-  const int sub = threadIdx.x / LPR, cl = threadIdx.x % LPR;
+  const int cl = threadIdx.x % LPR, slot = (int)blockIdx.x * ROWS + (int)threadIdx.x / LPR;
   int L = a.lens[(size_t)b * a.pages.TH + (a.pages.TH == 1 ? 0 : h)];
   if (L < 0 || L > a.Lcap) {
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.status) atomicOr(a.status, CORM_DEV_BAD_LENS);
     L = L < 0 ? 0 : a.Lcap;
   }
-  L = min(L, a.n);
-  const int32_t* table = table_of(a.pages, b, h);
-  const int s0 = (int)blockIdx.x * (ROWS * READ_ROWS) + sub;
-  int id[READ_ROWS];
-#pragma unroll
-  for (int u = 0; u < READ_ROWS; ++u) id[u] = s0 + u * ROWS < L ? table[(s0 + u * ROWS) >> a.pages.shift] : -1;
-  uint4 k[READ_ROWS], v[READ_ROWS];
-#pragma unroll
-  for (int u = 0; u < READ_ROWS; ++u) {
-    if (!is_page(a.pages, id[u])) continue;
-    const size_t row = pool_row(a.pages, id[u], h, s0 + u * ROWS);
-    k[u] = widen_row<C, DT, D>(a.pages.K, a.pages.ks, row, cl);
-    v[u] = widen_row<C, DT, D>(a.pages.V, a.pages.vs, row, cl);
+  if (slot >= min(L, a.n)) return;
+  const int id = table_of(a.pages, b, h)[slot >> a.pages.shift];
+  if (!is_page(a.pages, id)) {
+    if (cl == 0 && a.status) atomicOr(a.status, CORM_DEV_BAD_PAGE);
+    return;
   }
-#pragma unroll
-  for (int u = 0; u < READ_ROWS; ++u) {
-    const int slot = s0 + u * ROWS;
-    if (is_page(a.pages, id[u])) {
-      const size_t to = (((size_t)unit * a.n + slot) * D) * DT::ESZ + (size_t)cl * 16;
-      *reinterpret_cast<uint4*>(a.K_out + to) = k[u];
-      *reinterpret_cast<uint4*>(a.V_out + to) = v[u];
-    } else if (slot < L && cl == 0 && a.status) {
-      atomicOr(a.status, CORM_DEV_BAD_PAGE);
-    }
-  }
+  const size_t row = pool_row(a.pages, id, h, slot), to = (((size_t)unit * a.n + slot) * D) * DT::ESZ + (size_t)cl * 16;
+  const u32x4_t k = widen_row<C, DT, D>(a.pages.K, a.pages.ks, row, cl), v = widen_row<C, DT, D>(a.pages.V, a.pages.vs, row, cl);
+  __builtin_nontemporal_store(k, reinterpret_cast<u32x4_t*>(a.K_out + to));
+  __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(a.V_out + to));
 }
 
 }  // namespace

@@ -1,0 +1,254 @@
+// HIP kernels (gfx950 / CDNA4, wave64) and C ABI of a cache of pages and of the rows on their way into it.
+// One translation unit:
+//   codes.hpp   8-bit codes
+//   rows.hpp    norms of queries and keys, the position rotation, rows into pages and out of them
+//   paged.hpp   attention of one new token over pages
+// Kernel boundaries are the only synchronization between workgroups, and nothing is kept from one call for the next.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+#include <math.h>
+#include <algorithm>
+#include <cmath>
+#include <mutex>
+
+#include "corm.h"
+
+#include "common.hpp"
+#include "attend.hpp"
+#include "codes.hpp"
+#include "/root/repo/_work/rows_var.hpp"
+#include "paged.hpp"
+#include "checks.hpp"
+
+namespace {
+
+int elem_bytes(const corm_desc* d) { return d->kv_dtype == CORM_F32 ? 4 : 2; }
+bool in_codes(const corm_pages* p) { return p->dtype == CORM_I8 || p->dtype == CORM_E4M3; }
+
+int check_pages(const corm_desc* d, const corm_pages* p) {
+  if (!p || !p->K || !p->V || !p->table) return CORM_EINVAL;
+  if (!in_codes(p) && p->dtype != d->kv_dtype) return CORM_EUNSUPPORTED;
+  if (misaligned16(p->K) || misaligned16(p->V) || misaligned4(p->table)) return CORM_EINVAL;
+  if (in_codes(p) && (!p->k_scale || !p->v_scale || misaligned16(p->k_scale) || misaligned16(p->v_scale))) return CORM_EINVAL;
+  if (p->page != 16 && p->page != 32 && p->page != 64 && p->page != 128 && p->page != 256) return CORM_EUNSUPPORTED;
+  if (p->npages < 1 || p->max_pages < 1) return CORM_EINVAL;
+  if (p->table_heads != 1 && p->table_heads != d->Hkv) return CORM_EINVAL;
+  if ((long long)p->max_pages * p->page < d->Lcap) return CORM_EINVAL;
+  return CORM_OK;
+}
+
+PageView view_of(const corm_desc* d, const corm_pages* p) {
+  PageView v;
+  v.K = reinterpret_cast<char*>(p->K); v.V = reinterpret_cast<char*>(p->V); v.ks = p->k_scale; v.vs = p->v_scale;
+  v.table = p->table; v.npages = p->npages; v.max_pages = p->max_pages; v.TH = p->table_heads; v.HP = d->Hkv / p->table_heads;
+  v.shift = 4;
+  while ((1 << v.shift) < p->page) ++v.shift;
+  return v;
+}
+
+int check_rotation(const corm_desc* d, const corm_rotation* r, const int32_t* positions) {
+  if (!r) return CORM_OK;
+  if (r->rot < 0 || r->rot > d->d || r->rot % 16 != 0 || r->axes < 1 || r->axes > 4) return CORM_EINVAL;
+  if (r->pairing != CORM_HALVES && r->pairing != CORM_NEIGHBOURS) return CORM_EINVAL;
+  if (!(r->eps >= 0.f) || !std::isfinite(r->eps) || !std::isfinite(r->gain)) return CORM_EINVAL;
+  if (misaligned16(r->q_norm) || misaligned16(r->k_norm)) return CORM_EINVAL;
+  if (r->rot == 0) return CORM_OK;
+  if (!r->inv_freq || misaligned4(r->inv_freq) || !positions || misaligned4(positions)) return CORM_EINVAL;
+  long long sum = 0;
+  for (int x = 0; x < r->axes; ++x) {
+    if (r->section[x] < 0) return CORM_EINVAL;
+    sum += r->section[x];
+    // dealt in turn, the axis has pairs x, x + axes, ..: there have to be as many
+    if (r->in_turn && x > 0 && r->section[x] > 0 && x + ((long long)r->section[x] - 1) * r->axes >= r->rot / 2) return CORM_EINVAL;
+  }
+  return sum == r->rot / 2 ? CORM_OK : CORM_EINVAL;
+}
+
+int check_rows(const corm_desc* d, const corm_rows* r, bool with_q) {
+  if (!r || !r->k || !r->v || misaligned16(r->k) || misaligned16(r->v)) return CORM_EINVAL;
+  if (with_q && (!r->q || misaligned16(r->q))) return CORM_EINVAL;
+  const int per16 = 16 / elem_bytes(d);
+  for (int i = 0; i < 3; ++i) {
+    if (r->k_stride[i] < 0 || r->v_stride[i] < 0 || r->k_stride[i] % per16 || r->v_stride[i] % per16) return CORM_EINVAL;
+    if (with_q && (r->q_stride[i] < 0 || r->q_stride[i] % per16)) return CORM_EINVAL;
+  }
+  return CORM_OK;
+}
+
+RowStrides bytes_of(const int64_t* s, int esz) { return RowStrides{s[0] * esz, s[1] * esz, s[2] * esz}; }
+
+void bind_rows(const corm_desc* d, const corm_rows* r, const corm_rotation* rot, const int32_t* positions, int n, const int32_t* n_new,
+               RowsArgs& a) {
+  const int esz = elem_bytes(d);
+  a = RowsArgs();
+  a.q = reinterpret_cast<const char*>(r->q); a.k = reinterpret_cast<const char*>(r->k); a.v = reinterpret_cast<const char*>(r->v);
+  a.qs = bytes_of(r->q_stride, esz); a.ks = bytes_of(r->k_stride, esz); a.vs = bytes_of(r->v_stride, esz);
+  a.n_new = n_new; a.B = d->B; a.n = n; a.Hkv = d->Hkv; a.Lcap = d->Lcap;
+  a.axes = 1;
+  if (rot) {
+    a.inv_freq = rot->inv_freq; a.positions = positions;
+    a.q_norm = reinterpret_cast<const char*>(rot->q_norm); a.k_norm = reinterpret_cast<const char*>(rot->k_norm);
+    a.rot = rot->rot; a.axes = rot->axes; a.in_turn = rot->in_turn != 0;
+    for (int i = 0; i < 4; ++i) a.section[i] = i < rot->axes ? rot->section[i] : 0;
+    a.eps = rot->eps; a.gain = rot->gain;
+  }
+  a.joined = a.rot == 0 || rot->pairing == CORM_NEIGHBOURS;
+}
+
+template <typename C, typename DT, int D>
+int launch_rows_d(RowsArgs& a, hipStream_t s) {
+  constexpr int RPW = 512 / D;   // rows of a wave
+  const int heads = a.Hq + 2 * a.Hkv;
+  // Groups of tokens once they make two workgroups per compute unit, else a workgroup a token.  Us, a token | a group: bf16, d 128, 48 heads, 512, 1024,
+  // 2048, 4096 and 8192 tokens 6.5 | 12.2, 10.0 | 13.1, 16.9 | 15.9, 31.2 | 22.2 and 67 | 47; fp32, d 64, 10 heads, 2048 and 8192 4.9 | 5.8 and 10.4 | 9.7.
+  const bool tokens = a.n >= RPW && (long)a.n * a.B >= 2L * RPW * device_cus();
+  const dim3 grid((unsigned)(tokens ? (a.n + RPW - 1) / RPW : a.n), a.B), wg(64 * (tokens ? 4 : std::min(16, (heads + RPW - 1) / RPW)));
+  a.lens_here = a.lens_out && (grid.x == 1 || a.lens_out != a.lens);
+  auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, 0, s, a); };
+  if (tokens) a.joined ? launch(corm_rows_kernel<C, DT, D, true, true>) : launch(corm_rows_kernel<C, DT, D, true, false>);
+  else a.joined ? launch(corm_rows_kernel<C, DT, D, false, true>) : launch(corm_rows_kernel<C, DT, D, false, false>);
+  const int rc = launch_status();
+  if (rc || !a.lens_out || a.lens_here) return rc;
+  hipLaunchKernelGGL(corm_rows_lens_kernel, dim3(a.B), dim3(WG), 0, s, a);
+  return launch_status();
+}
+
+template <typename C>
+int launch_rows(const corm_desc* d, RowsArgs& a, hipStream_t s) {
+  if (d->kv_dtype == CORM_F32) return d->d == 64 ? launch_rows_d<C, F32, 64>(a, s) : launch_rows_d<C, F32, 128>(a, s);
+  return d->d == 64 ? launch_rows_d<C, BF16, 64>(a, s) : launch_rows_d<C, BF16, 128>(a, s);
+}
+
+// Parts of a unit, at most: enough for eight workgroups per compute unit of a large device, and not below 64 slots each.
+int most_parts(const corm_desc* d) {
+  const long units = (long)d->B * d->Hkv;
+  return (int)std::min<long>((d->Lcap + 63) / 64, std::max<long>(8, (2048 + units - 1) / units));
+}
+size_t paged_workspace(const corm_desc* d) { return align_up((size_t)d->B * d->Hq * most_parts(d) * (d->d + 2) * sizeof(float), 256); }
+
+// kernel<pool, query type, d> by the call's types
+template <typename F>
+int by_pool(const corm_desc* d, const corm_pages* p, const F& f) {
+  auto inner = [&](auto pool, auto dt) {
+    return d->d == 64 ? f(pool, dt, std::integral_constant<int, 64>()) : f(pool, dt, std::integral_constant<int, 128>());
+  };
+  const bool f32 = d->kv_dtype == CORM_F32;
+  if (p->dtype == CORM_I8) return f32 ? inner(PoolI8(), F32()) : inner(PoolI8(), BF16());
+  if (p->dtype == CORM_E4M3) return f32 ? inner(PoolE4M3(), F32()) : inner(PoolE4M3(), BF16());
+  return f32 ? inner(PoolF32(), F32()) : inner(PoolBF16(), BF16());
+}
+
+}  // namespace
+
+extern "C" {
+
+int corm_rotate(const corm_desc* desc, const corm_rows* rows, const corm_rotation* rotation, const int32_t* positions, int32_t n,
+                const int32_t* n_new, void* q_out, void* k_out, void* v_out, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!rotation || !k_out || !v_out || misaligned16(q_out) || misaligned16(k_out) || misaligned16(v_out)) return CORM_EINVAL;
+  if (n < 1 || misaligned4(n_new)) return CORM_EINVAL;
+  rc = check_rows(desc, rows, q_out != nullptr);
+  if (rc) return rc;
+  rc = check_rotation(desc, rotation, positions);
+  if (rc) return rc;
+  RowsArgs a;
+  bind_rows(desc, rows, rotation, positions, n, n_new, a);
+  a.Hq = q_out ? desc->Hq : 0;
+  a.q_out = reinterpret_cast<char*>(q_out); a.k_out = reinterpret_cast<char*>(k_out); a.v_out = reinterpret_cast<char*>(v_out);
+  return launch_rows<AsIs>(desc, a, (hipStream_t)stream);
+}
+
+int corm_paged_append(const corm_desc* desc, const corm_pages* pages, const corm_rows* rows, const corm_rotation* rotation,
+                      const int32_t* positions, int32_t n, const int32_t* n_new, void* q_out, const int32_t* lens, int32_t* lens_out,
+                      int32_t* status, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  rc = check_pages(desc, pages);
+  if (rc) return rc;
+  if (!lens || !lens_out || misaligned4(lens) || misaligned4(lens_out) || misaligned4(status) || misaligned4(n_new) || misaligned16(q_out))
+    return CORM_EINVAL;
+  if (n < 1 || n > desc->Lcap) return CORM_EINVAL;
+  rc = check_rows(desc, rows, q_out != nullptr);
+  if (rc) return rc;
+  rc = check_rotation(desc, rotation, positions);
+  if (rc) return rc;
+  RowsArgs a;
+  bind_rows(desc, rows, rotation, positions, n, n_new, a);
+  a.Hq = q_out ? desc->Hq : 0;
+  a.q_out = reinterpret_cast<char*>(q_out);
+  a.pages = view_of(desc, pages);
+  a.lens = lens; a.lens_out = lens_out; a.status = status;
+  hipStream_t s = (hipStream_t)stream;
+  if (pages->dtype == CORM_I8) return launch_rows<CodeI8>(desc, a, s);
+  if (pages->dtype == CORM_E4M3) return launch_rows<CodeE4M3>(desc, a, s);
+  return launch_rows<AsIs>(desc, a, s);
+}
+
+int corm_paged_read(const corm_desc* desc, const corm_pages* pages, const int32_t* lens, int32_t n, void* K_out, void* V_out,
+                    int32_t* status, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  rc = check_pages(desc, pages);
+  if (rc) return rc;
+  if (!lens || !K_out || !V_out || misaligned4(lens) || misaligned16(K_out) || misaligned16(V_out) || misaligned4(status) || n < 1)
+    return CORM_EINVAL;
+  ReadArgs a;
+  a.pages = view_of(desc, pages);
+  a.lens = lens; a.K_out = reinterpret_cast<char*>(K_out); a.V_out = reinterpret_cast<char*>(V_out); a.status = status;
+  a.Hkv = desc->Hkv; a.Lcap = desc->Lcap; a.n = n;
+  const int rows = WG / (row_bytes(desc) / 16);   // of a workgroup
+  const dim3 grid((std::min(n, desc->Lcap) + rows - 1) / rows, desc->B * desc->Hkv);
+  return by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
+    using P = decltype(pool);
+    using C = std::conditional_t<std::is_same_v<P, PoolI8>, CodeI8, std::conditional_t<std::is_same_v<P, PoolE4M3>, CodeE4M3, AsIs>>;
+    hipLaunchKernelGGL((corm_paged_read_kernel<C, decltype(dt), decltype(dd)::value>), grid, dim3(WG), 0, (hipStream_t)stream, a);
+    return launch_status();
+  });
+}
+
+int corm_paged_workspace_bytes(const corm_desc* desc, size_t* bytes) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  if (!bytes) return CORM_EINVAL;
+  *bytes = paged_workspace(desc);
+  return CORM_OK;
+}
+
+int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void* q, const int32_t* lens, float* out, void* workspace,
+                      size_t workspace_bytes, int32_t* status, void* stream) {
+  int rc = validate_desc(desc);
+  if (rc) return rc;
+  rc = check_pages(desc, pages);
+  if (rc) return rc;
+  if (!q || !lens || !out || misaligned16(q) || misaligned4(lens) || misaligned4(out) || misaligned4(status)) return CORM_EINVAL;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CORM_EINVAL;
+  if (workspace_bytes < paged_workspace(desc)) return CORM_ECAPACITY;
+  PagedArgs a;
+  a.pages = view_of(desc, pages);
+  a.q = q; a.lens = lens; a.out = out; a.partials = reinterpret_cast<float*>(workspace); a.status = status;
+  a.Hkv = desc->Hkv; a.G = desc->Hq / desc->Hkv; a.Lcap = desc->Lcap;
+  a.scale_log2 = (desc->sm_scale > 0.f ? desc->sm_scale : 1.0f / sqrtf((float)desc->d)) * LOG2E;
+  const long units = (long)desc->B * desc->Hkv, cus = device_cus();
+  a.units = (int)units;
+  const int tile = in_codes(pages) ? PoolI8::TILE : desc->kv_dtype == CORM_F32 ? PoolF32::TILE : PoolBF16::TILE;
+  const int tiles = (desc->Lcap + tile - 1) / tile;
+  // Parts of whole rounds of tiles over the waves.
+  const long want = std::min<long>(most_parts(desc), units >= 2 * cus ? 1 : (4 * cus + units - 1) / units);
+  a.part_tiles = (int)((((long)tiles + want - 1) / want + WAVES - 1) / WAVES * WAVES);
+  a.npart = (tiles + a.part_tiles - 1) / a.part_tiles;
+  const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
+  if (groups * WG > 4294967295L) return CORM_EUNSUPPORTED;   // (threads of a launch)
+  hipStream_t s = (hipStream_t)stream;
+  rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
+    hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, 2>), dim3((unsigned)groups), dim3(WG), 0, s, a);
+    return launch_status();
+  });
+  if (rc || a.npart == 1) return rc;
+  const dim3 heads((unsigned)(desc->B * desc->Hq));
+  if (desc->d == 64) hipLaunchKernelGGL(corm_paged_merge_kernel<64>, heads, dim3(PAGED_MERGE_WG), 0, s, a, tile);
+  else hipLaunchKernelGGL(corm_paged_merge_kernel<128>, heads, dim3(PAGED_MERGE_WG), 0, s, a, tile);
+  return launch_status();
+}
+
+}  // extern "C"
