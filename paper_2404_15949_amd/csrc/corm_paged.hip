@@ -119,12 +119,17 @@ int launch_rows(const corm_desc* d, RowsArgs& a, hipStream_t s) {
   return d->d == 64 ? launch_rows_d<C, BF16, 64>(a, s) : launch_rows_d<C, BF16, 128>(a, s);
 }
 
-// Parts of a unit, at most: enough for eight workgroups per compute unit of a large device, and not below 64 slots each.
-int most_parts(const corm_desc* d) {
-  const long units = (long)d->B * d->Hkv;
-  return (int)std::min<long>((d->Lcap + 63) / 64, std::max<long>(8, (2048 + units - 1) / units));
+// Workgroups that share all units' tiles, at most, or of few short units, twice as many; a shared one has two partials.
+constexpr int PAGED_MOST = 1024;
+struct PagedWorkspace {
+  size_t parts_off, total;
+};
+PagedWorkspace paged_workspace(const corm_desc* d) {
+  PagedWorkspace w;
+  w.parts_off = align_up((size_t)PAGED_MOST * 2 * (d->Hq / d->Hkv) * (d->d + 2) * sizeof(float), 256);
+  w.total = align_up(w.parts_off + (size_t)d->B * d->Hkv * sizeof(int2), 256);
+  return w;
 }
-size_t paged_workspace(const corm_desc* d) { return align_up((size_t)d->B * d->Hq * most_parts(d) * (d->d + 2) * sizeof(float), 256); }
 
 // kernel<pool, query type, d> by the call's types
 template <typename F>
@@ -211,7 +216,7 @@ int corm_paged_workspace_bytes(const corm_desc* desc, size_t* bytes) {
   int rc = validate_desc(desc);
   if (rc) return rc;
   if (!bytes) return CORM_EINVAL;
-  *bytes = paged_workspace(desc);
+  *bytes = paged_workspace(desc).total;
   return CORM_OK;
 }
 
@@ -223,31 +228,41 @@ int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void
   if (rc) return rc;
   if (!q || !lens || !out || misaligned16(q) || misaligned4(lens) || misaligned4(out) || misaligned4(status)) return CORM_EINVAL;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u)) return CORM_EINVAL;
-  if (workspace_bytes < paged_workspace(desc)) return CORM_ECAPACITY;
+  const PagedWorkspace w = paged_workspace(desc);
+  if (workspace_bytes < w.total) return CORM_ECAPACITY;
   PagedArgs a;
   a.pages = view_of(desc, pages);
-  a.q = q; a.lens = lens; a.out = out; a.partials = reinterpret_cast<float*>(workspace); a.status = status;
+  a.q = q; a.lens = lens; a.out = out; a.partials = reinterpret_cast<float*>(workspace);
+  a.parts = reinterpret_cast<int2*>(reinterpret_cast<char*>(workspace) + w.parts_off); a.status = status;
   a.Hkv = desc->Hkv; a.G = desc->Hq / desc->Hkv; a.Lcap = desc->Lcap;
   a.scale_log2 = (desc->sm_scale > 0.f ? desc->sm_scale : 1.0f / sqrtf((float)desc->d)) * LOG2E;
-  const long units = (long)desc->B * desc->Hkv, cus = device_cus();
-  a.units = (int)units;
+  a.units = desc->B * desc->Hkv;
   const int tile = in_codes(pages) ? PoolI8::TILE : desc->kv_dtype == CORM_F32 ? PoolF32::TILE : PoolBF16::TILE;
-  const int tiles = (desc->Lcap + tile - 1) / tile;
-  // Parts of whole rounds of tiles over the waves.
-  const long want = std::min<long>(most_parts(desc), units >= 2 * cus ? 1 : (4 * cus + units - 1) / units);
-  a.part_tiles = (int)((((long)tiles + want - 1) / want + WAVES - 1) / WAVES * WAVES);
-  a.npart = (tiles + a.part_tiles - 1) / a.part_tiles;
-  const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
-  if (groups * WG > 4294967295L) return CORM_EUNSUPPORTED;   // (threads of a launch)
+  const long units = a.units, cus = device_cus(), rounds = ((desc->Lcap + tile - 1) / tile + WAVES - 1) / WAVES;   // of a unit, at most
+  a.tables = desc->B * pages->table_heads;
+  a.workgroups = (int)std::min<long>(PAGED_MOST, 2 * cus);
+  const bool shared = units < 2 * cus && a.tables <= SHARE_TABLES && units * rounds > a.workgroups && units * rounds * WAVES < 2147483647L;
+  a.npart = units >= 2 * cus ? 1 : (int)std::min<long>({rounds, (a.workgroups + units - 1) / units, 2 * PAGED_MOST / units});
   hipStream_t s = (hipStream_t)stream;
+  const dim3 heads((unsigned)(desc->B * desc->Hq)), merge_wg(PAGED_MERGE_WG);
+  if (shared) {
+    rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
+      hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, true>), dim3(a.workgroups), dim3(WG), 0, s, a);
+      return launch_status();
+    });
+    if (rc) return rc;
+    if (desc->d == 64) hipLaunchKernelGGL((corm_paged_merge_kernel<64, true>), heads, merge_wg, 0, s, a, tile);
+    else hipLaunchKernelGGL((corm_paged_merge_kernel<128, true>), heads, merge_wg, 0, s, a, tile);
+    return launch_status();
+  }
+  const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
   rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
-    hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, 2>), dim3((unsigned)groups), dim3(WG), 0, s, a);
+    hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, false>), dim3((unsigned)groups), dim3(WG), 0, s, a);
     return launch_status();
   });
   if (rc || a.npart == 1) return rc;
-  const dim3 heads((unsigned)(desc->B * desc->Hq));
-  if (desc->d == 64) hipLaunchKernelGGL(corm_paged_merge_kernel<64>, heads, dim3(PAGED_MERGE_WG), 0, s, a, tile);
-  else hipLaunchKernelGGL(corm_paged_merge_kernel<128>, heads, dim3(PAGED_MERGE_WG), 0, s, a, tile);
+  if (desc->d == 64) hipLaunchKernelGGL((corm_paged_merge_kernel<64, false>), heads, merge_wg, 0, s, a, tile);
+  else hipLaunchKernelGGL((corm_paged_merge_kernel<128, false>), heads, merge_wg, 0, s, a, tile);
   return launch_status();
 }
 

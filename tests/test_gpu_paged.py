@@ -440,6 +440,46 @@ def test_attend_many_units_and_long_ones(dtype, code):
         assert torch.equal(c.out, again) and int(c.status) == 0
 
 
+@pytest.mark.parametrize("per_head", [False, True])
+@pytest.mark.parametrize("dtype,code", [("bf16", None), ("f32", None), ("bf16", "e4m3")])
+def test_attend_units_of_every_length(dtype, code, per_head):
+    """Hundreds of units, and few long ones, of any lengths: none, one slot, fewer tiles than waves and workgroups, more."""
+    g = _gen(21)
+    for B, Hkv, most in ((130, 2, 200), (3, 2, 20000), (1, 1, 40), (400, 2, 33)):
+        c = Cache(g, B, 2 * Hkv, Hkv, 64, most, dtype, code, 16, per_head, spare=1)
+        n = Hkv if per_head else 1
+        lens = torch.randint(0, most + 1, (B, n), generator=g)
+        lens = torch.where(torch.rand(B, n, generator=g) < 0.25, torch.randint(0, 2, (B, n), generator=g) * most, lens)
+        c.fill(g, lens.tolist(), (2.0, 2.0))
+        q = _normal(g, dtype, B, 2 * Hkv, 64, scale=3.0)
+        c.attend(q)
+        c.check_out(q)
+
+
+def test_attend_thousands_of_units():
+    g = _gen(22)
+    B, d = 4100, 64
+    lens = torch.randint(0, 65, (B, 1), generator=g, dtype=torch.int32)
+    K, V = _normal(g, "bf16", B, 1, 64, d).to(DEV), _normal(g, "bf16", B, 1, 64, d).to(DEV)
+    q = _normal(g, "bf16", B, 2, d, scale=2.0)
+    desc = corm.make_desc(B, 2, 1, d, 64, 64, 1, 1, "bf16")
+    table = torch.randperm(B * 4, generator=g).to(torch.int32).view(B, 1, 4)
+    at = table.view(B, 4).long().to(DEV)
+    pool = [torch.zeros(B * 4, 1, 16, d, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    for p, x in zip(pool, (K, V)):
+        p[at.view(-1), 0] = x.view(B * 4, 16, d)
+    out, ws = _nan(B, 2, d), torch.empty(corm.corm_paged_workspace_bytes(desc), dtype=torch.uint8, device=DEV)
+    corm.corm_paged_attend(desc, corm.Pages(desc, *pool, table.to(DEV)), q.to(DEV), lens.to(DEV), out, ws)
+    got = out.cpu().double()
+    for b in range(0, B, 17):
+        k, v, x = K[b, 0, :lens[b]].cpu().double(), V[b, 0, :lens[b]].cpu().double(), q[b].double()
+        assert float((got[b] - ref.attend(x, k, v, ref.sm_of(d))).abs().max()) <= ref.attend_error(x, k, v, ref.sm_of(d)), b
+    live = (torch.arange(64, device=DEV) < lens.to(DEV)).unsqueeze(1)
+    s = torch.matmul(q.to(DEV).float(), K[:, 0].float().transpose(1, 2).contiguous()) * ref.sm_of(d)
+    p = torch.softmax(s.masked_fill(~live, float("-inf")), -1).nan_to_num()
+    assert float((torch.matmul(p, V[:, 0].float()) - out).abs().max()) < 1e-4
+
+
 def test_attend_lengths_that_are_none_and_scale():
     g = _gen(18)
     c = Cache(g, 3, 4, 2, 128, 200, "bf16", None, 16, False)

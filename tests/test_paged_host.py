@@ -127,13 +127,13 @@ def test_rotations(name):
 
 
 def test_workspace():
-    d = _desc()
-    assert corm.corm_paged_workspace_bytes(d) == (2 * 8 * 16 * 130 * 4 + 255) // 256 * 256        # 16 parts of 64 slots
-    for kw in (dict(Lcap=1), dict(Lcap=131072), dict(Hq=1, Hkv=1, B=1, Lcap=4194303), dict(B=64, Hq=64, Hkv=64)):
-        n = corm.corm_paged_workspace_bytes(_desc(**kw))
-        assert n % 256 == 0 and 0 < n < 1 << 30
+    """Two partials of each of 1024 workgroups, and eight bytes a unit: no more for longer caches."""
+    for kw in (dict(), dict(Lcap=1), dict(Lcap=131072), dict(Hq=1, Hkv=1, B=1, Lcap=4194303), dict(B=64, Hq=64, Hkv=64), dict(B=8191, Hq=64, Hkv=8)):
+        d = _desc(**kw)
+        partials = 1024 * 2 * (d.Hq // d.Hkv) * 130 * 4
+        assert partials % 256 == 0 and corm.corm_paged_workspace_bytes(d) == (partials + d.B * d.Hkv * 8 + 255) // 256 * 256
     assert corm.corm_paged_workspace_bytes(_desc(d=96), check=False) == corm.CORM_EUNSUPPORTED
-    assert corm.lib().corm_paged_workspace_bytes(ctypes.byref(d), None) == corm.CORM_EINVAL
+    assert corm.lib().corm_paged_workspace_bytes(ctypes.byref(_desc()), None) == corm.CORM_EINVAL
 
 
 def test_structures_have_the_headers_layout():
