@@ -241,29 +241,38 @@ int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void
   const long units = a.units, cus = device_cus(), rounds = ((desc->Lcap + tile - 1) / tile + WAVES - 1) / WAVES;   // of a unit, at most
   a.tables = desc->B * pages->table_heads;
   a.workgroups = (int)std::min<long>(PAGED_MOST, 2 * cus);
-  const bool shared = units < 2 * cus && a.tables <= SHARE_TABLES && units * rounds > a.workgroups && units * rounds * WAVES < 2147483647L;
-  a.npart = units >= 2 * cus ? 1 : (int)std::min<long>({rounds, (a.workgroups + units - 1) / units, 2 * PAGED_MOST / units});
+  // A workgroup takes a whole unit where there are two units per compute unit, or one and they are short, or where they are very short; units whose rounds
+  // all fit the chip at once get a workgroup for each; else all units' tiles are shared out.  Us, bf16, d 128, four heads a unit, rounds of 128 slots:
+  //   whole | shared           256 units x 760, 1500 and 4096 slots 20.0 | 25.3, 34.8 | 42.4 and 84.7 | 90.9; 384 x 760 and 4096 32.2 | 37.1 and 149 | 132;
+  //                            320 x 0 .. 1500 and 1000 .. 6000 44.8 | 50.3 and 157 | 100; 512 x 548 .. 2048 67 | 71
+  //   whole | one each, merged 8 x 250, 380 and 510 6.9 | 8.4, 7.9 | 8.2 and 9.4 | 8.4; 128 x 380 10.9 | 13.3
+  //   shared | units in equal parts, whatever their lengths   128 x 4192 .. 8192 73 | 77, x 0 .. 16384 102 | 120, x 4096 51 | 50; 8 x 131072 int8 55 | 53
+  const bool alone = units >= 2 * cus || (units >= cus && rounds <= 16) || rounds <= 3;
+  const bool shared = !alone && units * rounds > a.workgroups && a.tables <= SHARE_TABLES && units * rounds * WAVES < 2147483647L;
+  a.npart = alone ? 1 : (int)std::min<long>({rounds, (a.workgroups + units - 1) / units, 2 * PAGED_MOST / units});
   hipStream_t s = (hipStream_t)stream;
-  const dim3 heads((unsigned)(desc->B * desc->Hq)), merge_wg(PAGED_MERGE_WG);
+  // (a merge of few partials by 256 threads, of many by 1024)
+  auto merge = [&](auto shared_, int parts) {
+    constexpr bool SHARED = decltype(shared_)::value;
+    const bool many = parts > 32;
+    auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)(desc->B * desc->Hq)), dim3(many ? 1024 : 256), 0, s, a, tile); };
+    if (desc->d == 64) many ? launch(corm_paged_merge_kernel<64, SHARED, 1024>) : launch(corm_paged_merge_kernel<64, SHARED, 256>);
+    else many ? launch(corm_paged_merge_kernel<128, SHARED, 1024>) : launch(corm_paged_merge_kernel<128, SHARED, 256>);
+    return launch_status();
+  };
   if (shared) {
     rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
       hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, true>), dim3(a.workgroups), dim3(WG), 0, s, a);
       return launch_status();
     });
-    if (rc) return rc;
-    if (desc->d == 64) hipLaunchKernelGGL((corm_paged_merge_kernel<64, true>), heads, merge_wg, 0, s, a, tile);
-    else hipLaunchKernelGGL((corm_paged_merge_kernel<128, true>), heads, merge_wg, 0, s, a, tile);
-    return launch_status();
+    return rc ? rc : merge(std::true_type(), (int)(a.workgroups / units) + 2);
   }
   const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
   rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
     hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, false>), dim3((unsigned)groups), dim3(WG), 0, s, a);
     return launch_status();
   });
-  if (rc || a.npart == 1) return rc;
-  if (desc->d == 64) hipLaunchKernelGGL((corm_paged_merge_kernel<64, false>), heads, merge_wg, 0, s, a, tile);
-  else hipLaunchKernelGGL((corm_paged_merge_kernel<128, false>), heads, merge_wg, 0, s, a, tile);
-  return launch_status();
+  return rc || a.npart == 1 ? rc : merge(std::false_type(), a.npart);
 }
 
 }  // extern "C"

@@ -491,10 +491,10 @@ __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArg
 
 // out of a head from the partials of its unit.  A few kilobytes a head, so its time is that of its latencies: a thread has a channel and every GROUPS'th
 // partial, a batch of them under way at once (not shared: before it is known how many the unit has; the others are memory of the workspace, not used).
-constexpr int PAGED_MERGE_WG = 1024, PAGED_MERGE_BATCH = 8;
-template <int D, bool SHARED>
-__global__ __launch_bounds__(PAGED_MERGE_WG) void corm_paged_merge_kernel(const PagedArgs a, int tile) {
-  constexpr int GROUPS = PAGED_MERGE_WG / D;
+constexpr int PAGED_MERGE_BATCH = 8;
+template <int D, bool SHARED, int MERGE_WG>
+__global__ __launch_bounds__(MERGE_WG) void corm_paged_merge_kernel(const PagedArgs a, int tile) {
+  constexpr int GROUPS = MERGE_WG / D;
   __shared__ float sh_m[GROUPS], sh_z[GROUPS], sh_v[GROUPS][D];
   const int head = blockIdx.x, unit = head / a.G, grp = threadIdx.x / D, c = threadIdx.x % D;
   int2 where = make_int2(0, 0);

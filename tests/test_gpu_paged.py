@@ -456,6 +456,45 @@ def test_attend_units_of_every_length(dtype, code, per_head):
         c.check_out(q)
 
 
+@pytest.mark.parametrize("B,Hkv,most,per_head", [(60, 2, 1100, True), (100, 1, 900, False), (170, 3, 2100, True), (255, 2, 2070, False), (2, 1, 70000, False),
+                                                 (512, 1, 2100, False)])
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("f32", 64)])
+def test_attend_shares_of_all_units(dtype, d, B, Hkv, most, per_head):
+    """Units whose tiles are shared out: of every length, runs that begin and end inside them, empty ones between, long ones over many runs."""
+    g = _gen(23)
+    TH, G, page = (Hkv if per_head else 1), 2, 64
+    maxp = (most + page - 1) // page
+    lens = torch.randint(0, most + 1, (B, TH), generator=g, dtype=torch.int32)
+    lens[torch.rand(B, TH, generator=g) < 0.2] = 0
+    lens[torch.rand(B, TH, generator=g) < 0.1] = most
+    lens[-1] = most if B < 100 else 0                       # (the last run ends with the last unit, or with empty ones)
+    npages = B * TH * maxp // 2 + 1                         # pages are shared by tables: they are only read
+    table = torch.randint(0, npages, (B, TH, maxp), generator=g, dtype=torch.int32)
+    shape = (npages,) + (() if per_head else (Hkv,)) + (page, d)
+    gd = torch.Generator(device=DEV).manual_seed(23)
+    K, V = ((torch.randn(shape, generator=gd, device=DEV) * 2).to(DT[dtype]) for _ in range(2))
+    q = _normal(g, dtype, B, Hkv * G, d, scale=2.0).to(DEV)
+    desc = corm.make_desc(B, Hkv * G, Hkv, d, most, most, 1, 1, dtype)
+    out, ws = _nan(B, Hkv * G, d), torch.full((corm.corm_paged_workspace_bytes(desc),), 0xA5, dtype=torch.uint8, device=DEV)
+    status = torch.zeros(1, dtype=torch.int32, device=DEV)
+    td, ld = table.to(DEV), lens.to(DEV)
+    corm.corm_paged_attend(desc, corm.Pages(desc, K, V, td), q, ld, out, ws, status=status)
+    assert int(status) == 0 and not bool(out.isnan().any())
+    for b in range(B):
+        for h in range(Hkv):
+            n = int(lens[b, h if per_head else 0])
+            x, got = q[b, h * G:(h + 1) * G].double(), out[b, h * G:(h + 1) * G].double()
+            if not n:
+                assert not got.any()
+                continue
+            ids = td[b, h if per_head else 0, :(n + page - 1) // page].long()
+            k, v = ((p if per_head else p[:, h])[ids].reshape(-1, d)[:n].double() for p in (K, V))
+            s = torch.mm(x, k.t()) * ref.sm_of(d)
+            want = torch.mm(torch.softmax(s, -1), v)
+            bound = ref.attend_error(x, k, v, ref.sm_of(d))
+            assert float((got - want).abs().max()) <= bound, (b, h, n)
+
+
 def test_attend_thousands_of_units():
     g = _gen(22)
     B, d = 4100, 64
