@@ -46,8 +46,8 @@ class corm_launch_opts(ctypes.Structure):
 
 
 class corm_rows(ctypes.Structure):
-    _fields_ = [("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("q_stride", ctypes.c_int64 * 3),
-                ("k_stride", ctypes.c_int64 * 3), ("v_stride", ctypes.c_int64 * 3)]
+    # (the header's arrays of three strides one by one: arrays take longer to fill than a launch does to be queued)
+    _fields_ = [(x, ctypes.c_void_p) for x in "qkv"] + [(f"{x}_{of}", ctypes.c_int64) for x in "qkv" for of in ("seq", "token", "head")]
 
 
 class corm_rotation(ctypes.Structure):
@@ -578,15 +578,15 @@ def _strided(x, shape, kv, name, device):
         raise ValueError(f"{name}: expected {shape} of {kv} on the current device with its rows whole, got {x.dtype} {tuple(x.shape)} with strides "
                          f"{at} on {x.device}")
     B, heads, n, _ = shape
-    return x.data_ptr(), (at[0] if B > 1 else 0, at[2] if n > 1 else 0, at[1] if heads > 1 else 0)
+    return x.data_ptr(), at[0] if B > 1 else 0, at[2] if n > 1 else 0, at[1] if heads > 1 else 0
 
 
 def _rows_of(desc, q, k, v, n, device):
     B, Hkv, d, kv = desc.B, desc.Hkv, desc.d, _FLOATS.get(desc.kv_dtype)
-    qp, qs = (None, (0, 0, 0)) if q is None else _strided(q, (B, desc.Hq, n, d), kv, "q", device)
-    kp, ks = _strided(k, (B, Hkv, n, d), kv, "k", device)
-    vp, vs = _strided(v, (B, Hkv, n, d), kv, "v", device)
-    return corm_rows(qp, kp, vp, qs, ks, vs)
+    q, *qs = (None, 0, 0, 0) if q is None else _strided(q, (B, desc.Hq, n, d), kv, "q", device)
+    k, *ks = _strided(k, (B, Hkv, n, d), kv, "k", device)
+    v, *vs = _strided(v, (B, Hkv, n, d), kv, "v", device)
+    return corm_rows(q, k, v, *qs, *ks, *vs)
 
 
 def _tokens(k) -> int:

@@ -117,27 +117,27 @@ struct Four {
   }
 };
 
-// A lane's eight channels, c0 .. +4 and c1 .. +4.  JOINED: c1 = c0 + 4, one access where the type is small enough.
+// A lane's eight channels, four and four that lie `apart` bytes behind.  JOINED: side by side, one access where the type is small enough.
 template <typename DT, bool JOINED>
-__device__ __forceinline__ void load_eight(Four<DT> (&f)[2], const char* row, int c0, int c1) {
+__device__ __forceinline__ void load_eight(Four<DT> (&f)[2], const char* at, int apart) {
   if constexpr (JOINED && DT::ESZ == 2) {
-    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(row + c0 * 2);
+    const u32x4_t x = *reinterpret_cast<const u32x4_t*>(at);
     f[0].w[0] = x.x; f[0].w[1] = x.y; f[1].w[0] = x.z; f[1].w[1] = x.w;
   } else {
-    f[0].load(row + c0 * DT::ESZ);
-    f[1].load(row + c1 * DT::ESZ);
+    f[0].load(at);
+    f[1].load(at + apart);
   }
 }
 template <typename DT, bool JOINED>
-__device__ __forceinline__ void store_eight(char* row, int c0, int c1, const float* y) {
+__device__ __forceinline__ void store_eight(char* at, int apart, const float* y) {
   Four<DT> f[2];
   f[0].round(y);
   f[1].round(y + 4);
   if constexpr (JOINED && DT::ESZ == 2) {
-    __builtin_nontemporal_store(u32x4_t{f[0].w[0], f[0].w[1], f[1].w[0], f[1].w[1]}, reinterpret_cast<u32x4_t*>(row + c0 * 2));
+    __builtin_nontemporal_store(u32x4_t{f[0].w[0], f[0].w[1], f[1].w[0], f[1].w[1]}, reinterpret_cast<u32x4_t*>(at));
   } else {
-    f[0].store(row + c0 * DT::ESZ);
-    f[1].store(row + c1 * DT::ESZ);
+    f[0].store(at);
+    f[1].store(at + apart);
   }
 }
 
@@ -170,7 +170,7 @@ __device__ __forceinline__ uint32_t row_allreduce_max(uint32_t v) {
 template <typename C, typename DT, int D, bool JOINED>
 __device__ __forceinline__ void put_row(char* pool, float* scales, size_t row, int cl, int c0, int c1, const float* y) {
   if constexpr (C::ID < 0) {
-    store_eight<DT, JOINED>(pool + row * (D * DT::ESZ), c0, c1, y);
+    store_eight<DT, JOINED>(pool + row * (D * DT::ESZ) + c0 * DT::ESZ, (c1 - c0) * DT::ESZ, y);
   } else {
     uint32_t top = 0;   // as bits: what is not a number is above infinity, and that above all others
 #pragma unroll
@@ -235,18 +235,35 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
       Four<DT> x[U][2];
       int L0[U];
     };
-    auto kind_of = [&](int head) { return head < a.Hq ? 0 : head < a.Hq + a.Hkv ? 1 : 2; };
+    const int nq = a.Hq, nqk = a.Hq + a.Hkv;
+    const bool paged = !a.k_out;
+    // Where this lane's channels of its token lie.  TOKENS: what does not depend on the head is formed once (else a wave has hardly more than one).
+    const char *q0 = nullptr, *k0 = nullptr, *v0 = nullptr;
+    if constexpr (TOKENS) {
+      q0 = a.q + b * a.qs.seq + tok * a.qs.token + c0 * DT::ESZ;
+      k0 = a.k + b * a.ks.seq + tok * a.ks.token + c0 * DT::ESZ;
+      v0 = a.v + b * a.vs.seq + tok * a.vs.token + c0 * DT::ESZ;
+    }
+    const int64_t qh = a.qs.head, kh = a.ks.head, vh = a.vs.head, oh = (int64_t)a.n * (D * DT::ESZ);   // bytes from head to head
+    char* const qo = a.q_out + ((int64_t)b * a.Hq * a.n + tok) * (D * DT::ESZ) + c0 * DT::ESZ;
+    const int64_t kv_row = ((int64_t)b * a.Hkv * a.n + tok) * (D * DT::ESZ) + c0 * DT::ESZ;
+    const int apart = (c1 - c0) * DT::ESZ;   // bytes between the lane's two fours
     auto load = [&](Batch& t, int h0) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int head = h0 + u * step + (TOKENS ? 0 : sub);
         if (head >= end || !in) continue;
-        const int kind = kind_of(head), h = head - (kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + a.Hkv);
-        const char* base = kind == 0 ? a.q : kind == 1 ? a.k : a.v;
-        const int64_t sq = kind == 0 ? a.qs.seq : kind == 1 ? a.ks.seq : a.vs.seq, st = kind == 0 ? a.qs.token : kind == 1 ? a.ks.token : a.vs.token,
-                      sh = kind == 0 ? a.qs.head : kind == 1 ? a.ks.head : a.vs.head;
-        load_eight<DT, JOINED>(t.x[u], base + b * sq + h * sh + tok * st, c0, c1);
-        if (!a.k_out && kind != 0) t.L0[u] = a.lens[(size_t)b * a.pages.TH + (a.pages.TH == 1 ? 0 : h)];
+        const bool isq = head < nq, isk = !isq && head < nqk;
+        const int h = head - (isq ? 0 : isk ? nq : nqk);
+        if constexpr (TOKENS) {
+          load_eight<DT, JOINED>(t.x[u], isq ? q0 + h * qh : isk ? k0 + h * kh : v0 + h * vh, apart);
+        } else {
+          const char* base = isq ? a.q : isk ? a.k : a.v;
+          const int64_t sq = isq ? a.qs.seq : isk ? a.ks.seq : a.vs.seq, st = isq ? a.qs.token : isk ? a.ks.token : a.vs.token,
+                        sh = isq ? a.qs.head : isk ? a.ks.head : a.vs.head;
+          load_eight<DT, JOINED>(t.x[u], base + b * sq + h * sh + tok * st + c0 * DT::ESZ, apart);
+        }
+        if (paged && head >= nq) t.L0[u] = a.lens[(size_t)b * a.pages.TH + (a.pages.TH == 1 ? 0 : h)];
       }
     };
     Batch now;
@@ -267,35 +284,34 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
       for (int e = 0; e < 4; ++e) turn[e] = turns[wv][TOKENS ? sub : 0][4 * cl + e];
     }
     Four<DT> wq[2], wk[2];
-    if (a.q_norm) load_eight<DT, JOINED>(wq, a.q_norm, c0, c1);
-    if (a.k_norm) load_eight<DT, JOINED>(wk, a.k_norm, c0, c1);
+    if (a.q_norm) load_eight<DT, JOINED>(wq, a.q_norm + c0 * DT::ESZ, apart);
+    if (a.k_norm) load_eight<DT, JOINED>(wk, a.k_norm + c0 * DT::ESZ, apart);
     for (int h0 = wv * each; h0 < end; h0 += step * U) {
       Batch next;
       load(next, h0 + step * U);
       int id[U];
-      if (!a.k_out) {   // the pages, behind the loads of the next rows
+      if (paged) {   // the pages, behind the loads of the next rows
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-          const int head = h0 + u * step + (TOKENS ? 0 : sub), kind = kind_of(head), h = head - (kind == 1 ? a.Hq : a.Hq + a.Hkv);
-          if (head >= end || !in || kind == 0 || !has_room(now.L0[u], take, a.Lcap)) continue;
-          id[u] = table_of(a.pages, b, h)[(now.L0[u] + tok) >> a.pages.shift];
+          const int head = h0 + u * step + (TOKENS ? 0 : sub);
+          if (head >= end || !in || head < nq || !has_room(now.L0[u], take, a.Lcap)) continue;
+          id[u] = table_of(a.pages, b, head < nqk ? head - nq : head - nqk)[(now.L0[u] + tok) >> a.pages.shift];
         }
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const int head = h0 + u * step + (TOKENS ? 0 : sub);
         if (head >= end || !in) continue;
-        const int kind = kind_of(head), h = head - (kind == 0 ? 0 : kind == 1 ? a.Hq : a.Hq + a.Hkv);
         float y[8];
         now.x[u][0].widen(y);
         now.x[u][1].widen(y + 4);
-        if (kind != 2) {
-          if (kind == 0 ? a.q_norm : a.k_norm) {
+        if (head < nqk) {
+          if (head < nq ? a.q_norm : a.k_norm) {
             float ss = 0.f, w[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
             const float r = rsqrtf(row_allreduce_sum<LPR>(ss) * (1.0f / D) + a.eps);
-            const Four<DT> f[2] = {kind == 0 ? wq[0] : wk[0], kind == 0 ? wq[1] : wk[1]};
+            const Four<DT> f[2] = {head < nq ? wq[0] : wk[0], head < nq ? wq[1] : wk[1]};
             f[0].widen(w);
             f[1].widen(w + 4);
 #pragma unroll
@@ -311,14 +327,16 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
             }
           }
         }
-        char* dense = kind == 0 ? a.q_out : kind == 1 ? a.k_out : a.v_out;
-        if (dense) {
-          const size_t row = ((size_t)b * (kind == 0 ? a.Hq : a.Hkv) + h) * a.n + tok;
-          store_eight<DT, JOINED>(dense + row * (D * DT::ESZ), c0, c1, y);
-        } else if (kind != 0 && has_room(now.L0[u], take, a.Lcap)) {   // (the same for all lanes of the row)
+        if (head < nq) {
+          store_eight<DT, JOINED>(qo + head * oh, apart, y);
+        } else if (!paged) {
+          store_eight<DT, JOINED>((head < nqk ? a.k_out + kv_row + (head - nq) * oh : a.v_out + kv_row + (head - nqk) * oh), apart, y);
+        } else if (has_room(now.L0[u], take, a.Lcap)) {   // (the same for all lanes of the row)
+          const bool isk = head < nqk;
+          const int h = head - (isk ? nq : nqk);
           if (is_page(a.pages, id[u])) {
-            put_row<C, DT, D, JOINED>(kind == 1 ? a.pages.K : a.pages.V, kind == 1 ? a.pages.ks : a.pages.vs,
-                                      pool_row(a.pages, id[u], h, now.L0[u] + tok), cl, c0, c1, y);
+            put_row<C, DT, D, JOINED>(isk ? a.pages.K : a.pages.V, isk ? a.pages.ks : a.pages.vs, pool_row(a.pages, id[u], h, now.L0[u] + tok), cl, c0, c1,
+                                      y);
           } else if (cl == 0 && a.status) {
             atomicOr(a.status, CORM_DEV_BAD_PAGE);
           }

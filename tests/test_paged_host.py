@@ -19,9 +19,13 @@ def _desc(**kw):
 
 
 def _rows(**kw):
-    r = corm.corm_rows(A, A, A, *[(ctypes.c_int64 * 3)(1536, 768, 128) for _ in range(3)])
+    r = corm.corm_rows(A, A, A, *([1536, 768, 128] * 3))
     for k, v in kw.items():
-        setattr(r, k, v if not isinstance(v, tuple) else (ctypes.c_int64 * 3)(*v))
+        if k.endswith("_stride"):
+            for of, x in zip(("seq", "token", "head"), v):
+                setattr(r, k.replace("stride", of), x)
+        else:
+            setattr(r, k, v)
     return r
 
 
@@ -137,7 +141,7 @@ def test_workspace():
 
 
 def test_structures_have_the_headers_layout():
-    assert ctypes.sizeof(corm.corm_rows) == 96 and corm.corm_rows.q_stride.offset == 24
+    assert ctypes.sizeof(corm.corm_rows) == 96 and corm.corm_rows.q_seq.offset == 24 and corm.corm_rows.v_head.offset == 88
     assert ctypes.sizeof(corm.corm_rotation) == 64 and corm.corm_rotation.eps.offset == 32 and corm.corm_rotation.inv_freq.offset == 40
     assert ctypes.sizeof(corm.corm_pages) == 64 and corm.corm_pages.K.offset == 24 and corm.corm_pages.table.offset == 56
 
