@@ -212,11 +212,11 @@ __device__ __forceinline__ void write_lens(const RowsArgs& a, int b, int take) {
 //
 // A row is the work of D / 8 lanes; a lane has four channels and the four that are paired with them, so nothing but the sum of squares goes from lane to
 // lane.  A workgroup has a group of tokens (TOKENS: as many as a wave has rows, so that what depends on the head is uniform; else one token, a head a
-// row), its waves share their heads.  A wave's angles are formed once, a pair a lane, and handed out through LDS.
+// row), its waves share their heads.  The angles are formed once, a pair a thread, and handed out through LDS.
 template <typename C, typename DT, int D, bool TOKENS, bool JOINED>
 __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const RowsArgs a) {
   constexpr int LPR = D / 8, RPW = 64 / LPR, TW = TOKENS ? RPW : 1, U = TOKENS ? 4 : 1;   // lanes of a row, rows and tokens of a wave, heads in flight
-  __shared__ float2 turns[TOKENS ? 4 : 16][TW][D / 2 + 2];   // (a token's angles start on other banks than its neighbours')
+  __shared__ float2 turns[TW][D / 2 + 2];   // (a token's angles start on other banks than its neighbours')
   const int b = blockIdx.y, wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int shares = blockDim.x >> 6, t0 = (int)blockIdx.x * TW;
   const int take = rows_taken(a, b);
@@ -269,19 +269,19 @@ __global__ __launch_bounds__(TOKENS ? 256 : 1024) void corm_rows_kernel(const Ro
     Batch now;
     load(now, wv * each);
     // the angles, behind the loads of the first rows
-    for (int i = lane; i < TW * half; i += 64) {
+    for (int i = threadIdx.x; i < TW * half; i += blockDim.x) {
       const int t = TOKENS ? i / half : 0, pair = i - t * half;
       const int pos = a.positions[((size_t)axis_of(a, pair) * a.B + b) * a.n + min(t0 + t, a.n - 1)];
       const double x = (double)pos * (double)a.inv_freq[pair] * HALF_TURNS;
       float s, c;
       sincospif((float)(x - 2.0 * rint(0.5 * x)), &s, &c);
-      turns[wv][t][pair] = make_float2(c * a.gain, s * a.gain);
+      turns[t][pair] = make_float2(c * a.gain, s * a.gain);
     }
-    __builtin_amdgcn_wave_barrier();   // (LDS operations of a wave are done in order)
+    __syncthreads();
     float2 turn[4];
     if (turned) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) turn[e] = turns[wv][TOKENS ? sub : 0][4 * cl + e];
+      for (int e = 0; e < 4; ++e) turn[e] = turns[TOKENS ? sub : 0][4 * cl + e];
     }
     Four<DT> wq[2], wk[2];
     if (a.q_norm) load_eight<DT, JOINED>(wq, a.q_norm + c0 * DT::ESZ, apart);
