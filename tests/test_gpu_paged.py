@@ -101,6 +101,74 @@ def test_rotate(dtype, d, kind):
         assert _same(only[0], outs[1]) and _same(only[1], outs[2])
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("bf16", 64), ("f32", 128), ("f32", 64)])
+@pytest.mark.parametrize("kind", [0, 1, 2, 6, 9])
+def test_rotate_long_prompts(dtype, d, kind):
+    """As many tokens as are taken in groups: odd numbers of them, a ragged batch, sequences without any."""
+    g = _gen(200 + kind)
+    for B, Hq, Hkv, n, n_new in ((6, 4, 2, 701, [701, 0, 700, 5, 698, 1]), (1, 3, 3, 4099, None)):
+        t = Turn(g, dtype, d, **TURNS[kind])
+        (q, k, v), (cq, ck, cv) = _packed(g, dtype, B, Hq, Hkv, n, d)
+        pos = torch.randint(0, 200000, (len(t.sections), B, n), generator=g, dtype=torch.int32)
+        outs = _nan(B, Hq, n, d, dtype=dtype), _nan(B, Hkv, n, d, dtype=dtype), _nan(B, Hkv, n, d, dtype=dtype)
+        corm.corm_rotate(corm.make_desc(B, Hq, Hkv, d, n, n, 1, 1, dtype), q, k, v, t.c, pos.to(DEV), *outs, n_new=None if n_new is None else _i32(n_new))
+        want = t.plain(cq, 0, pos), t.plain(ck, 1, pos)
+        for b in range(B):
+            take = n if n_new is None else n_new[b]
+            assert all(bool(o[b, :, take:].isnan().all()) for o in outs) and torch.equal(outs[2][b, :, :take].cpu(), cv[b, :, :take])
+            for i in range(2 if take else 0):
+                _close(outs[i][b, :, :take], want[i][0][b, :, :take], want[i][1][b, :, :take], dtype, (B, n, b, i))
+
+
+@pytest.mark.parametrize("dtype,code", [("bf16", None), ("f32", None), ("bf16", "i8"), ("bf16", "e4m3"), ("f32", "i8"), ("f32", "e4m3")])
+@pytest.mark.parametrize("d,per_head", [(128, False), (64, True)])
+def test_append_long_prompts(dtype, code, d, per_head):
+    """Groups of tokens into pages, the lengths replaced in place: ragged, behind rows that are there, without room, without a page."""
+    g = _gen(24)
+    B, n = 6, 701
+    c = Cache(g, B, 2, 2, d, 1500, dtype, code, 32, per_head)
+    c.append(_normal(g, dtype, B, 2, 7, d), _normal(g, dtype, B, 2, 7, d), [7, 0, 1, 3, 7, 2])
+    for n_new in ([701, 0, 700, 5, 698, 1], [701, 701, 701, 701, 701, 0]):
+        c.append(_normal(g, dtype, B, 2, n, d), _normal(g, dtype, B, 2, n, d, scale=9.0), n_new)
+        c.check()
+    assert int(c.status) == 0
+    c.append(_normal(g, dtype, B, 2, n, d), _normal(g, dtype, B, 2, n, d), [701, 701, 701, 0, 90, 701])       # no room in the first, the third
+    c.check()
+    assert int(c.status) == corm.CORM_DEV_UNIT_FULL
+    q = _normal(g, dtype, B, 2, d, scale=2.0)
+    c.attend(q)
+    c.check_out(q)
+    c = Cache(g, B, 2, 2, d, 704, dtype, code, 32, per_head)
+    c.dev_table[2, 0, 3] = -1
+    c.append(_normal(g, dtype, B, 2, n, d), _normal(g, dtype, B, 2, n, d), None)
+    assert int(c.status) == corm.CORM_DEV_BAD_PAGE and bool((c.lens == n).all())
+    c.attend(q)
+    c.check_out(q, lambda b, h: range(96, 128) if b == 2 and (h == 0 or not per_head) else ())
+
+
+def test_rows_of_any_strides():
+    """Rows shared by heads and sequences (stride 0), tokens apart by more than a row, every layout the same rows."""
+    g = _gen(25)
+    t = Turn(g, "bf16", 128)
+    B, n = 2, 33
+    desc = corm.make_desc(B, 4, 2, 128, n, n, 1, 1, "bf16")
+    pos = torch.arange(B * n, dtype=torch.int32, device=DEV).view(1, B, n)
+    one = _normal(g, "bf16", 1, 1, n, 128).to(DEV)
+    q, k = one.expand(B, 4, n, 128), one.expand(B, 2, n, 128)
+    v = _normal(g, "bf16", n, 2, 3, B, 128).to(DEV)[:, :, 1].permute(2, 1, 0, 3)
+    outs = []
+    for x in ((q, k, v), (q.contiguous(), k.contiguous(), v.contiguous())):
+        o = [_nan(B, h, n, 128, dtype="bf16") for h in (4, 2, 2)]
+        corm.corm_rotate(desc, *x, t.c, pos, *o)
+        outs.append(o)
+    assert all(torch.equal(a, b) for a, b in zip(*outs)) and torch.equal(outs[0][2], v.contiguous())
+    bad = _normal(g, "bf16", B, 4, n, 132).to(DEV)[..., :128]           # rows that are not 16 bytes apart
+    with pytest.raises(corm.CormError):
+        corm.corm_rotate(desc, bad, k, v, t.c, pos, *outs[0])
+    with pytest.raises(ValueError):                                     # channels that do not lie together
+        corm.corm_rotate(desc, q, k, v.transpose(2, 3).contiguous().transpose(2, 3), t.c, pos, *outs[0])
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rotate_far_positions(dtype):
     """Angles of positions up to the largest int32 are as exact as near ones."""
@@ -701,6 +769,34 @@ def test_pages_beside_a_layer_state():
                 err = 2 * ref.attend_error(s[0][b, 4 * h:4 * h + 4].cpu().double(), K, V, ref.sm_of(d))
                 assert float((pg.out - st.out)[b, 4 * h:4 * h + 4].abs().max()) <= err
     assert int(pg.status) == 0 and int(st.status) == 0
+
+
+def test_two_graphs_share_a_workspace():
+    """Attention over two caches of other shapes, captured with one workspace and replayed in turns, with eager calls between."""
+    g = _gen(43)
+    caches = [Cache(g, 3, 8, 2, 128, 9000, "bf16", "i8", 64, False), Cache(g, 40, 4, 2, 64, 1100, "f32", None, 16, True), Cache(g, 2, 4, 4, 128, 50, "bf16")]
+    ws = torch.empty(max(corm.corm_paged_workspace_bytes(c.desc) for c in caches), dtype=torch.uint8, device=DEV)
+    qs, want = [], []
+    for c in caches:
+        n = c.Hkv if c.per_head else 1
+        c.fill(g, [[(997 * (b * n + h) + 331) % (c.desc.Lcap + 1) for h in range(n)] for b in range(c.B)])
+        c.ws = ws
+        qs.append(_normal(g, c.dtype, c.B, c.Hq, c.d).to(DEV))
+        c.attend(qs[-1])
+        c.check_out(qs[-1].cpu())
+        want.append(c.out.clone())
+    graphs = []
+    for c, q in zip(caches, qs):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            corm.corm_paged_attend(c.desc, c.pages, q, c.lens, c.out, ws)
+    for i in (0, 1, 2, 1, 0, 2, 2, 0, 1):
+        caches[i].out.zero_()
+        graphs[i].replay()
+        assert torch.equal(caches[i].out, want[i])
+        caches[(i + 1) % 3].attend(qs[(i + 1) % 3])
+        torch.cuda.synchronize()
+        assert torch.equal(caches[(i + 1) % 3].out, want[(i + 1) % 3])
 
 
 @pytest.mark.parametrize("code", [None, "i8"])
