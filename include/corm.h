@@ -369,7 +369,8 @@ int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int
  * elements of a row lie together.  Bases 16-byte aligned, strides >= 0 and whole multiples of 16 bytes.
  *
  * corm_rotation: what queries and keys go through, all in fp32 and rounded once where they are stored:
- *   norm      y = x * weight / sqrt(mean of x^2 over the d channels + eps), per head, where q_norm (k_norm) [d], kv_dtype, is given
+ *   norm      y = x * weight / sqrt(mean of x^2 over the d channels + eps), per head, where q_norm (k_norm) [d], kv_dtype, is given (the squares'
+ *             sum is fp32: rows of elements beyond 10^18 have none)
  *   rotation  of the first rot channels, rot / 2 pairs: pair i is turned by the angle positions[axis(i)][b][token] * inv_freq[i], formed in
  *             64 bits:  (u, v) -> gain * (u cos - v sin, v cos + u sin).  CORM_HALVES: pair i is channels i and i + rot / 2;
  *             CORM_NEIGHBOURS: 2i and 2i + 1.  Channels at and above rot are normed only, values go as they are.
@@ -411,7 +412,7 @@ int corm_rotate(const corm_desc* desc, const corm_rows* rows, const corm_rotatio
  *           (amax < 2^-100: zeros with scale 0; an element that is infinite or not a number: codes 0 and a scale that is none).
  * page 16, 32, 64, 128 or 256; Lcap (the descriptor's) <= max_pages * page bounds every length.  Entries of the table behind a unit's last
  * page are never used and may hold anything.  An entry below 0 or >= npages is no page: its slots are neither written nor read
- * (CORM_DEV_BAD_PAGE).  A page that several tables hold is read by all of them; two units that write to it race. */
+ * (CORM_DEV_BAD_PAGE).  A page that several tables hold is read by all of them; two units that write to it race, and so does one whose table holds it twice. */
 typedef struct corm_pages {
   int32_t dtype, page, npages, max_pages, table_heads;
   int32_t reserved;            /* 0 */
@@ -434,7 +435,8 @@ int corm_paged_read(const corm_desc* desc, const corm_pages* pages, const int32_
                     int32_t* status, void* stream);
 
 /* Decode attention (Eq. 1) over the slots < lens: q [B, Hq, d] kv_dtype, out [B, Hq, d] float32, 0 where a unit has no slot that can be read.
- * Workspace (256-byte aligned, of corm_paged_workspace_bytes): partials alone; nothing in it has to be prepared or survives a call. */
+ * (A row whose scale is none makes the outputs over it none.)  Workspace (256-byte aligned, of corm_paged_workspace_bytes): partials and where they
+ * lie; nothing in it has to be prepared or survives a call, so calls on one stream, and graphs that are replayed one after the other, may share it. */
 int corm_paged_workspace_bytes(const corm_desc* desc, size_t* bytes);
 int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void* q, const int32_t* lens, float* out, void* workspace,
                       size_t workspace_bytes, int32_t* status, void* stream);

@@ -102,7 +102,7 @@ int launch_rows_d(RowsArgs& a, hipStream_t s) {
   // Groups of tokens once they make two workgroups per compute unit, else a workgroup a token.  Us, a token | a group: bf16, d 128, 48 heads, 512, 1024,
   // 2048, 4096 and 8192 tokens 6.5 | 12.2, 10.0 | 13.1, 16.9 | 15.9, 31.2 | 22.2 and 67 | 47; fp32, d 64, 10 heads, 2048 and 8192 4.9 | 5.8 and 10.4 | 9.7.
   const bool tokens = a.n >= RPW && (long)a.n * a.B >= 2L * RPW * device_cus();
-  const dim3 grid((unsigned)(tokens ? (a.n + RPW - 1) / RPW : a.n), a.B), wg(64 * (tokens ? 4 : std::min(16, (heads + RPW - 1) / RPW)));
+  const dim3 grid((unsigned)(tokens ? ((long)a.n + RPW - 1) / RPW : a.n), a.B), wg(64 * (tokens ? 4 : std::min(16, (heads + RPW - 1) / RPW)));
   if ((long long)grid.x * wg.x > 4294967295LL) return CORM_EUNSUPPORTED;   // (threads of a launch)
   a.lens_here = a.lens_out && (grid.x == 1 || a.lens_out != a.lens);
   auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, wg, 0, s, a); };

@@ -99,9 +99,52 @@ static void arguments() {
   EXPECT(corm_version() >= 100);
 }
 
+// the cache of pages and the rows on their way into it
+static void pages() {
+  corm_desc d = desc(2, 8, 2, 128, 1024, 1024, 16, 16, CORM_BF16, CORM_BF16);
+  alignas(256) static unsigned char fake[4096];
+  int32_t* i = reinterpret_cast<int32_t*>(fake);
+  float* f = reinterpret_cast<float*>(fake);
+  corm_pages p;
+  std::memset(&p, 0, sizeof p);
+  p.dtype = CORM_BF16; p.page = 16; p.npages = 2147483647; p.max_pages = 64; p.table_heads = 1;
+  p.K = fake; p.V = fake; p.table = i;
+  corm_rows r;
+  std::memset(&r, 0, sizeof r);
+  r.q = r.k = r.v = fake;
+  corm_rotation t;
+  std::memset(&t, 0, sizeof t);
+  t.rot = 128; t.axes = 4; t.section[0] = 61; t.section[1] = t.section[2] = t.section[3] = 1; t.in_turn = 1; t.gain = 1.f; t.inv_freq = f;
+  size_t n = 0;
+  EXPECT(corm_paged_workspace_bytes(&d, &n) == CORM_OK && n % 256 == 0);
+  EXPECT(corm_paged_workspace_bytes(&d, nullptr) == CORM_EINVAL && corm_paged_workspace_bytes(nullptr, &n) == CORM_EINVAL);
+  // fine but for the workspace
+  EXPECT(corm_paged_attend(&d, &p, fake, i, f, fake, n - 1, nullptr, nullptr) == CORM_ECAPACITY);
+  EXPECT(corm_paged_attend(&d, &p, fake, i, f, fake + 16, n, nullptr, nullptr) == CORM_EINVAL);
+  corm_pages bad = p;
+  bad.max_pages = 63;                      // fewer slots than the descriptor's
+  EXPECT(corm_paged_attend(&d, &bad, fake, i, f, fake, n, nullptr, nullptr) == CORM_EINVAL);
+  bad = p; bad.max_pages = 2147483647; bad.page = 256; bad.table_heads = 3;
+  EXPECT(corm_paged_read(&d, &bad, i, 4, fake, fake, nullptr, nullptr) == CORM_EINVAL);
+  bad = p; bad.dtype = CORM_I8;            // codes without scales
+  EXPECT(corm_paged_append(&d, &bad, &r, nullptr, nullptr, 1, nullptr, nullptr, i, i, nullptr, nullptr) == CORM_EINVAL);
+  EXPECT(corm_paged_append(&d, &p, &r, nullptr, nullptr, 1025, nullptr, nullptr, i, i, nullptr, nullptr) == CORM_EINVAL);
+  corm_rotation u = t;
+  u.section[1] = 2147483647;               // sums and places in 64 bits
+  u.section[2] = 2147483647;
+  EXPECT(corm_rotate(&d, &r, &u, i, 4, nullptr, fake, fake, fake, nullptr) == CORM_EINVAL);
+  u = t; u.section[0] = -2147483647 - 1;
+  EXPECT(corm_rotate(&d, &r, &u, i, 4, nullptr, fake, fake, fake, nullptr) == CORM_EINVAL);
+  corm_rows s = r;
+  s.k_stride[1] = INT64_MAX;               // no multiple of 16 bytes
+  EXPECT(corm_rotate(&d, &s, &t, i, 4, nullptr, fake, fake, fake, nullptr) == CORM_EINVAL);
+  EXPECT(corm_rotate(&d, &r, &t, i, 2147483647, nullptr, fake, fake, fake, nullptr) == CORM_EUNSUPPORTED);   // more threads than a launch has
+}
+
 int main() {
   limits();
   arguments();
+  pages();
   // the same checks from two threads at once: the library keeps no mutable state of its own
   std::vector<std::thread> th;
   for (int k = 0; k < 2; ++k)
@@ -109,6 +152,7 @@ int main() {
       for (int rep = 0; rep < 200; ++rep) {
         limits();
         arguments();
+        pages();
       }
     });
   for (auto& t : th) t.join();
