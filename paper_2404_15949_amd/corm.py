@@ -974,6 +974,8 @@ class PagedState:
     def step(self, q, k_new, v_new, rotation=None, positions=None, stream=None) -> None:
         """One decode step: the new row goes in, the query attends to all keys, itself among them.  With a rotation queries and keys come as the
         projection leaves them (positions [axes,B,1])."""
+        if _tokens(k_new) != 1:
+            raise ValueError(f"k_new {tuple(k_new.shape)}: a step has one token")
         if rotation is None:
             _check_query(self.desc, q)
             self.append(k_new, v_new, stream=stream)

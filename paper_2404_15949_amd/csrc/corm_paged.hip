@@ -252,7 +252,6 @@ int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void
   const bool shared = !alone && units * rounds > a.workgroups && a.tables <= SHARE_TABLES && units * rounds * WAVES < 2147483647L;
   a.npart = alone ? 1 : (int)std::min<long>({rounds, (a.workgroups + units - 1) / units, 2 * PAGED_MOST / units});
   hipStream_t s = (hipStream_t)stream;
-  // (a merge of few partials by 256 threads, of many by 1024)
   auto merge = [&](auto shared_, int parts) {
     constexpr bool SHARED = decltype(shared_)::value;
     const bool many = parts > 32;

@@ -170,6 +170,22 @@ def test_wrappers_refuse_what_does_not_fit():
         corm.Rotation(torch.zeros(64), pairing="thirds")
 
 
+def test_states_refuse_before_a_row_goes_in():
+    st = corm.PagedState(2, 8, 2, 128, 7, 4, "bf16", device="cpu")
+    assert bool((st.table == -1).all()) and tuple(st.K.shape) == (7, 2, 16, 128) and tuple(st.lens.shape) == (2, 1)
+    with pytest.raises(corm.CormError):
+        st.deal()                                                   # eight pages
+    rows = torch.zeros(2, 2, 3, 128, dtype=torch.bfloat16)
+    for rotation in (None, corm.Rotation(torch.zeros(64))):
+        with pytest.raises(ValueError):
+            st.step(torch.zeros(2, 8, 128, dtype=torch.bfloat16), rows, rows, rotation=rotation)
+    st = corm.PagedState(1, 4, 4, 64, 8, 2, "f32", page=32, code="e4m3", per_head=True, device="cpu")
+    st.deal()
+    assert st.table.flatten().tolist() == list(range(8)) and tuple(st.k_scale.shape) == (8, 32) and st.K.dtype == torch.float8_e4m3fn
+    with pytest.raises(corm.CormError):
+        corm.PagedState(1, 4, 4, 64, 8, 2, "f32", device="cpu", workspace=torch.zeros(16))
+
+
 def test_the_plain_rotation_keeps_lengths_and_turns_by_differences():
     """Norms stay; the product of a query and a key depends on the difference of their positions alone."""
     g = torch.Generator().manual_seed(3)
