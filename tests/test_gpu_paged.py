@@ -563,6 +563,48 @@ def test_attend_shares_of_all_units(dtype, d, B, Hkv, most, per_head):
             assert float((got - want).abs().max()) <= bound, (b, h, n)
 
 
+@pytest.mark.parametrize("B,Hkv,most", [(3, 2, 20000), (90, 6, 300), (2, 2, 300)])
+def test_attend_bad_lengths_and_pages_in_every_launch(B, Hkv, most):
+    """Shared tiles, whole units, a workgroup a round: lengths that are none are held to the bounds, pages that are none are not seen, both are reported."""
+    g = _gen(26)
+    d, G, page = 64, 2, 32
+    maxp = (most + page - 1) // page
+    lens = torch.randint(0, most + 1, (B, 1), generator=g, dtype=torch.int32)
+    lens[0], lens[1] = -5, most + 9
+    held = lens.clamp(0, most)
+    npages = 50
+    table = torch.randint(0, npages, (B, 1, maxp), generator=g, dtype=torch.int32)
+    K, V = ((torch.randn(npages, Hkv, page, d, generator=g) * 2).to(torch.bfloat16).to(DEV) for _ in range(2))
+    q = _normal(g, "bf16", B, Hkv * G, d, scale=2.0).to(DEV)
+    desc = corm.make_desc(B, Hkv * G, Hkv, d, most, most, 1, 1, "bf16")
+    ws, status = torch.empty(corm.corm_paged_workspace_bytes(desc), dtype=torch.uint8, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    outs = []
+    for x in (held, lens):
+        status.zero_()
+        outs.append(_nan(B, Hkv * G, d))
+        corm.corm_paged_attend(desc, corm.Pages(desc, K, V, table.to(DEV)), q, x.to(DEV), outs[-1], ws, status=status)
+        assert int(status) == (0 if x is held else corm.CORM_DEV_BAD_LENS)
+    assert torch.equal(*outs)
+    gone = torch.rand(B, 1, maxp, generator=g) < 0.3
+    gone[1, 0, 0] = True
+    td = torch.where(gone, torch.where(torch.rand(B, 1, maxp, generator=g) < 0.5, -1, npages), table).to(torch.int32).to(DEV)
+    out = _nan(B, Hkv * G, d)
+    status.zero_()
+    corm.corm_paged_attend(desc, corm.Pages(desc, K, V, td), q, held.to(DEV), out, ws, status=status)
+    assert int(status) == corm.CORM_DEV_BAD_PAGE
+    for b in range(0, B, 1 if B < 10 else 7):
+        n = int(held[b])
+        seen = ~gone[b, 0, torch.arange(n) // page].to(DEV)
+        for h in range(Hkv):
+            k, v = (p[table[b, 0].long().to(DEV), h].reshape(-1, d)[:n][seen].double() for p in (K, V))
+            x, got = q[b, h * G:(h + 1) * G].double(), out[b, h * G:(h + 1) * G].double()
+            if not k.shape[0]:
+                assert not got.any()
+                continue
+            want = torch.mm(torch.softmax(torch.mm(x, k.t()) * ref.sm_of(d), -1), v)
+            assert float((got - want).abs().max()) <= ref.attend_error(x, k, v, ref.sm_of(d)), (b, h, n)
+
+
 def test_attend_thousands_of_units():
     g = _gen(22)
     B, d = 4100, 64
