@@ -67,11 +67,9 @@ int check_rotation(const corm_desc* d, const corm_rotation* r, const int32_t* po
 int check_rows(const corm_desc* d, const corm_rows* r, bool with_q) {
   if (!r || !r->k || !r->v || misaligned16(r->k) || misaligned16(r->v)) return CORM_EINVAL;
   if (with_q && (!r->q || misaligned16(r->q))) return CORM_EINVAL;
-  const int per16 = 16 / elem_bytes(d);
-  for (int i = 0; i < 3; ++i) {
-    if (r->k_stride[i] < 0 || r->v_stride[i] < 0 || r->k_stride[i] % per16 || r->v_stride[i] % per16) return CORM_EINVAL;
-    if (with_q && (r->q_stride[i] < 0 || r->q_stride[i] % per16)) return CORM_EINVAL;
-  }
+  auto bad = [&](int64_t x) { return x < 0 || x > (1LL << 40) || x % (16 / elem_bytes(d)) != 0; };   // (more than any memory: offsets stay in 64 bits)
+  for (int i = 0; i < 3; ++i)
+    if (bad(r->k_stride[i]) || bad(r->v_stride[i]) || (with_q && bad(r->q_stride[i]))) return CORM_EINVAL;
   return CORM_OK;
 }
 

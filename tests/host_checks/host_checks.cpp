@@ -138,6 +138,8 @@ static void pages() {
   corm_rows s = r;
   s.k_stride[1] = INT64_MAX;               // no multiple of 16 bytes
   EXPECT(corm_rotate(&d, &s, &t, i, 4, nullptr, fake, fake, fake, nullptr) == CORM_EINVAL);
+  s.k_stride[1] = INT64_MAX - 7;           // beyond any memory
+  EXPECT(corm_rotate(&d, &s, &t, i, 4, nullptr, fake, fake, fake, nullptr) == CORM_EINVAL);
   EXPECT(corm_rotate(&d, &r, &t, i, 2147483647, nullptr, fake, fake, fake, nullptr) == CORM_EUNSUPPORTED);   // more threads than a launch has
 }
 
