@@ -214,8 +214,9 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, int wg, int tile_s
 // each, without loss, so everything is exact but for the sums, which are fp32.
 //
 // Bound by HBM: 16 x 32 units of 3352 .. 4352 bf16 slots, d 128, 162 us (6.2 TB/s), vector ALU 14 % and matrix cores 8 % busy (8 int8 units of 131072: 44 and
-// 12 %).  Tiles of 32 slots for codes: 64 take the registers of a third wave (512 int8 units x 8192 180 us | 198).  Fading in every tile, where all
-// lanes have to agree on the maximum first: int8 units of 131072 63.4 us | 62.4.  Two workgroups per compute unit have enough under way (shares of
+// 12 %).  Tiles of 32 slots for codes: 64 take the registers of a third wave (512 int8 units x 8192 180 us | 198).  Sums fade in tiles that raise a
+// maximum: fading in every tile, where all lanes have to agree on it first, 63.4 us | 62.4 for int8 units of 131072; letting it fall short by up to 2^8, so that
+// hardly a tile raises it, gains nothing (66.6 | 65.7, others the same) and takes 2^8 from the range of the sums.  Two workgroups per compute unit have enough under way (shares of
 // 128 units of 4192 .. 8192 bf16 slots: one 72 us, two 74, three 78; of 8 int8 units of 131072 78, 56, 60).
 template <typename P, typename DT, int D, bool SHARED>
 __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArgs a) {
@@ -225,9 +226,6 @@ __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArg
   constexpr int VL = P::ESZ == 4 ? D / 64 : 1;         // loads of a value row by its sixteen lanes,
   constexpr int VW = P::ESZ == 4 ? 4 : RB / 64;        // of so many words
   constexpr int CT = D / 16;
-  // What a head's exponentials are relative to may be below its maximum by so much before it is raised: the sums are floating, so nothing is lost, and
-  // hardly a tile has to fade them.
-  constexpr float SLACK = 8.f;
   __shared__ float sh_acc[WAVES][8][D];
   __shared__ float sh_m[WAVES][8], sh_z[WAVES][8];
   __shared__ int sh_share[SHARED ? WAVES + 3 : 1];
@@ -261,7 +259,7 @@ __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArg
     // (row of a slot in the pool; with a number that is none: some row)
     auto row_at = [&](int id, int slot) { return pool_row(a.pages, is_page(a.pages, id) ? id : 0, h, slot); };
     PagedQuery<P, DT, D> q;
-    float m_run = neg_inf(), z_run = 0.f;   // what head n's exponentials are relative to (the same in all its lanes), their sum over this lane's slots
+    float m_run = neg_inf(), z_run = 0.f;   // head n's maximum (the same in all its lanes), the exponentials' sum over this lane's slots
     f32x4_t acc[CT] = {};                   // CPL channels of this lane's columns (f32: four of each 64)
     int tile = first + wv;
     // the unit behind this one, if the run goes on there
@@ -356,7 +354,7 @@ __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArg
             s[t][j] = x;
             top = fmaxf(top, x);
           }
-        if (__any(top > m_run + SLACK)) {
+        if (__any(top > m_run)) {   // (no weight is above 1, so sums overflow only where the values' own sum does)
           const float m = fmaxf(m_run, rows_allreduce_max(top));
           const float fade = m == neg_inf() ? 0.f : fast_exp2(m_run - m);
           m_run = m;

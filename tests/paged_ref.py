@@ -63,3 +63,18 @@ def attend_error(q, K, V, sm):
 
 def sm_of(d):
     return 1.0 / math.sqrt(d)
+
+
+def weighted_error(q, K, V, sm):
+    """Bound [G,d] of the output's error where every logit is ONE product (queries of one channel), relative to what the channel's sum is made of,
+    sum p |v|, so that nothing hides behind the largest value of another row or channel.
+
+    A logit: a product (two steps at most, an fp32 query over codes in three parts), the scale (root, quotient, log2 e, its product, itself: five
+    halves), the row's scale (one): 10 EPS of it, of the maximum as much, their difference 2: 22 EPS of the largest; the exponential a step (2 EPS).
+    Both sums have that.  A sum of n weights, each in three parts: 4 n + 16 additions and products, a step (2 EPS) each if they are cut off."""
+    n = K.shape[0]
+    if n == 0:
+        return torch.zeros_like(q)
+    p = ref.attention(q, K, V, sm)[1]
+    a = float((q.abs() @ K.abs().t()).max()) * sm
+    return (2 * (22 * a + 2) + 2 * (4 * n + 16)) * EPS * (p @ V.abs())

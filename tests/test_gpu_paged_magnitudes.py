@@ -1,0 +1,70 @@
+"""Attention over pages where magnitudes matter: values near the largest that the type has, infinite ones, rows whose scales lie far apart, and outputs
+held to what each channel's sum is made of."""
+import pytest
+import torch
+
+from paper_2404_15949_amd import corm
+from tests import paged_inputs as inp
+from tests import paged_ref as ref
+from tests.test_gpu_paged import DEV, FORMS, Cache, _gen
+
+pytestmark = pytest.mark.gpu
+
+# B, Hkv, the bound of a length, lengths: whole units by one workgroup, a workgroup a round and a merge, shares of all units' tiles
+LAUNCHES = {"whole": (2, 1, 190, [190, 150]), "parts": (2, 1, 2000, [190, 1999]), "shares": (8, 2, 9000, [190, 8999, 1, 33, 700, 0, 128, 2500])}
+
+
+def _cache(g, launch, dtype, code, d, G=4, page=64):
+    B, Hkv, most, lens = LAUNCHES[launch]
+    return Cache(g, B, G * Hkv, Hkv, d, most, dtype, code, page, False), lens
+
+
+def _hold(c, k, v, lens):
+    """Units of `lens` rows of k and v [B,Hkv,n,d]"""
+    corm.corm_paged_append(c.desc, c.pages, k.to(DEV), v.to(DEV), c.lens, c.lens, n_new=torch.tensor(lens, dtype=torch.int32, device=DEV), status=c.status)
+    for b in range(c.B):
+        for h in range(c.Hkv):
+            c.rows[b][h] = [list(k[b, h, :lens[b]]), list(v[b, h, :lens[b]])]
+
+
+def _check(c, q):
+    """... against 64 bits, channel by channel; infinities and what is not a number where the definition has them"""
+    G, sm, got = c.Hq // c.Hkv, ref.sm_of(c.d), c.out.cpu().double()
+    assert int(c.status) == 0
+    for b in range(c.B):
+        for h in range(c.Hkv):
+            K, V = c.unit(b, h, 0), c.unit(b, h, 1)
+            x, o = q[b, h * G:(h + 1) * G].double(), got[b, h * G:(h + 1) * G]
+            if not K.shape[0]:
+                assert not o.any()
+                continue
+            odd = ~V.isfinite()
+            F = V.masked_fill(odd, 0.0)
+            want, bound = ref.attend(x, K, F, sm), ref.weighted_error(x, K, F, sm)
+            plus, minus, none = ((V == float("inf")).any(0), (V == -float("inf")).any(0), V.isnan().any(0))
+            none = none | (plus & minus)
+            plus, minus = plus & ~none, minus & ~none
+            assert torch.equal(o.isnan(), none.expand_as(o)), (b, h)
+            assert torch.equal(o == float("inf"), plus.expand_as(o)) and torch.equal(o == -float("inf"), minus.expand_as(o)), (b, h)
+            fine = ~odd.any(0)
+            err = ((o - want).abs() - bound)[:, fine].max()
+            assert float(err) <= 0, (b, h, K.shape[0], float(((o - want).abs() / bound)[:, fine].max()))
+
+
+@pytest.mark.parametrize("dtype,code", FORMS)
+@pytest.mark.parametrize("d", [128, 64])
+def test_values_near_the_largest(dtype, code, d):
+    """The sum of all magnitudes is within fp32, so is every output: also where the maximum of the scores rises from tile to tile by less than would
+    matter for smaller values, in steps of 7.8 (log2), and where one value alone is nearly the largest."""
+    g = _gen(62)
+    c, lens = _cache(g, "whole", dtype, code, d)
+    q, k, _ = inp.one_channel(g, dtype, c.B, c.Hq, c.Hkv, max(lens), d)
+    q[..., 0], k[..., 0] = 1.0, 0.0
+    at = 64 if dtype == "f32" and code is None else 128            # slots that the waves take at a time
+    k[:, :, at:, 0] = 7.8 * 0.6931 * d ** 0.5
+    v = (1 + torch.rand(c.B, c.Hkv, max(lens), d, generator=g)) * 2.0 ** 118 * (1 - 2 * torch.randint(0, 2, (c.B, c.Hkv, max(lens), d), generator=g))
+    v[0, 0, at + 1] = 0
+    v[0, 0, at + 1, ::3] = 2.0 ** 126
+    _hold(c, k, v.to(k.dtype), lens)
+    c.attend(q)
+    _check(c, q)
