@@ -436,7 +436,8 @@ int corm_paged_read(const corm_desc* desc, const corm_pages* pages, const int32_
 
 /* Decode attention (Eq. 1) over the slots < lens: q [B, Hq, d] kv_dtype, out [B, Hq, d] float32, 0 where a unit has no slot that can be read.
  * (A row whose scale is none makes the outputs over it none.)  Sums are fp32, no weight in them is above 1: outputs are finite where the sum of the magnitudes of
- * a channel's values is.  Workspace (256-byte aligned, of corm_paged_workspace_bytes): partials and where they
+ * a channel's values is.  A value that is seen and not a number makes its channel of the outputs none, an infinite one (of a weight above 2^-90) infinite.
+ * Workspace (256-byte aligned, of corm_paged_workspace_bytes): partials and where they
  * lie; nothing in it has to be prepared or survives a call, so calls on one stream, and graphs that are replayed one after the other, may share it. */
 int corm_paged_workspace_bytes(const corm_desc* desc, size_t* bytes);
 int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void* q, const int32_t* lens, float* out, void* workspace,

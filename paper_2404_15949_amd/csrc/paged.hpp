@@ -50,8 +50,13 @@ __device__ __forceinline__ bf16x8_t bf16x8_of(uint32_t a, uint32_t b, uint32_t c
 // the upper halves of two numbers, side by side
 __device__ __forceinline__ uint32_t uppers(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
 
-// Eight numbers as three bf16 each, towards zero: 24 bits together, so nothing is lost.
+// Eight numbers as three bf16 each, cut off: 24 bits together, so nothing is lost.
+// WEIGHTS: the numbers are not negative, and no part of one above 0 is 0, so that an infinite value times its parts is infinite and not 0 x infinity: what
+// is cut is a last place of fp32 less.  Nothing is lost so either: with R the first rest in last places of x, 1 <= R <= 2^16, the second part is below R by
+// at most 2^8 of them, a whole number, which the third has (where it is in range: x at and above 2^-95; 0 stays 0).
+template <bool WEIGHTS>
 __device__ __forceinline__ void split3(const float* x, bf16x8_t (&part)[3]) {
+  auto cut = [](float f) { return WEIGHTS ? __builtin_elementwise_sub_sat(__float_as_uint(f), 1u) : __float_as_uint(f); };
   uint32_t w[3][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -59,9 +64,9 @@ __device__ __forceinline__ void split3(const float* x, bf16x8_t (&part)[3]) {
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       const float f = x[2 * i + k];
-      u[0][k] = __float_as_uint(f);
+      u[0][k] = cut(f);
       const float r = f - __uint_as_float(u[0][k] & 0xffff0000u);
-      u[1][k] = __float_as_uint(r);
+      u[1][k] = cut(r);
       u[2][k] = __float_as_uint(r - __uint_as_float(u[1][k] & 0xffff0000u));
     }
 #pragma unroll
@@ -131,7 +136,7 @@ struct PagedQuery {
           bf16x8_t s[3];
 #pragma unroll
           for (int e = 0; e < 8; ++e) y[e] = element<DT>(x[e / DT::EPL], e % DT::EPL);
-          split3(y, s);
+          split3<false>(y, s);
 #pragma unroll
           for (int p = 0; p < 3; ++p) part[p][kb] = s[p];
         }
@@ -397,7 +402,7 @@ __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArg
 #pragma unroll
           for (int u = 0; u < GROUP / 8; ++u) {
             bf16x8_t pp[3];
-            split3(p + 8 * u, pp);
+            split3<!P::CODES>(p + 8 * u, pp);   // (codes are finite)
             auto product = [&](int i, const uint32_t (&w)[4]) {
               const bf16x8_t x = bf16x8_of(w[0], w[1], w[2], w[3]);
 #pragma unroll

@@ -68,3 +68,25 @@ def test_values_near_the_largest(dtype, code, d):
     _hold(c, k, v.to(k.dtype), lens)
     c.attend(q)
     _check(c, q)
+
+
+@pytest.mark.parametrize("launch", LAUNCHES)
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d", [128, 64])
+def test_infinite_values_stay_in_their_channel(launch, dtype, d):
+    """A value that is infinite makes its channel's output so, the largest weight's and small ones'; one of each sign, or one that is no number, none; others are not touched."""
+    g = _gen(63)
+    c, lens = _cache(g, launch, dtype, None, d)
+    q, k, v = inp.one_channel(g, dtype, c.B, c.Hq, c.Hkv, max(lens), d)
+    k[:, :, 5, 0] = k[:, :, :, 0].max() + 1                        # the largest weight, of 1 where one wave has all slots
+    k[:, :, 6, 0] = -30.0
+    inf = float("inf")
+    v[:, :, 5, 1], v[:, :, 6, 2], v[:, :, 7, 3], v[:, :, 20, d - 1] = inf, -inf, inf, -inf
+    v[:, :, 8, 9], v[:, :, 9, 9] = inf, -inf
+    v[:, :, 10, 11] = float("nan")
+    for b, n in enumerate(lens):
+        if n > 100:
+            v[b, :, n - 1, 20], v[b, :, n // 2, 21] = inf, -inf
+    _hold(c, k, v, lens)
+    c.attend(q)
+    _check(c, q)
