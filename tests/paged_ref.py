@@ -78,3 +78,21 @@ def weighted_error(q, K, V, sm):
     p = ref.attention(q, K, V, sm)[1]
     a = float((q.abs() @ K.abs().t()).max()) * sm
     return (2 * (22 * a + 2) + 2 * (4 * n + 16)) * EPS * (p @ V.abs())
+
+
+def in_parts(x, parts):
+    """fp32 numbers as so many bf16, each cut off, added up again"""
+    left, out = x.float(), torch.zeros_like(x, dtype=torch.float64)
+    for _ in range(parts):
+        hi = (left.view(torch.int32) & -65536).view(torch.float32)
+        out += hi.double()
+        left = left - hi
+    return out
+
+
+def attend_in_parts(q, K, V, sm, parts, scale=None):
+    """Attention whose weights (times the rows' scales: V are codes then) are held in so many bf16 parts."""
+    s = q @ K.t() * sm
+    p = torch.exp(s - s.amax(-1, keepdim=True))
+    w = p.float() if scale is None else p.float() * scale.float()
+    return in_parts(w, parts) @ V / p.sum(-1, keepdim=True)

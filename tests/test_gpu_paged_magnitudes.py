@@ -51,6 +51,35 @@ def _check(c, q):
             assert float(err) <= 0, (b, h, K.shape[0], float(((o - want).abs() / bound)[:, fine].max()))
 
 
+@pytest.mark.parametrize("launch", LAUNCHES)
+@pytest.mark.parametrize("dtype,code", FORMS)
+@pytest.mark.parametrize("d", [128, 64])
+def test_every_channel_by_what_its_sum_is_made_of(launch, dtype, code, d):
+    g = _gen(60)
+    c, lens = _cache(g, launch, dtype, code, d)
+    q, k, v = inp.one_channel(g, dtype, c.B, c.Hq, c.Hkv, max(lens), d)
+    _hold(c, k, v, lens)
+    c.attend(q)
+    _check(c, q)
+
+
+@pytest.mark.parametrize("code", ["i8", "e4m3"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("d,most", [(128, 256), (64, 256), (128, 9000), (64, 60000)])
+def test_rows_with_tiny_scales_count_whole(dtype, code, d, most):
+    """A head whose weight lies on one row has that row, to the last bits, whatever the scales of the others: in one workgroup, in parts, in shares."""
+    for G in (1, 8):
+        g = _gen(61)
+        q, k, v, target = inp.one_row(g, dtype, G, 256, d)
+        c = Cache(g, 1, G, 1, d, most, dtype, code, 64, False)
+        c.append(k, v)
+        c.attend(q)
+        want = c.unit(0, 0, 1)[target]
+        assert int(c.status) == 0 and float(want.abs().amax(-1).min()) < 1e-22
+        got = c.out[0].cpu().double()
+        assert bool(((got - want).abs() <= inp.ONE_ROW * want.abs()).all()), (G, float(((got - want).abs() / want.abs().clamp(min=1e-99)).max()))
+
+
 @pytest.mark.parametrize("dtype,code", FORMS)
 @pytest.mark.parametrize("d", [128, 64])
 def test_values_near_the_largest(dtype, code, d):
