@@ -505,11 +505,27 @@ def corm_evict_mask_weight(desc, weight, lens, budget, keep, workspace, workspac
 
 # ---- a cache of pages, and the rows on their way into it
 
+def _watched(name):
+    """An attribute that holds a tensor: set anew, it is looked at by the next call."""
+    def put(self, x):
+        setattr(self, "_" + name, x)
+        self._seen = None
+    return property(operator.attrgetter("_" + name), put)
+
+
+def _memory(x):
+    """A tensor's memory, which stays its own as long as this is held: no other tensor gets its address meanwhile."""
+    return None if x is None else x.detach()
+
+
 class Rotation:
     """What a model does to its queries and keys before attention (corm_rotation): norms per head and the position rotation.  Made once.
 
     inv_freq [rot / 2] float32 (None: norms alone); q_norm, k_norm [d] in the KV type; pairing "halves" or "neighbours"; sections: the pairs of
-    each axis (None: one axis), dealt in blocks or in_turn."""
+    each axis (None: one axis), dealt in blocks or in_turn.  A tensor may be set anew, or get other memory or another type (a module that is moved): it is
+    looked at again.  One whose shape or strides are changed in place has to be set anew."""
+
+    inv_freq, q_norm, k_norm = (_watched(x) for x in ("inv_freq", "q_norm", "k_norm"))
 
     def __init__(self, inv_freq, q_norm=None, k_norm=None, eps=1e-6, pairing="halves", sections=None, in_turn=False, gain=1.0):
         half = 0 if inv_freq is None else inv_freq.numel()
@@ -522,15 +538,16 @@ class Rotation:
         self._seen = None
 
     def _bind(self, desc, device):
-        # the tensors are looked at again only where one has got other memory (a module moved its weights), or another call wants another type of them
-        seen = (device, desc.kv_dtype, desc.d, *[None if x is None else x.data_ptr() for x in (self.inv_freq, self.q_norm, self.k_norm)])
+        f, q, k = self._inv_freq, self._q_norm, self._k_norm
+        seen = (device, desc.kv_dtype, desc.d, None if f is None else (f.data_ptr(), f.dtype), None if q is None else (q.data_ptr(), q.dtype),
+                None if k is None else (k.data_ptr(), k.dtype))
         if seen != self._seen:
             _, _, _, kv = _sizes(desc)
             self._seen = None
-            self.c.inv_freq = _dev(self.inv_freq, self.rot // 2, _F4, "inv_freq", device)
-            self.c.q_norm = _dev(self.q_norm, desc.d, kv, "q_norm", device)
-            self.c.k_norm = _dev(self.k_norm, desc.d, kv, "k_norm", device)
-            self._seen = seen
+            self.c.inv_freq = _dev(f, self.rot // 2, _F4, "inv_freq", device)
+            self.c.q_norm = _dev(q, desc.d, kv, "q_norm", device)
+            self.c.k_norm = _dev(k, desc.d, kv, "k_norm", device)
+            self._held, self._seen = (_memory(f), _memory(q), _memory(k)), seen
         return ctypes.byref(self.c)
 
 
@@ -538,7 +555,9 @@ class Pages:
     """A pool of pages and the tables of the units (corm_pages).  Made once; the tensors' contents may change, the tables' among them.
 
     K, V [npages, page, d] with table [B, Hkv, max_pages] int32, or [npages, Hkv, page, d] with table [B, 1, max_pages]: in the KV type, or int8 or
-    float8_e4m3fn with k_scale and v_scale, float32, of the same shape without d."""
+    float8_e4m3fn with k_scale and v_scale, float32, of the same shape without d.  (As in Rotation: set anew or moved, a tensor is looked at again.)"""
+
+    K, V, table, k_scale, v_scale = (_watched(x) for x in ("K", "V", "table", "k_scale", "v_scale"))
 
     def __init__(self, desc, K, V, table, k_scale=None, v_scale=None):
         if table.dim() != 3 or K.dim() not in (3, 4) or K.shape != V.shape or K.dtype != V.dtype:
@@ -558,16 +577,17 @@ class Pages:
     def _bind(self, desc, device):
         if (desc.B, desc.Hkv, desc.d, desc.kv_dtype) != self._of:
             raise ValueError("pages: made for another descriptor")
-        seen = (device, self.K.data_ptr(), self.V.data_ptr(), self.table.data_ptr(), 0 if self.k_scale is None else self.k_scale.data_ptr(),
-                0 if self.v_scale is None else self.v_scale.data_ptr())
-        if seen != self._seen:      # (as in Rotation)
-            n, c = self.K.numel(), self.c
+        K, V, t, ks, vs = self._K, self._V, self._table, self._k_scale, self._v_scale
+        seen = (device, K.data_ptr(), K.dtype, V.data_ptr(), V.dtype, t.data_ptr(), t.dtype, None if ks is None else (ks.data_ptr(), ks.dtype),
+                None if vs is None else (vs.data_ptr(), vs.dtype))
+        if seen != self._seen:
+            n, c = K.numel(), self.c
             self._seen = None
-            c.K, c.V = _dev(self.K, n, self.types, "K", device), _dev(self.V, n, self.types, "V", device)
-            c.k_scale = _dev(self.k_scale, n // desc.d, _F4, "k_scale", device)
-            c.v_scale = _dev(self.v_scale, n // desc.d, _F4, "v_scale", device)
-            c.table = _dev(self.table, self.tables * c.max_pages, _I32, "table", device)
-            self._seen = seen
+            c.K, c.V = _dev(K, n, self.types, "K", device), _dev(V, n, self.types, "V", device)
+            c.k_scale = _dev(ks, n // desc.d, _F4, "k_scale", device)
+            c.v_scale = _dev(vs, n // desc.d, _F4, "v_scale", device)
+            c.table = _dev(t, self.tables * c.max_pages, _I32, "table", device)
+            self._held, self._seen = tuple(_memory(x) for x in (K, V, t, ks, vs)), seen
         return ctypes.byref(self.c)
 
 

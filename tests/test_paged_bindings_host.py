@@ -1,0 +1,124 @@
+"""What Rotation, Pages and PagedState keep of the tensors that they are given: nothing that another call's tensors could be taken for.  On CPU memory
+(device -1), which is looked at as device memory is; nothing is launched."""
+import pytest
+import torch
+
+from paper_2404_15949_amd import corm
+
+
+def _desc(**kw):
+    base = dict(B=2, Hq=8, Hkv=2, d=128, Lcap=1024, Tcap=1024, w=16, r=16, kv_dtype="bf16")
+    base.update(kw)
+    return corm.make_desc(**base)
+
+
+def _rotation(**kw):
+    base = dict(inv_freq=torch.ones(64), q_norm=torch.ones(128, dtype=torch.bfloat16), k_norm=torch.ones(128, dtype=torch.bfloat16))
+    base.update(kw)
+    return corm.Rotation(**base)
+
+
+def _bound(x, desc=None):
+    """Addresses as the call gets them"""
+    x._bind(_desc() if desc is None else desc, -1)
+    return {k: getattr(x.c, k) for k in (("inv_freq", "q_norm", "k_norm") if isinstance(x, corm.Rotation) else ("K", "V", "table", "k_scale", "v_scale"))}
+
+
+@pytest.mark.parametrize("name", ["q_norm", "k_norm"])
+def test_weights_that_became_another_type_in_the_same_memory(name):
+    r = _rotation()
+    _bound(r)
+    w = getattr(r, name)
+    w.data = w.data.view(torch.float16)
+    with pytest.raises(ValueError):
+        _bound(r)
+    with pytest.raises(ValueError):                                  # nor by the second call
+        _bound(r)
+    w.data = w.data.view(torch.bfloat16)
+    assert _bound(r)[name] == w.data_ptr()
+
+
+@pytest.mark.parametrize("name", ["inv_freq", "q_norm", "k_norm"])
+def test_other_weights_at_the_same_address(name):
+    r = _rotation()
+    _bound(r)
+    w = getattr(r, name)
+    wide = torch.ones(2 * w.numel(), dtype=w.dtype)
+    setattr(r, name, wide[:w.numel()])
+    assert _bound(r)[name] == wide.data_ptr()
+    for bad in (wide[::2], wide[:w.numel() // 2], wide):
+        assert bad.data_ptr() == wide.data_ptr()
+        setattr(r, name, bad)
+        with pytest.raises(ValueError):
+            _bound(r)
+    setattr(r, name, None)
+    if name == "inv_freq":
+        assert _bound(r)[name] is None                               # (the library refuses the call)
+    else:
+        assert _bound(r)[name] is None
+        new = torch.ones(128, dtype=torch.bfloat16)
+        setattr(r, name, new)
+        assert _bound(r)[name] == new.data_ptr()
+
+
+def test_weights_that_moved():
+    """Other memory of the same parameter is looked at and taken; the old memory is nobody else's before that."""
+    r = _rotation()
+    w = torch.nn.Parameter(torch.ones(128, dtype=torch.bfloat16))
+    r.q_norm = w
+    at = _bound(r)["q_norm"]
+    w.data = w.data.float()
+    others = [torch.zeros(128, dtype=torch.bfloat16) for _ in range(200)]
+    assert at not in [x.data_ptr() for x in others]
+    with pytest.raises(ValueError):                                  # float32 now
+        _bound(r)
+    w.data = w.data.to(torch.bfloat16)
+    assert _bound(r)["q_norm"] == w.data_ptr()
+
+
+def _pages(code=None, pool=12, desc=None, per_head=False):
+    d = _desc() if desc is None else desc
+    shape = (pool,) + (() if per_head else (d.Hkv,)) + (16, d.d)
+    K, V = (torch.zeros(shape, dtype=torch.int8 if code else torch.bfloat16) for _ in range(2))
+    sc = [torch.zeros(shape[:-1]) for _ in range(2)] if code else [None, None]
+    return corm.Pages(d, K, V, torch.zeros(d.B, d.Hkv if per_head else 1, 64, dtype=torch.int32), *sc)
+
+
+def test_pools_of_another_type_or_layout_at_the_same_address():
+    for name in ("K", "V"):
+        p = _pages()
+        _bound(p)
+        x = getattr(p, name)
+        x.data = x.data.view(torch.float16)
+        with pytest.raises(ValueError):
+            _bound(p)
+        p = _pages()
+        _bound(p)
+        setattr(p, name, getattr(p, name).transpose(1, 2))
+        with pytest.raises(ValueError):
+            _bound(p)
+    for name in ("k_scale", "v_scale"):
+        p = _pages("i8")
+        _bound(p)
+        x = getattr(p, name)
+        x.data = x.data.view(torch.int32)
+        with pytest.raises(ValueError):
+            _bound(p)
+        setattr(p, name, torch.zeros(12, 2, 32)[..., ::2])
+        with pytest.raises(ValueError):
+            _bound(p)
+
+
+def test_a_table_that_became_a_view_of_a_wider_one():
+    big = torch.zeros(2, 1, 200, dtype=torch.int32)
+    p = _pages()
+    p.table = big[:, :, :64].contiguous()
+    _bound(p)
+    p.table = big[:, :, :64]
+    with pytest.raises(ValueError):
+        _bound(p)
+    p = corm.Pages(_desc(), p.K, p.V, big)
+    _bound(p)
+    p.table = big[:, :, :64]                                         # the same address
+    with pytest.raises(ValueError):
+        _bound(p)
