@@ -560,19 +560,25 @@ class Pages:
     K, V, table, k_scale, v_scale = (_watched(x) for x in ("K", "V", "table", "k_scale", "v_scale"))
 
     def __init__(self, desc, K, V, table, k_scale=None, v_scale=None):
+        self._of = (desc.B, desc.Hkv, desc.d, desc.kv_dtype)
+        self._K, self._V, self._table, self._k_scale, self._v_scale = K, V, table, k_scale, v_scale
+        self.c = corm_pages()
+        self._seen = None
+        self._sizes()
+
+    def _sizes(self) -> None:
+        """What the tensors' shapes and types say."""
+        K, V, table = self._K, self._V, self._table
+        B, Hkv, d, kv = self._of
         if table.dim() != 3 or K.dim() not in (3, 4) or K.shape != V.shape or K.dtype != V.dtype:
             raise ValueError(f"pages: K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}, table {tuple(table.shape)}")
-        _, _, _, kv = _sizes(desc)
-        code = _code_ids.get(K.dtype)
-        self.K, self.V, self.table, self.k_scale, self.v_scale = K, V, table, k_scale, v_scale
-        self.types = kv if code is None else (K.dtype,)
         shared = K.dim() == 4
-        if tuple(K.shape[1:]) != ((desc.Hkv,) if shared else ()) + (K.shape[-2], desc.d) or tuple(table.shape[:2]) != (desc.B, 1 if shared else desc.Hkv):
-            raise ValueError(f"pages: K {tuple(K.shape)} and table {tuple(table.shape)} are not those of B {desc.B}, Hkv {desc.Hkv}, d {desc.d}")
-        self._of = (desc.B, desc.Hkv, desc.d, desc.kv_dtype)
-        self.tables = desc.B * table.shape[1]
-        self.c = corm_pages(desc.kv_dtype if code is None else code, K.shape[-2], K.shape[0], table.shape[2], table.shape[1], 0)
-        self._seen = None
+        if tuple(K.shape[1:]) != ((Hkv,) if shared else ()) + (K.shape[-2], d) or tuple(table.shape[:2]) != (B, 1 if shared else Hkv):
+            raise ValueError(f"pages: K {tuple(K.shape)} and table {tuple(table.shape)} are not those of B {B}, Hkv {Hkv}, d {d}")
+        code, c = _code_ids.get(K.dtype), self.c
+        self.types = (_FLOATS.get(kv) if code is None else K.dtype,)
+        self.tables = B * table.shape[1]
+        c.dtype, c.page, c.npages, c.max_pages, c.table_heads = kv if code is None else code, K.shape[-2], K.shape[0], table.shape[2], table.shape[1]
 
     def _bind(self, desc, device):
         if (desc.B, desc.Hkv, desc.d, desc.kv_dtype) != self._of:
@@ -581,8 +587,9 @@ class Pages:
         seen = (device, K.data_ptr(), K.dtype, V.data_ptr(), V.dtype, t.data_ptr(), t.dtype, None if ks is None else (ks.data_ptr(), ks.dtype),
                 None if vs is None else (vs.data_ptr(), vs.dtype))
         if seen != self._seen:
-            n, c = K.numel(), self.c
             self._seen = None
+            self._sizes()
+            n, c = K.numel(), self.c
             c.K, c.V = _dev(K, n, self.types, "K", device), _dev(V, n, self.types, "V", device)
             c.k_scale = _dev(ks, n // desc.d, _F4, "k_scale", device)
             c.v_scale = _dev(vs, n // desc.d, _F4, "v_scale", device)

@@ -122,3 +122,39 @@ def test_a_table_that_became_a_view_of_a_wider_one():
     p.table = big[:, :, :64]                                         # the same address
     with pytest.raises(ValueError):
         _bound(p)
+
+
+def _sizes(p):
+    _bound(p)
+    return p.c.npages, p.c.page, p.c.max_pages, p.c.table_heads, p.tables
+
+
+def test_pools_and_tables_of_other_sizes():
+    """The sizes that a call goes by are those of the tensors that it reads: page numbers beyond a smaller pool are none."""
+    p = _pages()
+    assert _sizes(p) == (12, 16, 64, 1, 2)
+    p.K, p.V = (torch.zeros(5, 2, 16, 128, dtype=torch.bfloat16) for _ in range(2))
+    assert _sizes(p) == (5, 16, 64, 1, 2)
+    p.K, p.V = (torch.zeros(5, 2, 32, 128, dtype=torch.bfloat16) for _ in range(2))
+    assert _sizes(p) == (5, 32, 64, 1, 2)
+    p.table = torch.zeros(2, 1, 200, dtype=torch.int32)
+    assert _sizes(p) == (5, 32, 200, 1, 2)
+    p.K.data, p.V.data = (torch.zeros(3, 2, 16, 128, dtype=torch.bfloat16) for _ in range(2))      # the same tensors, moved
+    assert _sizes(p) == (3, 16, 200, 1, 2)
+    p.table = torch.zeros(2, 2, 64, dtype=torch.int32)                                              # a table for each head of a pool shared by them
+    with pytest.raises(ValueError):
+        _bound(p)
+    p.K, p.V = (torch.zeros(7, 16, 128, dtype=torch.bfloat16) for _ in range(2))
+    assert _sizes(p) == (7, 16, 64, 2, 4)
+    p.K = torch.zeros(8, 16, 128, dtype=torch.bfloat16)
+    with pytest.raises(ValueError):
+        _bound(p)
+    with pytest.raises(ValueError):                                                                 # nor by the second call
+        _bound(p)
+    p.K, p.V = (torch.zeros(7, 16, 128, dtype=torch.int8) for _ in range(2))                        # codes, once there are scales for them
+    assert p._bind(_desc(), -1) and (p.c.dtype, p.c.k_scale) == (corm.CORM_I8, None)                # (the library refuses the call)
+    p.k_scale, p.v_scale = (torch.zeros(7, 16) for _ in range(2))
+    assert _bound(p)["v_scale"] == p.v_scale.data_ptr()
+    p.k_scale = torch.zeros(6, 16)
+    with pytest.raises(ValueError):
+        _bound(p)
