@@ -949,9 +949,16 @@ class Q8State:
         self.attend(q, nsel, nlast, stream=stream)
 
 
+def _of_pages(name):
+    return property(lambda self: getattr(self.pages, name), lambda self, x: setattr(self.pages, name, x))
+
+
 class PagedState:
     """The device arrays of one layer's cache of pages, in the layouts corm.h documents.  The caller deals the pages: table [B, 1, max_pages], or
-    [B, Hkv, max_pages] with per_head, holds -1 (no page) until it is written (deal() gives every unit max_pages of its own)."""
+    [B, Hkv, max_pages] with per_head, holds -1 (no page) until it is written (deal() gives every unit max_pages of its own).  The pools, their scales and
+    the table are those of `pages`; set anew on either, they are the ones that the next call takes."""
+
+    K, V, table, k_scale, v_scale = (_of_pages(x) for x in ("K", "V", "table", "k_scale", "v_scale"))
 
     def __init__(self, B, Hq, Hkv, d, npages, max_pages, dtype, page=16, code=None, per_head=False, device="cuda",
                  workspace: Optional[torch.Tensor] = None):
@@ -962,13 +969,10 @@ class PagedState:
         self.B, self.Hq, self.Hkv, self.d, self.page, self.dtype, self.code = B, Hq, Hkv, d, page, tdt, code
         shape = (npages,) + (() if per_head else (Hkv,)) + (page, d)
         tables = Hkv if per_head else 1
-        self.K = torch.zeros(shape, dtype=torch.int8 if code else tdt, device=device).view(cdt)
-        self.V = torch.zeros(shape, dtype=torch.int8 if code else tdt, device=device).view(cdt)
-        self.k_scale = torch.zeros(shape[:-1], dtype=torch.float32, device=device) if code else None
-        self.v_scale = torch.zeros(shape[:-1], dtype=torch.float32, device=device) if code else None
-        self.table = torch.full((B, tables, max_pages), -1, dtype=torch.int32, device=device)
+        K, V = (torch.zeros(shape, dtype=torch.int8 if code else tdt, device=device).view(cdt) for _ in range(2))
+        ks, vs = (torch.zeros(shape[:-1], dtype=torch.float32, device=device) if code else None for _ in range(2))
+        self.pages = Pages(self.desc, K, V, torch.full((B, tables, max_pages), -1, dtype=torch.int32, device=device), ks, vs)
         self.lens = torch.zeros(B, tables, dtype=torch.int32, device=device)
-        self.pages = Pages(self.desc, self.K, self.V, self.table, self.k_scale, self.v_scale)
         self.q = torch.zeros(B, Hq, d, dtype=tdt, device=device)   # a step's queries, rotated
         self.out = torch.zeros(B, Hq, d, dtype=torch.float32, device=device)
         self.status = torch.zeros(1, dtype=torch.int32, device=device)

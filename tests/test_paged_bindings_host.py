@@ -158,3 +158,24 @@ def test_pools_and_tables_of_other_sizes():
     p.k_scale = torch.zeros(6, 16)
     with pytest.raises(ValueError):
         _bound(p)
+
+
+@pytest.mark.parametrize("code", [None, "i8"])
+def test_a_state_whose_tensors_are_set_anew(code):
+    """They are the ones that the calls take, whether they are set on the state or on its pages."""
+    st = corm.PagedState(2, 8, 2, 128, 7, 4, "bf16", code=code, device="cpu")
+    st.table = torch.arange(8, dtype=torch.int32).view(2, 1, 4)
+    st.K, st.V = (torch.zeros(9, 2, 16, 128, dtype=st.K.dtype) for _ in range(2))
+    if code:
+        st.k_scale, st.v_scale = (torch.ones(9, 2, 16) for _ in range(2))
+    for _ in range(2):
+        at = _bound(st.pages, st.desc)
+        for name, x in at.items():
+            assert x == (None if getattr(st, name) is None else getattr(st, name).data_ptr()), name
+        assert st.pages.c.npages == 9 and st.table.data_ptr() == st.pages.table.data_ptr()
+    st.deal()                                                        # nine pages: into the table that is there now
+    assert st.table.flatten().tolist() == list(range(8))
+    st.pages.table = torch.full((2, 1, 4), 3, dtype=torch.int32)
+    assert st.table is st.pages.table and _bound(st.pages, st.desc)["table"] == st.table.data_ptr()
+    st.table[0, 0, 1] = 5
+    assert st.pages.table[0, 0, 1] == 5
