@@ -366,7 +366,8 @@ int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int
  *
  * corm_rows: where a call finds its rows of queries, keys and values (kv_dtype), e.g. in the packed output of a projection
  * [B, n, (Hq + 2 Hkv) d].  Row of sequence b, token i, head h: base + b stride[0] + i stride[1] + h stride[2], in elements; the d
- * elements of a row lie together.  Bases 16-byte aligned, strides 0 .. 2^40 and whole multiples of 16 bytes.
+ * elements of a row lie together.  Bases 16-byte aligned, strides 0 .. 2^40 and whole multiples of 16 bytes, the last
+ * row within 2^62 bytes.
  *
  * corm_rotation: what queries and keys go through, all in fp32 and rounded once where they are stored:
  *   norm      y = x * weight / sqrt(mean of x^2 over the d channels + eps), per head, where q_norm (k_norm) [d], kv_dtype, is given (the squares'

@@ -64,13 +64,20 @@ int check_rotation(const corm_desc* d, const corm_rotation* r, const int32_t* po
   return sum == r->rot / 2 ? CORM_OK : CORM_EINVAL;
 }
 
-int check_rows(const corm_desc* d, const corm_rows* r, bool with_q) {
+int check_rows(const corm_desc* d, const corm_rows* r, int n, bool with_q) {
   if (!r || !r->k || !r->v || misaligned16(r->k) || misaligned16(r->v)) return CORM_EINVAL;
   if (with_q && (!r->q || misaligned16(r->q))) return CORM_EINVAL;
-  auto bad = [&](int64_t x) { return x < 0 || x > (1LL << 40) || x % (16 / elem_bytes(d)) != 0; };   // (more than any memory: offsets stay in 64 bits)
-  for (int i = 0; i < 3; ++i)
-    if (bad(r->k_stride[i]) || bad(r->v_stride[i]) || (with_q && bad(r->q_stride[i]))) return CORM_EINVAL;
-  return CORM_OK;
+  // strides: none is beyond any memory, and the last row's offset is well within 64 bits
+  auto bad = [&](const int64_t* s, int heads) {
+    const int rows[3] = {d->B, n, heads};
+    __int128 span = 0;
+    for (int i = 0; i < 3; ++i) {
+      if (s[i] < 0 || s[i] > (1LL << 40) || s[i] % (16 / elem_bytes(d)) != 0) return true;
+      span += (__int128)s[i] * (rows[i] - 1) * elem_bytes(d);
+    }
+    return span > ((__int128)1 << 62);
+  };
+  return bad(r->k_stride, d->Hkv) || bad(r->v_stride, d->Hkv) || (with_q && bad(r->q_stride, d->Hq)) ? CORM_EINVAL : CORM_OK;
 }
 
 RowStrides bytes_of(const int64_t* s, int esz) { return RowStrides{s[0] * esz, s[1] * esz, s[2] * esz}; }
@@ -152,7 +159,7 @@ int corm_rotate(const corm_desc* desc, const corm_rows* rows, const corm_rotatio
   if (rc) return rc;
   if (!rotation || !k_out || !v_out || misaligned16(q_out) || misaligned16(k_out) || misaligned16(v_out)) return CORM_EINVAL;
   if (n < 1 || misaligned4(n_new)) return CORM_EINVAL;
-  rc = check_rows(desc, rows, q_out != nullptr);
+  rc = check_rows(desc, rows, n, q_out != nullptr);
   if (rc) return rc;
   rc = check_rotation(desc, rotation, positions);
   if (rc) return rc;
@@ -173,7 +180,7 @@ int corm_paged_append(const corm_desc* desc, const corm_pages* pages, const corm
   if (!lens || !lens_out || misaligned4(lens) || misaligned4(lens_out) || misaligned4(status) || misaligned4(n_new) || misaligned16(q_out))
     return CORM_EINVAL;
   if (n < 1 || n > desc->Lcap) return CORM_EINVAL;
-  rc = check_rows(desc, rows, q_out != nullptr);
+  rc = check_rows(desc, rows, n, q_out != nullptr);
   if (rc) return rc;
   rc = check_rotation(desc, rotation, positions);
   if (rc) return rc;
