@@ -26,7 +26,7 @@ int elem_bytes(const corm_desc* d) { return d->kv_dtype == CORM_F32 ? 4 : 2; }
 bool in_codes(const corm_pages* p) { return p->dtype == CORM_I8 || p->dtype == CORM_E4M3; }
 
 int check_pages(const corm_desc* d, const corm_pages* p) {
-  if (!p || !p->K || !p->V || !p->table) return CORM_EINVAL;
+  if (!p || !p->K || !p->V || !p->table || p->reserved != 0) return CORM_EINVAL;
   if (!in_codes(p) && p->dtype != d->kv_dtype) return CORM_EUNSUPPORTED;
   if (misaligned16(p->K) || misaligned16(p->V) || misaligned4(p->table)) return CORM_EINVAL;
   if (in_codes(p) && (!p->k_scale || !p->v_scale || misaligned16(p->k_scale) || misaligned16(p->v_scale))) return CORM_EINVAL;

@@ -1,4 +1,6 @@
-"""Strides of rows on their way into a cache whose offsets leave 64 bits: refused on the host."""
+"""More refusals of the calls over pages, on the host: strides of rows whose offsets leave 64 bits, fields that have to be 0."""
+import pytest
+
 from paper_2404_15949_amd import corm
 from tests import test_paged_host as host
 
@@ -28,3 +30,10 @@ def test_strides_of_a_prompt_in_pages():
     d = host._desc(Lcap=1 << 21, kv_dtype="f32")
     pages = host._pages(dtype=corm.CORM_F32, max_pages=1 << 17)
     assert host._call("corm_paged_append", d, pages=pages, n=1 << 21, rows=host._rows(k_stride=(768, 1 << 40, 128))) == corm.CORM_EINVAL
+
+
+@pytest.mark.parametrize("name", [n for n in host.CALLS if "pages" in host.CALLS[n][0]])
+def test_reserved_fields_are_zero(name):
+    for x in (1, -1, 1 << 30):
+        assert host._call(name, pages=host._pages(reserved=x)) == corm.CORM_EINVAL, x
+    assert host._call("corm_paged_attend", pages=host._pages()) == corm.CORM_ECAPACITY       # 16 bytes of workspace: fine but for that
