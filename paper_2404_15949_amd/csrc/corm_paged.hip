@@ -125,7 +125,7 @@ int launch_rows(const corm_desc* d, RowsArgs& a, hipStream_t s) {
   return d->d == 64 ? launch_rows_d<C, BF16, 64>(a, s) : launch_rows_d<C, BF16, 128>(a, s);
 }
 
-// Workgroups that share all units' tiles, at most, or of few short units, twice as many; a shared one has two partials.
+// Workgroups that the workspace has room for, two partials each (of those that share all units' tiles; a round's workgroup of a short unit has one).
 constexpr int PAGED_MOST = 1024;
 struct PagedWorkspace {
   size_t parts_off, total;
@@ -136,6 +136,29 @@ PagedWorkspace paged_workspace(const corm_desc* d) {
   w.total = align_up(w.parts_off + (size_t)d->B * d->Hkv * sizeof(int2), 256);
   return w;
 }
+
+// How the tiles of a call are dealt out to workgroups.
+// A workgroup takes a whole unit where there are two units per compute unit, or one and they are short, or where they are very short; units whose rounds
+// all fit the chip at once get a workgroup for each; else all units' tiles are shared out.  Us, bf16, d 128, four heads a unit, rounds of 128 slots:
+//   whole | shared           256 units x 760, 1500 and 4096 slots 20.0 | 25.3, 34.8 | 42.4 and 84.7 | 90.9; 384 x 760 and 4096 32.2 | 37.1 and 149 | 132;
+//                            320 x 0 .. 1500 and 1000 .. 6000 44.8 | 50.3 and 157 | 100; 512 x 548 .. 2048 67 | 71
+//   whole | one each, merged 8 x 250, 380 and 510 6.9 | 8.4, 7.9 | 8.2 and 9.4 | 8.4; 128 x 380 10.9 | 13.3
+//   shared | units in equal parts, whatever their lengths   128 x 4192 .. 8192 73 | 77, x 0 .. 16384 102 | 120, x 4096 51 | 50; 8 x 131072 int8 55 | 53
+constexpr int PAGED_CUS = 256;   // compute units that the rule goes by, at most
+struct Deal {
+  bool shared;
+  int npart;        // not shared: workgroups of a unit, one or one for each round over its waves
+  int workgroups;   // shared: of all units
+};
+constexpr Deal deal_out(long units, long rounds, long cus) {   // rounds: of a unit as long as the lengths' bound allows
+  const bool alone = units >= 2 * cus || (units >= cus && rounds <= 16) || rounds <= 3;
+  const bool shared = !alone && units * rounds > 2 * cus;
+  return Deal{shared, alone || shared ? 1 : (int)rounds, (int)(2 * cus)};
+}
+// Units that are not dealt out whole are fewer than 2 PAGED_CUS, and those with parts have no more than so many of them: a workgroup can add the tables up, the
+// workspace holds the partials, and 32 bits count the tiles (of units of less than 2^31 / 512 slots).
+static_assert(2 * PAGED_CUS <= SHARE_TABLES && 2 * PAGED_CUS <= PAGED_MOST, "");
+static_assert(2L * PAGED_CUS * ((1L << 31) / 512 / PoolF32::TILE + 2 * WAVES) + 2 * PAGED_CUS < 2147483647L, "");
 
 // kernel<pool, query type, d> by the call's types
 template <typename F>
@@ -244,18 +267,10 @@ int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void
   a.scale_log2 = (desc->sm_scale > 0.f ? desc->sm_scale : 1.0f / sqrtf((float)desc->d)) * LOG2E;
   a.units = desc->B * desc->Hkv;
   const int tile = in_codes(pages) ? PoolI8::TILE : desc->kv_dtype == CORM_F32 ? PoolF32::TILE : PoolBF16::TILE;
-  const long units = a.units, cus = device_cus(), rounds = ((desc->Lcap + tile - 1) / tile + WAVES - 1) / WAVES;   // of a unit, at most
+  const Deal deal = deal_out(a.units, ((desc->Lcap + tile - 1) / tile + WAVES - 1) / WAVES, std::min(device_cus(), PAGED_CUS));
   a.tables = desc->B * pages->table_heads;
-  a.workgroups = (int)std::min<long>(PAGED_MOST, 2 * cus);
-  // A workgroup takes a whole unit where there are two units per compute unit, or one and they are short, or where they are very short; units whose rounds
-  // all fit the chip at once get a workgroup for each; else all units' tiles are shared out.  Us, bf16, d 128, four heads a unit, rounds of 128 slots:
-  //   whole | shared           256 units x 760, 1500 and 4096 slots 20.0 | 25.3, 34.8 | 42.4 and 84.7 | 90.9; 384 x 760 and 4096 32.2 | 37.1 and 149 | 132;
-  //                            320 x 0 .. 1500 and 1000 .. 6000 44.8 | 50.3 and 157 | 100; 512 x 548 .. 2048 67 | 71
-  //   whole | one each, merged 8 x 250, 380 and 510 6.9 | 8.4, 7.9 | 8.2 and 9.4 | 8.4; 128 x 380 10.9 | 13.3
-  //   shared | units in equal parts, whatever their lengths   128 x 4192 .. 8192 73 | 77, x 0 .. 16384 102 | 120, x 4096 51 | 50; 8 x 131072 int8 55 | 53
-  const bool alone = units >= 2 * cus || (units >= cus && rounds <= 16) || rounds <= 3;
-  const bool shared = !alone && units * rounds > a.workgroups && a.tables <= SHARE_TABLES && units * rounds * WAVES < 2147483647L;
-  a.npart = alone ? 1 : (int)std::min<long>({rounds, (a.workgroups + units - 1) / units, 2 * PAGED_MOST / units});
+  a.workgroups = deal.workgroups;
+  a.npart = deal.npart;
   hipStream_t s = (hipStream_t)stream;
   auto merge = [&](auto shared_, int parts) {
     constexpr bool SHARED = decltype(shared_)::value;
@@ -265,14 +280,14 @@ int corm_paged_attend(const corm_desc* desc, const corm_pages* pages, const void
     else many ? launch(corm_paged_merge_kernel<128, SHARED, 1024>) : launch(corm_paged_merge_kernel<128, SHARED, 256>);
     return launch_status();
   };
-  if (shared) {
+  if (deal.shared) {
     rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
       hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, true>), dim3(a.workgroups), dim3(WG), 0, s, a);
       return launch_status();
     });
-    return rc ? rc : merge(std::true_type(), (int)(a.workgroups / units) + 2);
+    return rc ? rc : merge(std::true_type(), a.workgroups / a.units + 2);
   }
-  const long groups = (units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
+  const long groups = ((long)a.units * a.npart + Q8_XCDS - 1) / Q8_XCDS * Q8_XCDS;
   rc = by_pool(desc, pages, [&](auto pool, auto dt, auto dd) {
     hipLaunchKernelGGL((corm_paged_attend_kernel<decltype(pool), decltype(dt), decltype(dd)::value, false>), dim3((unsigned)groups), dim3(WG), 0, s, a);
     return launch_status();

@@ -207,8 +207,8 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, int wg, int tile_s
   return s;
 }
 
-// SHARED: a workgroup has a run of tiles, which may begin and end inside units (its segments); else the npart workgroups of a unit take its tiles in turn, a
-// wave at a time, so that a wave's first tile does not depend on the length and its page is looked up while that is on its way.
+// SHARED: a workgroup has a run of tiles, which may begin and end inside units (its segments); else a unit has one workgroup, or one for each round over its
+// waves (npart), so that a wave's first tile does not depend on the length and its page is looked up while that is on its way.
 //
 // A tile is TILE slots; the lanes of group lg = l / 16 work for its slots GROUP*lg .. +GROUP (GROUP = TILE / 4 slots, which lie in one page).
 // S^T = K q^T: A = 16 keys x 32 channels (fp32: x 4) of rows as they lie, B = the heads in columns 0 .. G-1.  Row m of product t is key
