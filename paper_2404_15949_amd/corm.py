@@ -532,6 +532,8 @@ class Rotation:
         sections = [half] if sections is None else [operator.index(x) for x in sections]
         if not 1 <= len(sections) <= 4:
             raise ValueError(f"sections: one to four axes, got {len(sections)}")
+        if min(sections) < 0 or max(sections) > half:   # (the structure's integers would keep the lower 32 bits)
+            raise ValueError(f"sections: {sections} of {half} pairs")
         self.inv_freq, self.q_norm, self.k_norm, self.axes, self.rot = inv_freq, q_norm, k_norm, len(sections), 2 * half
         self.c = corm_rotation(2 * half, {"halves": CORM_HALVES, "neighbours": CORM_NEIGHBOURS}[pairing], len(sections), int(bool(in_turn)),
                                tuple(sections), eps, gain)

@@ -179,3 +179,12 @@ def test_a_state_whose_tensors_are_set_anew(code):
     assert st.table is st.pages.table and _bound(st.pages, st.desc)["table"] == st.table.data_ptr()
     st.table[0, 0, 1] = 5
     assert st.pages.table[0, 0, 1] == 5
+
+
+def test_sections_that_no_structure_holds():
+    for bad in ([2 ** 32 + 64], [64 - 2 ** 32, 0], [2 ** 31, 64], [65], [-1, 65]):
+        with pytest.raises(ValueError):
+            corm.Rotation(torch.ones(64), sections=bad)
+    with pytest.raises(ValueError):
+        corm.Rotation(None, sections=[2 ** 32])
+    assert list(corm.Rotation(torch.ones(64), sections=[40, 0, 24]).c.section) == [40, 0, 24, 0]
