@@ -563,24 +563,25 @@ class Pages:
 
     def __init__(self, desc, K, V, table, k_scale=None, v_scale=None):
         self._of = (desc.B, desc.Hkv, desc.d, desc.kv_dtype)
+        self.sizes = (desc.B, desc.Hkv, desc.d, (_FLOATS.get(desc.kv_dtype),))   # of the descriptor that every call's is like, and the KV type
         self._K, self._V, self._table, self._k_scale, self._v_scale = K, V, table, k_scale, v_scale
         self.c = corm_pages()
         self._seen = None
-        self._sizes()
+        self._look()
 
-    def _sizes(self) -> None:
+    def _look(self) -> None:
         """What the tensors' shapes and types say."""
         K, V, table = self._K, self._V, self._table
-        B, Hkv, d, kv = self._of
+        B, Hkv, d, kv = self.sizes
         if table.dim() != 3 or K.dim() not in (3, 4) or K.shape != V.shape or K.dtype != V.dtype:
             raise ValueError(f"pages: K {tuple(K.shape)} {K.dtype}, V {tuple(V.shape)} {V.dtype}, table {tuple(table.shape)}")
         shared = K.dim() == 4
         if tuple(K.shape[1:]) != ((Hkv,) if shared else ()) + (K.shape[-2], d) or tuple(table.shape[:2]) != (B, 1 if shared else Hkv):
             raise ValueError(f"pages: K {tuple(K.shape)} and table {tuple(table.shape)} are not those of B {B}, Hkv {Hkv}, d {d}")
         code, c = _code_ids.get(K.dtype), self.c
-        self.types = (_FLOATS.get(kv) if code is None else K.dtype,)
+        self.types = kv if code is None else (K.dtype,)
         self.tables = B * table.shape[1]
-        c.dtype, c.page, c.npages, c.max_pages, c.table_heads = kv if code is None else code, K.shape[-2], K.shape[0], table.shape[2], table.shape[1]
+        c.dtype, c.page, c.npages, c.max_pages, c.table_heads = self._of[3] if code is None else code, K.shape[-2], K.shape[0], table.shape[2], table.shape[1]
 
     def _bind(self, desc, device):
         if (desc.B, desc.Hkv, desc.d, desc.kv_dtype) != self._of:
@@ -590,7 +591,7 @@ class Pages:
                 None if vs is None else (vs.data_ptr(), vs.dtype))
         if seen != self._seen:
             self._seen = None
-            self._sizes()
+            self._look()
             n, c = K.numel(), self.c
             c.K, c.V = _dev(K, n, self.types, "K", device), _dev(V, n, self.types, "V", device)
             c.k_scale = _dev(ks, n // desc.d, _F4, "k_scale", device)
@@ -643,24 +644,23 @@ def corm_paged_append(desc, pages, k, v, lens, lens_out, n_new=None, q=None, q_o
     turn = pos = None
     if rotation is not None:
         turn, pos = rotation._bind(desc, at), _dev(positions, rotation.axes * desc.B * n, _I32, "positions", at)
-    rc = lib().corm_paged_append(ctypes.byref(desc), pages._bind(desc, at), ctypes.byref(rows), turn, pos, n,
-                                 _dev(n_new, desc.B, _I32, "n_new", at),
-                                 _dev(q_out, desc.B * desc.Hq * n * desc.d, (_FLOATS.get(desc.kv_dtype),), "q_out", at),
-                                 _dev(lens, pages.tables, _I32, "lens", at), _dev(lens_out, pages.tables, _I32, "lens_out", at),
-                                 _dev(status, None, _I32, "status", at), _on(stream, at))
+    of = pages._bind(desc, at)
+    B, _, d, kv = pages.sizes
+    rc = lib().corm_paged_append(ctypes.byref(desc), of, ctypes.byref(rows), turn, pos, n, _dev(n_new, B, _I32, "n_new", at),
+                                 _dev(q_out, B * desc.Hq * n * d, kv, "q_out", at), _dev(lens, pages.tables, _I32, "lens", at),
+                                 _dev(lens_out, pages.tables, _I32, "lens_out", at), _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_paged_append") if check else rc
 
 
 def corm_paged_read(desc, pages, lens, K_out, V_out, status=None, stream=None, check=True) -> int:
     """K_out, V_out [B,Hkv,n,d]"""
     at = _device()
-    units, _, _, kv = _sizes(desc)
     if K_out.dim() != 4 or K_out.shape != V_out.shape:
         raise ValueError(f"K_out {tuple(K_out.shape)}, V_out {tuple(V_out.shape)}: expected [B, Hkv, n, d]")
-    n = K_out.shape[2]
-    rc = lib().corm_paged_read(ctypes.byref(desc), pages._bind(desc, at), _dev(lens, pages.tables, _I32, "lens", at), n,
-                               _dev(K_out, units * n * desc.d, kv, "K_out", at), _dev(V_out, units * n * desc.d, kv, "V_out", at),
-                               _dev(status, None, _I32, "status", at), _on(stream, at))
+    of, n = pages._bind(desc, at), K_out.shape[2]
+    B, Hkv, d, kv = pages.sizes
+    rc = lib().corm_paged_read(ctypes.byref(desc), of, _dev(lens, pages.tables, _I32, "lens", at), n, _dev(K_out, B * Hkv * n * d, kv, "K_out", at),
+                               _dev(V_out, B * Hkv * n * d, kv, "V_out", at), _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_paged_read") if check else rc
 
 
@@ -676,10 +676,12 @@ def corm_paged_workspace_bytes(desc: corm_desc, check=True) -> int:
 def corm_paged_attend(desc, pages, q, lens, out, workspace, workspace_bytes=None, status=None, stream=None, check=True) -> int:
     """q [B,Hq,d] -> out [B,Hq,d] float32"""
     at = _device()
-    heads, kv = desc.B * desc.Hq, _sizes(desc)[3]
-    rc = lib().corm_paged_attend(ctypes.byref(desc), pages._bind(desc, at), _dev(q, heads * desc.d, kv, "q", at),
-                                 _dev(lens, pages.tables, _I32, "lens", at), _dev(out, heads * desc.d, _F4, "out", at), _scratch(workspace, at),
-                                 _nbytes(workspace, workspace_bytes), _dev(status, None, _I32, "status", at), _on(stream, at))
+    of = pages._bind(desc, at)
+    B, _, d, kv = pages.sizes
+    heads = B * desc.Hq
+    rc = lib().corm_paged_attend(ctypes.byref(desc), of, _dev(q, heads * d, kv, "q", at), _dev(lens, pages.tables, _I32, "lens", at),
+                                 _dev(out, heads * d, _F4, "out", at), _scratch(workspace, at), _nbytes(workspace, workspace_bytes),
+                                 _dev(status, None, _I32, "status", at), _on(stream, at))
     return _check(rc, "corm_paged_attend") if check else rc
 
 
