@@ -371,7 +371,7 @@ int corm_evict_mask_weight(const corm_desc* desc, const float* weight, const int
  *
  * corm_rotation: what queries and keys go through, all in fp32 and rounded once where they are stored:
  *   norm      y = x * weight / sqrt(mean of x^2 over the d channels + eps), per head, where q_norm (k_norm) [d], kv_dtype, is given (the squares'
- *             sum is fp32: rows of elements beyond 10^18 have none)
+ *             sum is fp32: rows of elements beyond 10^18 come out as zeros, and with eps = 0 rows of elements below 10^-18 may lose bits, or not be numbers)
  *   rotation  of the first rot channels, rot / 2 pairs: pair i is turned by the angle positions[axis(i)][b][token] * inv_freq[i], formed in
  *             64 bits:  (u, v) -> gain * (u cos - v sin, v cos + u sin).  CORM_HALVES: pair i is channels i and i + rot / 2;
  *             CORM_NEIGHBOURS: 2i and 2i + 1.  Channels at and above rot are normed only, values go as they are.
@@ -406,7 +406,8 @@ int corm_rotate(const corm_desc* desc, const corm_rows* rows, const corm_rotatio
  *   table_heads = 1     the KV heads of a sequence share a table and a length: table [B, 1, max_pages], lens [B, 1],
  *                       K, V [npages, Hkv, page, d]
  *   table_heads = Hkv   every KV head has its own, as eviction per head leaves them: table [B, Hkv, max_pages], lens [B, Hkv],
- *                       K, V [npages, page, d]
+ *                       K, V [npages, page, d].  (An append brings all heads of a sequence equally many rows, lengths that differ are the caller's
+ *                       to write: rows at and above a length are not seen.)
  *   dtype   kv_dtype: rows as they are.  CORM_I8, CORM_E4M3: codes with a scale per row, k_scale and v_scale (16-byte aligned) float32,
  *           laid out as K and V without d; with amax the largest magnitude of the row's elements (fp32, before any rounding) and Q = 127 or 448
  *             scale = fp32(amax / Q);  code = x * fp32(Q / amax) in fp32, rounded to the nearest (even) integer / e4m3 (OCP) value
@@ -438,6 +439,7 @@ int corm_paged_read(const corm_desc* desc, const corm_pages* pages, const int32_
 /* Decode attention (Eq. 1) over the slots < lens: q [B, Hq, d] kv_dtype, out [B, Hq, d] float32, 0 where a unit has no slot that can be read.
  * (A row whose scale is none makes the outputs over it none.)  Sums are fp32, no weight in them is above 1: outputs are finite where the sum of the magnitudes of
  * a channel's values is.  A value that is seen and not a number makes its channel of the outputs none, an infinite one (of a weight above 2^-90) infinite.
+ * Over codes a logit is formed from the codes before their scale: sums of |q| times 127 or 448 have to be within fp32.
  * Workspace (256-byte aligned, of corm_paged_workspace_bytes): partials and where they
  * lie; nothing in it has to be prepared or survives a call, so calls on one stream, and graphs that are replayed one after the other, may share it. */
 int corm_paged_workspace_bytes(const corm_desc* desc, size_t* bytes);

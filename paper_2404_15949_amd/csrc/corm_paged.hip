@@ -139,11 +139,13 @@ PagedWorkspace paged_workspace(const corm_desc* d) {
 
 // How the tiles of a call are dealt out to workgroups.
 // A workgroup takes a whole unit where there are two units per compute unit, or one and they are short, or where they are very short; units whose rounds
-// all fit the chip at once get a workgroup for each; else all units' tiles are shared out.  Us, bf16, d 128, four heads a unit, rounds of 128 slots:
+// all fit the chip at once get a workgroup for each; else all units' tiles are shared out.  The host knows the bound of the lengths, not the lengths: of two units
+// per compute unit and more, one that is far longer than the others holds the call up (64 sequences of 8 heads, one of 131072 slots and 63 of 500: 1750 us, where 63
+// such sequences, whose tiles are shared out, take 120).  Us, bf16, d 128, four heads a unit, rounds of 128 slots:
 //   whole | shared           256 units x 760, 1500 and 4096 slots 20.0 | 25.3, 34.8 | 42.4 and 84.7 | 90.9; 384 x 760 and 4096 32.2 | 37.1 and 149 | 132;
 //                            320 x 0 .. 1500 and 1000 .. 6000 44.8 | 50.3 and 157 | 100; 512 x 548 .. 2048 67 | 71
 //   whole | one each, merged 8 x 250, 380 and 510 6.9 | 8.4, 7.9 | 8.2 and 9.4 | 8.4; 128 x 380 10.9 | 13.3
-//   shared | units in equal parts, whatever their lengths   128 x 4192 .. 8192 73 | 77, x 0 .. 16384 102 | 120, x 4096 51 | 50; 8 x 131072 int8 55 | 53
+//   shared | units in equal parts, whatever their lengths   128 x 4192 .. 8192 73 | 77, x 0 .. 16384 102 | 120, x 4096 51 | 50; 8 x 131072 int8 55 | 53 (each pair on one card)
 constexpr int PAGED_CUS = 256;   // compute units that the rule goes by, at most
 struct Deal {
   bool shared;

@@ -219,10 +219,12 @@ __device__ __forceinline__ Share share_of(const PagedArgs& a, int wg, int tile_s
 // each, without loss, so everything is exact but for the sums, which are fp32.
 //
 // Bound by HBM: 16 x 32 units of 3352 .. 4352 bf16 slots, d 128, 162 us (6.2 TB/s), vector ALU 14 % and matrix cores 8 % busy (8 int8 units of 131072: 44 and
-// 12 %).  Tiles of 32 slots for codes: 64 take the registers of a third wave (512 int8 units x 8192 180 us | 198).  Sums fade in tiles that raise a
-// maximum: fading in every tile, where all lanes have to agree on it first, 63.4 us | 62.4 for int8 units of 131072; letting it fall short by up to 2^8, so that
-// hardly a tile raises it, gains nothing (66.6 | 65.7, others the same) and takes 2^8 from the range of the sums.  Two workgroups per compute unit have enough under way (shares of
-// 128 units of 4192 .. 8192 bf16 slots: one 72 us, two 74, three 78; of 8 int8 units of 131072 78, 56, 60).
+// 12 %).  What was compared, each pair one build beside the other on one card (the launch as it is takes 54 us of 8 int8 units of 131072 and 72 of 128 bf16
+// units of 4192 .. 8192 without a pause between the calls, single ones up to 67 and 90):
+//   tiles of 32 slots for codes | 64, which take the registers of a third wave: 512 int8 units x 8192 180 us | 198
+//   sums that fade in tiles that raise the maximum | that fade where it is 2^8 short, hardly ever: 8 int8 units of 131072 65.7 us | 66.6, others the same, and
+//   2^8 less range of the sums | that fade in every tile, where all lanes have to agree on the maximum first: 63.4, the second 62.4 beside it
+//   two workgroups per compute unit, one, three: shares of 128 units of 4192 .. 8192 bf16 slots 74, 72, 78; of 8 int8 units of 131072 56, 78, 60
 template <typename P, typename DT, int D, bool SHARED>
 __global__ __launch_bounds__(WG, 2) void corm_paged_attend_kernel(const PagedArgs a) {
   constexpr int TILE = P::TILE, GROUP = TILE / 4, T = GROUP / 4;
